@@ -478,6 +478,125 @@ int ee_pht_init(void* dev_row, void* stream);
  * skipped.  Enqueue only.  EE_ERR_INVALID_ARG on a null pointer or a batch of another model. */
 int ee_pht_push_step(void* dev_row, const ee_model* m, const ee_batch* b, void* stream);
 
+/* ------------------------------------------------------------------ rotary positions
+ *
+ * The layer calls above rotate whole heads in half-split pairs at unscaled frequencies, from the model's own table.  These
+ * calls are for everything else: both pairings, heads that rotate only in their leading part, frequencies scaled for contexts
+ * longer than the trained one, and the inverse (which is the rotation's gradient).
+ *
+ * With r = rot_dim and j < r/2, feature a of pair j is i = j (EE_ROPE_HALF; partner b = j + r/2) or i = 2j
+ * (EE_ROPE_INTERLEAVED; b = 2j + 1), and with the angle t = position * f_j:
+ *   y_a = x_a cos t - x_b sin t,   y_b = x_b cos t + x_a sin t      (inverse: -sin t);   features >= r are copied.
+ * Frequencies f_j = theta^(-2j/r), changed by
+ *   EE_ROPE_LINEAR  f_j / factor
+ *   EE_ROPE_BASE    theta replaced by theta * factor^(r/(r-2))  (r > 2): the slowest pair is stretched by factor, the fastest not
+ *   EE_ROPE_BANDS   f_j (w + (1 - w)/factor), w = clamp((n_j - low)/(high - low), 0, 1), n_j = trained_pos f_j / 2 pi: the turns
+ *                   pair j makes over the trained length; pairs of more than `high` turns stay, of fewer than `low` are stretched
+ * cos and sin are multiplied by `magnitude` (0 = 1).  They are computed in fp64 and kept as fp32 [max_pos][r/2][2]. */
+typedef enum { EE_ROPE_HALF = 0, EE_ROPE_INTERLEAVED = 1 } ee_rope_pairing;
+typedef enum { EE_ROPE_UNSCALED = 0, EE_ROPE_LINEAR = 1, EE_ROPE_BASE = 2, EE_ROPE_BANDS = 3 } ee_rope_scaling;
+typedef struct {
+    int32_t head_dim;
+    int32_t rot_dim;     /* r: even, 2 .. head_dim                                     */
+    int32_t pairing;     /* ee_rope_pairing                                            */
+    int32_t max_pos;     /* positions 0 .. max_pos-1                                   */
+    int32_t scaling;     /* ee_rope_scaling                                            */
+    int32_t trained_pos; /* EE_ROPE_BANDS: length the model was trained on             */
+    float   theta;       /* > 1                                                        */
+    float   factor;      /* > 0; not used by EE_ROPE_UNSCALED                          */
+    float   low, high;   /* EE_ROPE_BANDS: 0 <= low < high                             */
+    float   magnitude;   /* >= 0 and finite; 0 stands for 1                            */
+} ee_rope_config;
+typedef struct ee_rope ee_rope;
+
+/* Rows of heads: element (token t, head h, feature i) at dev + t * token_stride + h * head_stride + i, strides in elements.
+ * Any strides are taken; 16-byte aligned rows (base and strides) take the wide loads. */
+typedef struct {
+    void*   dev;
+    int64_t token_stride;
+    int64_t head_stride;
+} ee_heads;
+
+/* Set-up call: allocates the table and waits for the default stream.  The fp32 table takes max_pos * rot_dim * 4 bytes. */
+int ee_rope_create(const ee_rope_config* cfg, ee_rope** out);
+int ee_rope_destroy(ee_rope* r);
+/* Rotates n_heads heads of each of n_tokens rows at dev_pos[t]; x and y of type dtype (ee_dtype), computed in fp32.  y may be
+ * x itself (same strides), but must not overlap it otherwise.  A position outside the table: the row is not written and
+ * bit 1 of *dev_status (nullable) is set.  Enqueue only.
+ * Errors: EE_ERR_INVALID_ARG (null pointers, negative counts), EE_ERR_DTYPE. */
+int ee_rope_apply(const ee_rope* r, int dtype, const ee_heads* x, const ee_heads* y, const int32_t* dev_pos, int n_tokens,
+                  int n_heads, int inverse, int32_t* dev_status, void* stream);
+
+/* ------------------------------------------------------------------ paged cache
+ *
+ * A key/value pool of pages instead of rows of a fixed capacity: a sequence owns whichever pages its page table names, grows
+ * by a page when it needs one, and sequences may share the pages of a common beginning.  Who owns which page is the
+ * caller's bookkeeping; the calls read the page tables on the device.
+ *
+ * Pool: [layer][page][kv head][block of 2 * page_size * head_dim elements].  A block is that of the key/value pool above:
+ *   EE_F32 : K[page_size][hd], then V[page_size][hd]
+ *   EE_BF16: page_size / 32 groups of 32 positions, each [K 32*hd][V 32*hd]; with r the position in the group
+ *              K[r][i] at ((((r/16)*(hd/32) + i/32) * 4 + (i%32)/8) * 16 + r%16) * 8 + i%8
+ *              V[r][i] at 32*hd + (((i/16)*4 + (r%16)/4) * 16 + i%16) * 8 + (r/16)*4 + r%4
+ *   (at head_dim 128 a group is one of ee_kv's, byte for byte).
+ * page_size: a multiple of 32, up to 4096.  head_dim: EE_BF16 64, 96, 128, 192 or 256; EE_F32 a multiple of 4 up to 256. */
+typedef struct {
+    int32_t n_layers;
+    int32_t n_pages;     /* pages of every layer                                       */
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t page_size;   /* positions of a page                                        */
+    int32_t dtype;       /* ee_dtype                                                   */
+} ee_paged_config;
+typedef struct ee_paged ee_paged;
+
+/* The new tokens of one call.  Sequence s brings the rows q_start[s] .. q_start[s+1]-1 (none is allowed); its row j of q_len
+ * stands at position kv_len[s] - q_len + j; position p sits in page pages[s * pages_per_seq + p / page_size].  The host's
+ * figures size the launches, the device's say what is there; q_start rises from 0 to n_tokens. */
+typedef struct {
+    int32_t n_seqs;
+    int32_t n_tokens;            /* rows of the call                                       */
+    int32_t max_q_len;           /* no sequence brings more rows                           */
+    int32_t max_kv_len;          /* no sequence holds more positions, its new rows included */
+    int32_t pages_per_seq;       /* width of the page table                                */
+    const int32_t* dev_q_start;  /* [n_seqs + 1]                                           */
+    const int32_t* dev_kv_len;   /* [n_seqs]                                               */
+    const int32_t* dev_pages;    /* [n_seqs][pages_per_seq]; entries no position needs are not read */
+    int32_t* dev_status;         /* nullable; bits are set, never cleared:                 */
+                                 /*   1 = a position without a page or outside the rotary table */
+                                 /*   2 = a sequence outside the host's figures: none of its rows is served */
+} ee_paged_step;
+
+/* Bytes of the pool; 0 on a configuration ee_paged_bind refuses. */
+size_t ee_paged_pool_bytes(const ee_paged_config* cfg);
+/* The pool is the caller's and outlives the handle; 256-byte aligned.  No device work.
+ * Errors: EE_ERR_SHAPE, EE_ERR_DTYPE, EE_ERR_CAPACITY if the pool is too small, EE_ERR_INVALID_ARG. */
+int ee_paged_bind(const ee_paged_config* cfg, void* dev_pool, size_t pool_bytes, ee_paged** out);
+int ee_paged_destroy(ee_paged* p);
+
+/* Writes the rows' keys and values at their positions of `layer`, the keys rotated by `rope` (NULL: as they are), and, with
+ * n_q_heads > 0, the rotated queries to q_out (which may be q itself).  One launch; rotation in fp32, one rounding.
+ * A row at a negative position or one outside the rotary table is left out and sets status bit 1; so does a position
+ * whose page is not in 0 .. n_pages-1, of which the query is still written.
+ * Errors: EE_ERR_LAYER_NOT_RESIDENT if the pool has no such layer, EE_ERR_CAPACITY if max_kv_len exceeds the page table,
+ * EE_ERR_SHAPE if the rotary table is for another head_dim, EE_ERR_INVALID_ARG. */
+int ee_paged_append(const ee_paged* p, int layer, const ee_paged_step* step, const ee_rope* rope, const ee_heads* k,
+                    const ee_heads* v, const ee_heads* q, const ee_heads* q_out, int n_q_heads, void* stream);
+
+/* Attention of the call's rows over the cached positions, which must hold the rows' own keys and values already: the row at
+ * position p attends to positions max(0, p - window + 1) .. p (window 0: 0 .. p), query head h to kv head
+ * h / (n_q_heads / n_kv_heads):  out = sum_j softmax_j(scale * q.k_j) v_j.  Positions on pages outside 0 .. n_pages-1 are left
+ * out and set status bit 1.  A row that sees no position gets zeros.  What lies at positions a row does not see, infinities
+ * and NaN included, does not reach it.
+ * EE_BF16: scores, softmax statistics and sums in fp32, the probabilities rounded to bf16 for the product with V.
+ * Workspace: ee_paged_attention_workspace bytes, 256-byte aligned, for calls whose host's figures are at most these; its contents
+ * mean nothing between calls.  Calls that overlap in time need one each.
+ * n_q_heads: a multiple of n_kv_heads.  out may not overlap q.
+ * Errors: as ee_paged_append; EE_ERR_CAPACITY if the workspace is too small. */
+size_t ee_paged_attention_workspace(const ee_paged* p, int n_q_heads, const ee_paged_step* step);
+int ee_paged_attention(const ee_paged* p, int layer, const ee_paged_step* step, const ee_heads* q, const ee_heads* out,
+                       int n_q_heads, float scale, int window, void* dev_workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------ measurement aid */
 
 /* Kernel classes of the decode step, for ee_timing_read. */

@@ -13,6 +13,8 @@ EE_OK = 0
 EE_ERR_INVALID_ARG, EE_ERR_SHAPE, EE_ERR_CAPACITY = -1, -2, -3
 EE_ERR_LAYER_NOT_RESIDENT, EE_ERR_EXIT_NOT_RESIDENT, EE_ERR_DTYPE, EE_ERR_HIP = -4, -5, -6, -7
 EE_F32, EE_BF16 = 0, 1
+EE_ROPE_HALF, EE_ROPE_INTERLEAVED = 0, 1
+EE_ROPE_UNSCALED, EE_ROPE_LINEAR, EE_ROPE_BASE, EE_ROPE_BANDS = 0, 1, 2, 3
 
 
 class ee_model_config(C.Structure):
@@ -38,6 +40,27 @@ class ee_batch_layout(C.Structure):
 class ee_pht_row(C.Structure):
     _fields_ = [("tokens", C.c_int64), ("breaches", C.c_int64), ("exits", C.c_int64 * EE_MAX_EXITS),
                 ("nll", C.c_double)]
+
+
+class ee_rope_config(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("pairing", C.c_int32), ("max_pos", C.c_int32),
+                ("scaling", C.c_int32), ("trained_pos", C.c_int32), ("theta", C.c_float), ("factor", C.c_float),
+                ("low", C.c_float), ("high", C.c_float), ("magnitude", C.c_float)]
+
+
+class ee_heads(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class ee_paged_config(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_size", C.c_int32), ("dtype", C.c_int32)]
+
+
+class ee_paged_step(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("max_q_len", C.c_int32), ("max_kv_len", C.c_int32),
+                ("pages_per_seq", C.c_int32), ("dev_q_start", C.c_void_p), ("dev_kv_len", C.c_void_p),
+                ("dev_pages", C.c_void_p), ("dev_status", C.c_void_p)]
 
 
 _vp, _i, _sz, _f = C.c_void_p, C.c_int, C.c_size_t, C.c_float
@@ -87,6 +110,17 @@ _SIGS = {
     "ee_cbc_push_step": (_i, [_vp, _vp, _vp]),
     "ee_pht_init": (_i, [_vp, _vp]),
     "ee_pht_push_step": (_i, [_vp, _vp, _vp, _vp]),
+    "ee_rope_create": (_i, [C.POINTER(ee_rope_config), C.POINTER(_vp)]),
+    "ee_rope_destroy": (_i, [_vp]),
+    "ee_rope_apply": (_i, [_vp, _i, C.POINTER(ee_heads), C.POINTER(ee_heads), _vp, _i, _i, _i, _vp, _vp]),
+    "ee_paged_pool_bytes": (_sz, [C.POINTER(ee_paged_config)]),
+    "ee_paged_bind": (_i, [C.POINTER(ee_paged_config), _vp, _sz, C.POINTER(_vp)]),
+    "ee_paged_destroy": (_i, [_vp]),
+    "ee_paged_append": (_i, [_vp, _i, C.POINTER(ee_paged_step), _vp, C.POINTER(ee_heads), C.POINTER(ee_heads),
+                             C.POINTER(ee_heads), C.POINTER(ee_heads), _i, _vp]),
+    "ee_paged_attention_workspace": (_sz, [_vp, _i, C.POINTER(ee_paged_step)]),
+    "ee_paged_attention": (_i, [_vp, _i, C.POINTER(ee_paged_step), C.POINTER(ee_heads), C.POINTER(ee_heads), _i, _f, _i,
+                                _vp, _sz, _vp]),
     "ee_timing_enable": (_i, [_i]),
     "ee_timing_reset": (_i, []),
     "ee_timing_read": (_i, [_i, C.POINTER(_i), C.POINTER(_f)]),
