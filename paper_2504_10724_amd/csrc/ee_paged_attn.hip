@@ -1,70 +1,592 @@
-// ee_paged_attn.hip -- attention of new rows over the paged cache.
-#include "ee_paged_device.h"
+// ee_paged_attn.hip -- attention of new rows over the paged cache, bf16, and the join of position shares.
+//
+// Both kernels compute S^T = K Q^T and O^T = V^T P^T on 16x16x32 MFMAs with the keys and values as left operands: a group of 32
+// positions lies in the pool in exactly the order the lanes of a wave hold those operands (16 bytes a lane, 1 KiB a load), and
+// a lane's eight scores of a group are its eight elements of the right operand of the second product, so the probabilities never
+// leave their registers.  Lane (n16, gq) holds column n16 of a block of 16 and, of a group, the positions 16 b + 4 gq + r.
+//
+// Softmax: one pass, running maximum and sum in fp32 (log2 units).  Sums are rescaled only when a maximum rises by more than
+// 2^8: probabilities up to 256 lose nothing in bf16 or fp32.  Probabilities are rounded to bf16 for the second product (relative 2^-8
+// each, as the values they weigh were), the sum of the row takes them unrounded.
+#include "ee_paged_attn.h"
 
-// One wave per (row, query head): 64 positions at a time, a lane each for the scores, then the lanes share out the features.
-template <class T>
-__global__ void __launch_bounds__(256)
-k_paged_attn(PagedView pv, StepView st, HeadsView q, HeadsView out, int Hq, float scale, int window) {
-    __shared__ float qs[4][256];
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, hd = pv.hd, ps = pv.page_size;
-    const int64_t id = (int64_t)blockIdx.x * 4 + w;
-    const int t = (int)(id / Hq), h = (int)(id % Hq);
-    if (t >= st.n_tokens) return;
-    const int s = seq_of_slot(st, t, 1, 0);
-    const SeqRows sr = seq_rows(st, s);
-    if (t < sr.row0 || t >= sr.row0 + sr.n) return;
-    const int p = sr.len - sr.n + t - sr.row0;
-    const T* qr = (const T*)q.p + t * q.ts + h * q.hs;
-    for (int i = lane; i < hd; i += 64) qs[w][i] = to_f32(qr[i]) * scale;
-    __builtin_amdgcn_wave_barrier();
-    const int lo = window > 0 ? max(0, p - window + 1) : 0, g = h / (Hq / pv.n_kv_heads);
-    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    bool seen = false;
-    for (int c = lo; c <= p; c += 64) {
-        const int j = c + lane;
-        const T* blk = nullptr;
-        if (j <= p) {
-            const int page = st.pages[(int64_t)s * st.pages_per_seq + j / ps];
-            if (page >= 0 && page < pv.n_pages) blk = (const T*)pv.pool + ((int64_t)page * pv.n_kv_heads + g) * (2LL * ps * hd);
-            else if (st.status) atomicOr(st.status, 1);
-        }
-        float x = -INFINITY;
-        if (blk) {
-            x = 0.f;
-            for (int i = 0; i < hd; ++i) x = fmaf(qs[w][i], to_f32(blk[page_k<T>(j % ps, i, hd, ps)]), x);
-        }
-        seen = seen || __any(blk != nullptr);
-        float mx = x;
-        for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
-        mx = fmaxf(mx, m);
-        const float ref = mx == -INFINITY ? 0.f : mx, a = expf(m - ref);
-        const float e = blk ? expf(x - ref) : 0.f;
-        float sum = e;
-        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-        l = l * a + sum;
-        m = mx;
-        for (int k = 0; k < 4; ++k) o[k] *= a;
-        for (int jj = 0; jj < 64; ++jj) {
-            const uint64_t b = (uint64_t)blk;
-            const uint64_t at = ((uint64_t)(uint32_t)__shfl((int)(b >> 32), jj, 64) << 32) | (uint32_t)__shfl((int)b, jj, 64);
-            if (at == 0) continue;
-            const float ej = __shfl(e, jj, 64);
-            for (int k = 0; k < 4; ++k)
-                if (lane + 64 * k < hd) o[k] = fmaf(ej, to_f32(((const T*)at)[page_v<T>((c + jj) % ps, lane + 64 * k, hd, ps)]), o[k]);
-        }
-    }
-    T* dst = (T*)out.p + t * out.ts + h * out.hs;
-    for (int k = 0; k < 4; ++k)
-        if (lane + 64 * k < hd) dst[lane + 64 * k] = from_f32<T>(seen ? o[k] / l : 0.f);
+#include <algorithm>
+#include <cmath>
+
+__device__ __forceinline__ bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8, v); }
+__device__ __forceinline__ floatx4 mfma(uint4 a, uint4 b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
 
-size_t paged_attention_workspace(int, int, int, int, const StepView&) { return 0; }
+// 8 consecutive features of a row of heads, whatever its alignment
+__device__ __forceinline__ uint4 load_q8(const bf16_t* p, bool wide, uint32_t keep, uint32_t flip) {
+    uint4 v;
+    if (wide) {
+        v = *reinterpret_cast<const uint4*>(p);
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)p[2 * i] | ((uint32_t)p[2 * i + 1] << 16);
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return make_uint4((v.x & keep) ^ flip, (v.y & keep) ^ flip, (v.z & keep) ^ flip, (v.w & keep) ^ flip);
+}
+__device__ __forceinline__ void store_o4(bf16_t* p, bool wide, float a, float b, float c, float d) {
+    const uint2 v = make_uint2(bf16_pair(a, b), bf16_pair(c, d));
+    if (wide) {
+        *reinterpret_cast<uint2*>(p) = v;
+    } else {
+        p[0] = (bf16_t)v.x; p[1] = (bf16_t)(v.x >> 16); p[2] = (bf16_t)v.y; p[3] = (bf16_t)(v.y >> 16);
+    }
+}
+__device__ __forceinline__ bool wide_q(const HeadsView& h) { return (uintptr_t)h.p % 16 == 0 && h.ts % 8 == 0 && h.hs % 8 == 0; }
+__device__ __forceinline__ bool wide_o(const HeadsView& h) { return (uintptr_t)h.p % 8 == 0 && h.ts % 4 == 0 && h.hs % 4 == 0; }
+
+// ------------------------------------------------------------------ the columns of a wave
+// CB blocks of 16 columns of a (sequence, kv head), and what the softmax and the second product keep for them
+template <int NK, int CB> struct Columns {
+    int   lo[CB], hi[CB];          // positions the lane's column sees; hi < lo: none
+    float m[CB], l[CB];            // maximum in log2 units; the lane's part of the sum
+    uint32_t seen;                 // bit j: the column of block j has seen a position
+    floatx4 O[CB][2 * NK];         // [hb][r]: feature 16 hb + 4 gq + r
+    uint4 q[CB][NK];
+
+    // columns c0 .. of the n_cols of rows at positions first + c / G, token rows row0 + c / G
+    __device__ __forceinline__ void start(const AttnArgs& a, int g, int c0, int n_cols, int first, int row0) {
+        const int lane = threadIdx.x & 63, n16 = lane & 15, gq = lane >> 4;
+        const bool wide = wide_q(a.q);
+        seen = 0;
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+            const int c = c0 + 16 * j + n16, t = c / a.G;
+            const bool live = c < n_cols;
+            hi[j] = live ? first + t : -1;
+            lo[j] = lowest_seen(hi[j], a.window);
+            m[j] = -INFINITY;
+            l[j] = 0.f;
+#pragma unroll
+            for (int hb = 0; hb < 2 * NK; ++hb) O[j][hb] = floatx4{0.f, 0.f, 0.f, 0.f};
+            const bf16_t* p = (const bf16_t*)a.q.p + (int64_t)(row0 + t) * a.q.ts + (int64_t)(g * a.G + c - t * a.G) * a.q.hs + 8 * gq;
+#pragma unroll
+            for (int k = 0; k < NK; ++k) q[j][k] = live ? load_q8(p + 32 * k, wide, a.keep, a.flip) : make_uint4(0, 0, 0, 0);
+        }
+    }
+
+    // scores S[j][b][r] of positions pg + 16 b + 4 gq + r -> probabilities as right operands; edge: some column does not see all
+    __device__ __forceinline__ void softmax(floatx4 (&S)[CB][2], uint4 (&P)[CB], float scale2, bool edge, int pg) {
+        const int gq = (threadIdx.x & 63) >> 4;
+        if (edge) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j) {
+                if (max(lo[j], pg) <= min(hi[j], pg + 31)) seen |= 1u << j;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int p = pg + 16 * (i >> 2) + 4 * gq + (i & 3);
+                    if (p < lo[j] || p > hi[j]) S[j][i >> 2][i & 3] = -INFINITY;
+                }
+            }
+        } else {
+            seen = ~0u;
+        }
+        float mx[CB];
+        bool raise = false;
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+            mx[j] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mx[j] = fmaxf(mx[j], S[j][i >> 2][i & 3]);
+            mx[j] = quad_max(mx[j]) * scale2;
+            raise = raise || mx[j] > m[j] + 8.0f;
+        }
+        if (__any(raise)) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j) {
+                const float up = mx[j] > m[j] + 8.0f ? mx[j] : m[j], alpha = __builtin_amdgcn_exp2f(m[j] - reference(up));
+                l[j] *= up == m[j] ? 1.f : alpha;
+#pragma unroll
+                for (int hb = 0; hb < 2 * NK; ++hb) O[j][hb] = O[j][hb] * (up == m[j] ? 1.f : alpha);
+                m[j] = up;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+            float e[8];
+            const float ref = reference(m[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(S[j][i >> 2][i & 3], scale2, -ref));
+            l[j] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+            P[j] = make_uint4(bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7]));
+        }
+    }
+
+    // O += V^T P^T of the 16 features of block hb
+    __device__ __forceinline__ void weigh(int hb, uint4 v, const uint4 (&P)[CB]) {
+#pragma unroll
+        for (int j = 0; j < CB; ++j) O[j][hb] = mfma(v, P[j], O[j][hb]);
+    }
+
+    // The same where some column does not see all positions: a probability of zero does not keep an infinity or NaN among the
+    // values out of the sum (0 x inf), so these are taken out of the operand, and the columns that see them get them by counting:
+    // infinities of either sign met with a positive probability, NaN and everything non-finite met with a zero one.
+    // What no column sees (last_lo .. of the wave's columns) may be memory nobody has written: zero.
+    __device__ __forceinline__ void weigh_edge(int hb, uint4 v, const uint4 (&P)[CB], int pg, int min_lo, int max_hi) {
+        const int gq = (threadIdx.x & 63) >> 4;
+        uint32_t w[4] = {v.x, v.y, v.z, v.w}, pos[4], neg[4], nan[4], any = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            pos[i] = neg[i] = nan[i] = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int e = 2 * i + h, p = pg + 16 * (e >> 2) + 4 * gq + (e & 3);
+                const uint32_t x = (w[i] >> (16 * h)) & 0xffffu, one = 0x3f80u << (16 * h), keep = ~(0xffffu << (16 * h));
+                const bool out = p < min_lo || p > max_hi, odd = !out && (x & 0x7f80u) == 0x7f80u;
+                if (out || odd) w[i] &= keep;
+                if (odd) {
+                    any = 1;
+                    if (x & 0x7fu) nan[i] |= one;
+                    else if (x >> 15) neg[i] |= one;
+                    else pos[i] |= one;
+                }
+            }
+        }
+        weigh(hb, make_uint4(w[0], w[1], w[2], w[3]), P);
+        if (!__any(any != 0)) return;
+        const uint4 vp = make_uint4(pos[0], pos[1], pos[2], pos[3]), vn = make_uint4(neg[0], neg[1], neg[2], neg[3]),
+                    vx = make_uint4(nan[0], nan[1], nan[2], nan[3]),
+                    va = make_uint4(pos[0] | neg[0] | nan[0], pos[1] | neg[1] | nan[1], pos[2] | neg[2] | nan[2], pos[3] | neg[3] | nan[3]);
+        const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+            const uint32_t pw[4] = {P[j].x, P[j].y, P[j].z, P[j].w};
+            uint32_t some[4], none[4];                       // 1 where the column sees a position with P > 0, with P = 0
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                some[i] = none[i] = 0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int e = 2 * i + h, p = pg + 16 * (e >> 2) + 4 * gq + (e & 3);
+                    const bool sees = p >= lo[j] && p <= hi[j], positive = (pw[i] >> (16 * h)) & 0xffffu;
+                    const uint32_t one = 0x3f80u << (16 * h);
+                    if (sees && positive) some[i] |= one;
+                    if (sees && !positive) none[i] |= one;
+                }
+            }
+            const uint4 ps = make_uint4(some[0], some[1], some[2], some[3]), pz = make_uint4(none[0], none[1], none[2], none[3]);
+            const floatx4 up = mfma(vp, ps, zero), down = mfma(vn, ps, zero), bad = mfma(va, pz, mfma(vx, ps, zero));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (up[r] > 0.f) O[j][hb][r] += INFINITY;
+                if (down[r] > 0.f) O[j][hb][r] -= INFINITY;
+                if (bad[r] > 0.f) O[j][hb][r] = NAN;
+            }
+        }
+    }
+};
+
+// sums of four features to the result (one share) or to the shares' buffer
+struct ColumnOut {
+    bf16_t* row;                   // of the result, or null
+    float*  part;
+    bool    wide;
+    __device__ __forceinline__ void put(int f, floatx4 o) const {
+        if (row) store_o4(row + f, wide, o[0], o[1], o[2], o[3]);
+        else *reinterpret_cast<floatx4*>(part + f) = o;
+    }
+};
+__device__ __forceinline__ bf16_t* out_row(const AttnArgs& a, int g, int c, int row0) {
+    const int t = c / a.G;
+    return (bf16_t*)a.out.p + (int64_t)(row0 + t) * a.out.ts + (int64_t)(g * a.G + c - t * a.G) * a.out.hs;
+}
+
+// ------------------------------------------------------------------ sequences of few columns
+// One workgroup per (sequence, kv head, share of the positions); its four waves take the share's groups in turn, straight from
+// memory into registers, and join their sums through LDS at the end.
+template <int NK, int CB>
+__global__ void __launch_bounds__(256, 2)
+k_bf16_paged_rows(AttnArgs a) {
+    constexpr int HD = 32 * NK;
+    __shared__ float4 so[4][2 * NK][64];
+    __shared__ float sm[4][16 * CB], sl[4][16 * CB];
+    const int s = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - s * a.pv.n_kv_heads;
+    const SeqRows sr = seq_rows(a.st, s);
+    const int n_cols = sr.n * a.G;
+    if (sr.n == 0 || n_cols > a.rows_cols) return;
+    const int first = sr.len - sr.n, min_lo = lowest_seen(first, a.window), max_lo = lowest_seen(sr.len - 1, a.window);
+    const GroupRange all = groups_of(min_lo, sr.len - 1);
+    const int n_shares = shares_of(all.n, a.share);
+    if ((int)blockIdx.y >= n_shares) return;
+    const int lane = threadIdx.x & 63, n16 = lane & 15, w = to_scalar(threadIdx.x >> 6);
+    const int ga = all.g0 + blockIdx.y * a.share, gb = min(ga + a.share, all.g0 + all.n);
+
+    Columns<NK, CB> col;
+    col.start(a, g, 0, n_cols, first, sr.row0);
+    const char* pool = a.pv.pool;
+    const int n_mine = max(0, (gb - ga - w + 3) >> 2);       // this wave's groups: ga + w, ga + w + 4, ..
+    uint32_t where = 0;
+    for (int i = 0; i < n_mine; ++i) {
+        if ((i & 63) == 0) {
+            const int grp = ga + w + 4 * (i + lane);
+            where = grp < gb ? pool_group(a.pv, a.st, s, g, grp) : NO_GROUP;
+        }
+        const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)where, i & 63);
+        if (at == NO_GROUP) continue;
+        const uint4* kv = reinterpret_cast<const uint4*>(pool + (uint64_t)at * (HD * 128)) + lane;
+        const int pg = (ga + w + 4 * i) << 5;
+        const bool edge = pg + 31 > first || pg < max_lo;
+        constexpr int EARLY = NK > 6 ? NK / 2 : 2 * NK;          // values asked for before the scores: as many as fit the registers
+        uint4 kf[2 * NK], vf[2 * NK];
+#pragma unroll
+        for (int f = 0; f < 2 * NK; ++f) kf[f] = kv[f * 64];
+#pragma unroll
+        for (int f = 0; f < EARLY; ++f) vf[f] = kv[(2 * NK + f) * 64];
+        floatx4 S[CB][2];
+#pragma unroll
+        for (int j = 0; j < CB; ++j) S[j][0] = S[j][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int j = 0; j < CB; ++j) {
+                S[j][0] = mfma(kf[k], col.q[j][k], S[j][0]);
+                S[j][1] = mfma(kf[NK + k], col.q[j][k], S[j][1]);
+            }
+        if constexpr (EARLY < 2 * NK) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = EARLY; f < 2 * NK; ++f) vf[f] = kv[(2 * NK + f) * 64];
+        uint4 P[CB];
+        col.softmax(S, P, a.scale2, edge, pg);
+        if (edge) {
+#pragma unroll
+            for (int hb = 0; hb < 2 * NK; ++hb) col.weigh_edge(hb, vf[hb], P, pg, min_lo, sr.len - 1);
+        } else {
+#pragma unroll
+            for (int hb = 0; hb < 2 * NK; ++hb) col.weigh(hb, vf[hb], P);
+        }
+    }
+
+    // join the waves: maxima and sums first, then the weighted sums, a wave two features blocks of every four
+#pragma unroll
+    for (int j = 0; j < CB; ++j) {
+        const float l = quad_sum(col.l[j]);
+        if (lane < 16) {
+            sm[w][16 * j + n16] = col.m[j];
+            sl[w][16 * j + n16] = (col.seen >> j) & 1u ? l : -1.f;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < CB; ++j) {
+        if (16 * j >= n_cols) break;
+        __syncthreads();                                     // the statistics are there; the last block's sums have been read
+#pragma unroll
+        for (int hb = 0; hb < 2 * NK; ++hb) *reinterpret_cast<floatx4*>(&so[w][hb][lane]) = col.O[j][hb];
+        __syncthreads();
+        const int c = 16 * j + n16;
+        float m = -INFINITY, l = 0.f, wt[4];
+        bool seen = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { m = fmaxf(m, sm[i][c]); seen = seen || !(sl[i][c] < 0.f); }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            wt[i] = __builtin_amdgcn_exp2f(sm[i][c] - reference(m));
+            if (!(sl[i][c] < 0.f)) l += wt[i] * sl[i][c];
+        }
+        if (c >= n_cols) continue;
+        const int64_t slot = ((int64_t)blockIdx.x * a.shares + blockIdx.y) * a.rows_cols + c;
+        const bool last = n_shares == 1;
+        const ColumnOut dst{last ? out_row(a, g, c, sr.row0) : nullptr, last ? nullptr : a.part + slot * HD, wide_o(a.out)};
+        if (!last && w == 0 && lane < 16) a.stat[slot] = make_float2(m, seen ? l : -1.f);
+        const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
+        for (int hb = w; hb < 2 * NK; hb += 4) {
+            floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const floatx4 x = *reinterpret_cast<const floatx4*>(&so[i][hb][lane]);
+                if (!(sl[i][c] < 0.f)) o += x * wt[i];
+            }
+            dst.put(16 * hb + 4 * (lane >> 4), o * inv);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ sequences of many columns
+// 1 KiB (64 lanes x 16 bytes) from memory into LDS, past the registers; waited for with vmcnt by hand
+__device__ __forceinline__ void load_kib(const char* src, unsigned lane_bytes, unsigned lds_byte) {
+    const uint64_t a = reinterpret_cast<uint64_t>(src);
+    const uint64_t base = ((uint64_t)(uint32_t)to_scalar((int)(a >> 32)) << 32) | (uint32_t)to_scalar((int)a);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to_scalar(lds_byte)), "v"(lane_bytes), "s"(base)
+                 : "memory");
+}
+
+// One workgroup per (tile of 64 CB columns, kv head, share): the four waves take 16 CB columns each and share the keys and values,
+// which go through LDS SG groups at a time, the next stage under way while one is worked on.
+template <int NK, int CB>
+__global__ void __launch_bounds__(256, NK <= 4 ? 2 : 1)
+k_bf16_paged_tile(AttnArgs a, int n_slots) {
+    constexpr int HD = 32 * NK, C = 64 * CB, SG = NK <= 4 ? 2 : 1, KIB = 4 * NK;   // KiB of a group
+    __shared__ uint4 lds[2 * SG * KIB * 64];
+    const int sx = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - sx * a.pv.n_kv_heads;
+    const int slot = n_slots - 1 - sx;                       // later rows see more positions: they start first
+    const Tile tl = tile_of_slot(a.st, a.G, C, slot);
+    const int s = tl.s, tile = tl.tile;
+    const SeqRows sr = seq_rows(a.st, s);
+    const int n_cols = sr.n * a.G, c0 = tile * C;
+    if (sr.n == 0 || n_cols <= a.rows_cols || tile < 0 || c0 >= n_cols) return;
+    const int first = sr.len - sr.n;
+    const int t0 = c0 / a.G, t1 = (min(c0 + C, n_cols) - 1) / a.G;
+    const GroupRange all = groups_of(lowest_seen(first + t0, a.window), first + t1);
+    const int n_shares = shares_of(all.n, a.share);
+    if ((int)blockIdx.y >= n_shares) return;
+    const int ga = all.g0 + blockIdx.y * a.share, gb = min(ga + a.share, all.g0 + all.n);
+    const int lane = threadIdx.x & 63, n16 = lane & 15, w = to_scalar(threadIdx.x >> 6);
+    const int cw = c0 + w * 16 * CB;                         // the wave's columns and the positions they see
+    const int w_first = first + cw / a.G, w_last = cw < n_cols ? first + (min(cw + 16 * CB, n_cols) - 1) / a.G : -1;
+    const int min_lo = lowest_seen(w_first, a.window), max_lo = lowest_seen(w_last, a.window);
+
+    Columns<NK, CB> col;
+    col.start(a, g, cw, n_cols, first, sr.row0);
+#pragma unroll
+    for (int j = 0; j < CB; ++j)                             // in registers before the first load into LDS is under way
+#pragma unroll
+        for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(col.q[j][k].x), "+v"(col.q[j][k].y), "+v"(col.q[j][k].z), "+v"(col.q[j][k].w));
+
+    const unsigned lane_bytes = (unsigned)lane * 16u, lds0 = (unsigned)(size_t)lds;
+    const int n_st = (gb - ga + SG - 1) / SG;
+    uint32_t where = NO_GROUP, where_next = NO_GROUP;        // of the 64 groups around the current stage, and of the next 64
+    auto look_up = [&](int i) { return ga + i + lane < gb ? pool_group(a.pv, a.st, s, g, ga + i + lane) : NO_GROUP; };
+    // a wave sends SG NK of the SG 4 NK KiB of a stage; a group that is not there is replaced by the pool's first
+    auto issue = [&](int t, uint32_t known) {
+        const int k = w * SG / 4, i = (SG * t + k) & 63;
+        const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)known, i);
+        const char* src = a.pv.pool + (at == NO_GROUP ? 0ull : (uint64_t)at * (HD * 128)) + (w * SG % 4) * NK * 1024;
+        const unsigned dst = lds0 + (unsigned)((t & 1) * SG * KIB + w * SG * NK) * 1024u;
+#pragma unroll
+        for (int p = 0; p < SG * NK; ++p) load_kib(src + p * 1024, lane_bytes, dst + (unsigned)p * 1024u);
+    };
+    if (n_st > 0) {
+        where = look_up(0);
+        asm volatile("" : "+v"(where));
+        issue(0, where);
+    }
+    for (int t = 0; t < n_st; ++t) {
+        // this wave's part of the stage has landed; after the barrier everybody's has, and the other buffer has been read
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const int i0 = SG * t;
+        if (t + 1 < n_st) {
+            where_next = where;
+            if (((i0 + SG) & 63) == 0) where_next = look_up(i0 + SG);
+            issue(t + 1, where_next);
+        }
+#pragma unroll 1
+        for (int k = 0; k < SG; ++k) {
+            const int pg = (ga + i0 + k) << 5;
+            if (ga + i0 + k >= gb || pg > w_last) break;
+            if (pg + 31 < min_lo || (uint32_t)__builtin_amdgcn_readlane((int)where, (i0 + k) & 63) == NO_GROUP) continue;
+            const bool edge = pg + 31 > w_first || pg < max_lo || w_last < 0;
+            const uint4* kv = lds + ((t & 1) * SG + k) * KIB * 64 + lane;
+            uint4 kf[2 * NK];
+#pragma unroll
+            for (int f = 0; f < 2 * NK; ++f) kf[f] = kv[f * 64];
+            floatx4 S[CB][2];
+#pragma unroll
+            for (int j = 0; j < CB; ++j) S[j][0] = S[j][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int f = 0; f < NK; ++f)
+#pragma unroll
+                for (int j = 0; j < CB; ++j) {
+                    S[j][0] = mfma(kf[f], col.q[j][f], S[j][0]);
+                    S[j][1] = mfma(kf[NK + f], col.q[j][f], S[j][1]);
+                }
+            uint4 P[CB];
+            col.softmax(S, P, a.scale2, edge, pg);
+            if (edge) {
+#pragma unroll
+                for (int hb = 0; hb < 2 * NK; ++hb) col.weigh_edge(hb, kv[(2 * NK + hb) * 64], P, pg, min_lo, w_last);
+            } else {
+#pragma unroll
+                for (int hb = 0; hb < 2 * NK; ++hb) col.weigh(hb, kv[(2 * NK + hb) * 64], P);
+            }
+        }
+        where = where_next;
+    }
+
+    const bool last = n_shares == 1, wide = wide_o(a.out);
+    const int64_t block = ((int64_t)(slot * (int64_t)a.pv.n_kv_heads + g) * a.shares + blockIdx.y) * C;
+#pragma unroll
+    for (int j = 0; j < CB; ++j) {
+        const int c = cw + 16 * j + n16;
+        const float l = quad_sum(col.l[j]);
+        const bool seen = (col.seen >> j) & 1u;
+        if (c >= n_cols) continue;
+        const int64_t at = block + c - c0;
+        const ColumnOut dst{last ? out_row(a, g, c, sr.row0) : nullptr, last ? nullptr : a.part + at * HD, wide};
+        if (!last && lane < 16) a.stat[at] = make_float2(col.m[j], seen ? l : -1.f);
+        const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
+#pragma unroll
+        for (int hb = 0; hb < 2 * NK; ++hb) dst.put(16 * hb + 4 * (lane >> 4), seen ? col.O[j][hb] * inv : floatx4{0.f, 0.f, 0.f, 0.f});
+    }
+}
+
+// ------------------------------------------------------------------ join of the shares
+// A wave per column: the shares' maxima and sums, then their weighted sums, in share order (the same bits every time).
+// C = 0: sequences of few columns, blockIdx.x = (sequence, kv head); else tiles of C columns, blockIdx.x = (slot, kv head).
+__global__ void __launch_bounds__(256)
+k_bf16_paged_join(AttnArgs a, int C, int n_slots) {
+    const int x = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - x * a.pv.n_kv_heads;
+    const int slot = C > 0 ? n_slots - 1 - x : x;
+    Tile tl{x, 0};
+    if (C > 0) tl = tile_of_slot(a.st, a.G, C, slot);
+    const SeqRows sr = seq_rows(a.st, tl.s);
+    const int n_cols = sr.n * a.G, first = sr.len - sr.n, width = C > 0 ? C : a.rows_cols;
+    const int i = blockIdx.y * 4 + to_scalar(threadIdx.x >> 6), c0 = tl.tile * C, c = c0 + i;
+    if (sr.n == 0 || tl.tile < 0 || (C > 0) != (n_cols > a.rows_cols) || i >= width || c >= n_cols) return;
+    const int t0 = C > 0 ? c0 / a.G : 0, t1 = C > 0 ? (min(c0 + C, n_cols) - 1) / a.G : sr.n - 1;
+    const int shares = shares_of(groups_of(lowest_seen(first + t0, a.window), first + t1).n, a.share);
+    if (shares == 1) return;                                 // its workgroup has written the result
+    const int64_t at = ((int64_t)slot * a.pv.n_kv_heads + g) * a.shares * width + i;
+    const int lane = threadIdx.x & 63, hd = a.pv.hd, f = 4 * lane;
+    float m = -INFINITY;
+    bool seen = false;
+    for (int k = lane; k < shares; k += 64) {
+        const float2 st = a.stat[at + (int64_t)k * width];
+        m = fmaxf(m, st.x);
+        seen = seen || !(st.y < 0.f);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    seen = __any(seen);
+    float l = 0.f;
+    floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 0; k < shares; ++k) {
+        const float2 st = a.stat[at + (int64_t)k * width];
+        const floatx4 v = f < hd ? *reinterpret_cast<const floatx4*>(a.part + (at + (int64_t)k * width) * hd + f) : floatx4{0.f, 0.f, 0.f, 0.f};
+        if (st.y < 0.f) continue;
+        const float wt = __builtin_amdgcn_exp2f(st.x - reference(m));
+        l += wt * st.y;
+        o += v * wt;
+    }
+    if (f >= hd) return;
+    const float inv = seen ? 1.0f / l : 0.f;
+    store_o4(out_row(a, g, c, sr.row0) + f, wide_o(a.out), o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+}
+
+// ------------------------------------------------------------------ host side
+// Who serves what, and in how many shares.  From the host's figures alone: the device's are not known here.
+namespace {
+constexpr int ROWS_TARGET = 1024, ROWS_LEAST = 8;            // workgroups wanted; groups of 32 positions a share has at least
+constexpr int TILE_TARGET = 512, TILE_LEAST = 16;
+
+struct Split { int share = 1, shares = 1; };
+Split split(int64_t blocks, int groups, int target, int least) {
+    const int64_t want = std::max<int64_t>(1, (target + blocks - 1) / blocks);
+    const int share = (int)std::max<int64_t>(least, (groups + want - 1) / want);
+    return Split{share, std::max(1, (groups + share - 1) / share)};
+}
+
+int rows_limit(int hd) { return hd <= 128 ? 32 : 16; }       // columns that k_bf16_paged_rows holds
+constexpr int TILE_MOST = 128;                               // columns of the widest tile
+
+struct Plan {
+    bool rows = false, tile = false;
+    int rows_cols = 0, rows_cb = 1, tile_cb = 2;
+    int64_t rows_blocks = 0, n_slots = 0;
+    Split r, t;
+};
+// groups of 32 positions that `rows` neighbouring rows see together at most
+int groups_seen(const StepView& st, int64_t rows, int window) {
+    const int all = (st.max_kv_len + 31) / 32;
+    return window > 0 ? (int)std::min<int64_t>(all, (std::min<int64_t>(window, st.max_kv_len) + rows + 29) / 32 + 1) : all;
+}
+Plan make_plan(int hd, int Hkv, int G, const StepView& st, int window) {
+    Plan p;
+    const int64_t most = (int64_t)st.max_q_len * G;
+    const int limit = rows_limit(hd);
+    if (most <= limit) {
+        p.rows = true;
+        p.rows_cols = (int)most;
+    } else {
+        p.tile = true;
+        // single tokens beside longer sequences; if every sequence brings max_q_len rows there are none
+        p.rows = G <= limit && (int64_t)st.n_seqs * st.max_q_len != st.n_tokens;
+        p.rows_cols = p.rows ? (G + 15) / 16 * 16 : 0;
+        p.tile_cb = most <= 64 ? 1 : 2;
+        const int C = 64 * p.tile_cb;
+        p.n_slots = (int64_t)st.n_tokens * G / C + st.n_seqs;
+        p.t = split(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window), TILE_TARGET, TILE_LEAST);
+    }
+    while (16 * p.rows_cb < p.rows_cols) p.rows_cb *= 2;
+    p.rows_cols = std::min(p.rows_cols, 16 * p.rows_cb);
+    if (p.rows) {
+        p.rows_blocks = (int64_t)st.n_seqs * Hkv;
+        p.r = split(p.rows_blocks, groups_seen(st, (p.rows_cols + G - 1) / G, window), ROWS_TARGET, ROWS_LEAST);
+    }
+    return p;
+}
+size_t share_bytes(int hd) { return (size_t)hd * sizeof(float) + sizeof(float2); }     // of a column
+}  // namespace
+
+// split() makes at most target + blocks workgroups of fewer than target blocks, whatever the other figures are
+size_t paged_attention_workspace(int dtype, int hd, int Hkv, int n_q_heads, const StepView& st) {
+    if (dtype != EE_BF16) return 0;
+    const int64_t most = (int64_t)st.max_q_len * (n_q_heads / Hkv);
+    const int groups = (st.max_kv_len + 31) / 32, limit = rows_limit(hd);
+    size_t n = 0;
+    if (groups > ROWS_LEAST) n += (size_t)2 * ROWS_TARGET * std::min<int64_t>(limit, (most + 15) / 16 * 16) * share_bytes(hd);
+    if (groups > TILE_LEAST && most > limit) n += (size_t)2 * TILE_TARGET * TILE_MOST * share_bytes(hd);
+    return n;
+}
+
+template <int NK>
+static int run_bf16(const Plan& p, AttnArgs a, char* ws, hipStream_t s) {
+    const int Hkv = a.pv.n_kv_heads, hd = a.pv.hd;
+    auto place = [&](int64_t columns) {                      // sums and statistics of a kernel's shares
+        a.part = (float*)ws;
+        a.stat = (float2*)(ws + (size_t)columns * hd * sizeof(float));
+        ws += (size_t)columns * share_bytes(hd);
+    };
+    a.rows_cols = p.rows_cols;
+    if (p.tile) {
+        a.share = p.t.share; a.shares = p.t.shares;
+        const int C = 64 * p.tile_cb;
+        if (a.shares > 1) place(p.n_slots * Hkv * a.shares * C);
+        auto kern = p.tile_cb == 1 ? k_bf16_paged_tile<NK, 1> : k_bf16_paged_tile<NK, 2>;
+        hipLaunchKernelGGL(kern, dim3((unsigned)(p.n_slots * Hkv), a.shares), dim3(256), 0, s, a, (int)p.n_slots);
+        EE_LAUNCH_CHECK();
+        if (a.shares > 1) {
+            hipLaunchKernelGGL(k_bf16_paged_join, dim3((unsigned)(p.n_slots * Hkv), C / 4), dim3(256), 0, s, a, C, (int)p.n_slots);
+            EE_LAUNCH_CHECK();
+        }
+    }
+    if (p.rows) {
+        a.share = p.r.share; a.shares = p.r.shares;
+        if (a.shares > 1) place(p.rows_blocks * a.shares * a.rows_cols);
+        const dim3 grid((unsigned)p.rows_blocks, a.shares);
+        if (p.rows_cb == 1) hipLaunchKernelGGL((k_bf16_paged_rows<NK, 1>), grid, dim3(256), 0, s, a);
+        else if constexpr (NK <= 4) hipLaunchKernelGGL((k_bf16_paged_rows<NK, 2>), grid, dim3(256), 0, s, a);
+        EE_LAUNCH_CHECK();
+        if (a.shares > 1) {
+            hipLaunchKernelGGL(k_bf16_paged_join, dim3((unsigned)p.rows_blocks, (a.rows_cols + 3) / 4), dim3(256), 0, s, a, 0, 0);
+            EE_LAUNCH_CHECK();
+        }
+    }
+    return EE_OK;
+}
 
 int launch_paged_attention(int dtype, const PagedView& pv, const StepView& st, const HeadsView& q, const HeadsView& out, int n_q_heads,
-                           float scale, int window, char*, hipStream_t s) {
-    const int64_t waves = (int64_t)st.n_tokens * n_q_heads;
-    auto kern = dtype == EE_BF16 ? k_paged_attn<bf16_t> : k_paged_attn<float>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, pv, st, q, out, n_q_heads, scale, window);
-    EE_LAUNCH_CHECK();
-    return EE_OK;
+                           float scale, int window, char* ws, hipStream_t s) {
+    if (dtype != EE_BF16) return f32_paged_attention(pv, st, q, out, n_q_heads, scale, window, s);
+    AttnArgs a{};
+    a.pv = pv; a.st = st; a.q = q; a.out = out;
+    a.G = n_q_heads / pv.n_kv_heads;
+    a.scale2 = scale == 0.f ? 1.f : std::fabs(scale) * 1.44269504088896340736f;
+    a.flip = scale < 0.f ? 0x80008000u : 0u;
+    a.keep = scale == 0.f ? 0u : 0xffffffffu;
+    a.window = window;
+    const Plan p = make_plan(pv.hd, pv.n_kv_heads, a.G, st, window);
+    switch (pv.hd) {
+        case 64: return run_bf16<2>(p, a, ws, s);
+        case 96: return run_bf16<3>(p, a, ws, s);
+        case 128: return run_bf16<4>(p, a, ws, s);
+        case 192: return run_bf16<6>(p, a, ws, s);
+        default: return run_bf16<8>(p, a, ws, s);
+    }
 }
