@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8, v); }
 __device__ __forceinline__ floatx4 mfma(uint4 a, uint4 b, floatx4 c) {
@@ -42,11 +43,32 @@ __device__ __forceinline__ void store_o4(bf16_t* p, bool wide, float a, float b,
 __device__ __forceinline__ bool wide_q(const HeadsView& h) { return (uintptr_t)h.p % 16 == 0 && h.ts % 8 == 0 && h.hs % 8 == 0; }
 __device__ __forceinline__ bool wide_o(const HeadsView& h) { return (uintptr_t)h.p % 8 == 0 && h.ts % 4 == 0 && h.hs % 4 == 0; }
 
+// Positions lo .. hi of the group at pg as bits (bit r: position pg + r); of these the eight a lane holds (bit e: 16 (e / 4) + 4 gq +
+// e % 4); one of them as a mask; and all eight as masks of the halves of an operand's four words.
+__device__ __forceinline__ uint32_t seen_of_group(int lo, int hi, int pg) {
+    const int a = max(lo - pg, 0), e = min(hi - pg, 31);
+    return a > e ? 0u : (0xffffffffu >> (31 - e)) & (0xffffffffu << a);
+}
+__device__ __forceinline__ uint32_t seen_by_lane(uint32_t group) {
+    const uint32_t g = group >> (4 * ((threadIdx.x & 63) >> 4));
+    return (g & 15u) | ((g >> 12) & 0xf0u);
+}
+__device__ __forceinline__ uint32_t bit_mask(uint32_t bits, int i) { return (uint32_t)((int)(bits << (31 - i)) >> 31); }
+__device__ __forceinline__ void seen_words(uint32_t (&w)[4], int lo, int hi, int pg) {
+    const uint32_t mine = seen_by_lane(seen_of_group(lo, hi, pg));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (bit_mask(mine, 2 * i) & 0xffffu) | (bit_mask(mine, 2 * i + 1) & 0xffff0000u);
+}
+// bits 15 and 31: the half is an infinity or NaN; and such bits as masks of the halves
+__device__ __forceinline__ uint32_t odd_bits(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t half_mask(uint32_t bits) { bits >>= 15; return (bits << 16) - bits; }
+
 // ------------------------------------------------------------------ the columns of a wave
 // CB blocks of 16 columns of a (sequence, kv head), and what the softmax and the second product keep for them
 template <int NK, int CB> struct Columns {
     int   lo[CB], hi[CB];          // positions the lane's column sees; hi < lo: none
-    float m[CB], l[CB];            // maximum in log2 units; the lane's part of the sum
+    float neg[CB], lim[CB], l[CB]; // minus the exponents' reference (log2 units); how far above it a score may lie (see softmax); the
+                                   // lane's part of the sum
     uint32_t seen;                 // bit j: the column of block j has seen a position
     floatx4 O[CB][2 * NK];         // [hb][r]: feature 16 hb + 4 gq + r
     uint4 q[CB][NK];
@@ -62,7 +84,8 @@ template <int NK, int CB> struct Columns {
             const bool live = c < n_cols;
             hi[j] = live ? first + t : -1;
             lo[j] = lowest_seen(hi[j], a.window);
-            m[j] = -INFINITY;
+            neg[j] = 0.f;
+            lim[j] = -INFINITY;
             l[j] = 0.f;
 #pragma unroll
             for (int hb = 0; hb < 2 * NK; ++hb) O[j][hb] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -72,50 +95,93 @@ template <int NK, int CB> struct Columns {
         }
     }
 
-    // scores S[j][b][r] of positions pg + 16 b + 4 gq + r -> probabilities as right operands; edge: some column does not see all
-    __device__ __forceinline__ void softmax(floatx4 (&S)[CB][2], uint4 (&P)[CB], float scale2, bool edge, int pg) {
-        const int gq = (threadIdx.x & 63) >> 4;
-        if (edge) {
+    __device__ __forceinline__ float maximum(int j) const { return lim[j] == -INFINITY ? -INFINITY : -neg[j]; }
+
+    // Scores S[j][b][r] of positions pg + 16 b + 4 gq + r -> probabilities as right operands; EDGE: some column does not see all.
+    // A column's reference is its largest score when it was last moved: it moves when a score exceeds it by more than lim = 8, or,
+    // while nothing but -inf has been seen (lim = -inf), when any does.  A lane looks at its own eight scores only; the four lanes
+    // of a column meet when one of the wave's references has to move.
+    template <bool EDGE> __device__ __forceinline__ void softmax(const floatx4 (&S)[CB][2], uint4 (&P)[CB], float scale2, int pg) {
+        float x[CB][8], top[CB];
+        uint32_t mine[CB];
+        bool raise = false;
+        auto exponents = [&](int j) {
 #pragma unroll
-            for (int j = 0; j < CB; ++j) {
-                if (max(lo[j], pg) <= min(hi[j], pg + 31)) seen |= 1u << j;
+            for (int i = 0; i < 8; ++i) x[j][i] = fmaf(S[j][i >> 2][i & 3], scale2, neg[j]);
+            if constexpr (EDGE) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int p = pg + 16 * (i >> 2) + 4 * gq + (i & 3);
-                    if (p < lo[j] || p > hi[j]) S[j][i >> 2][i & 3] = -INFINITY;
+                    const uint32_t keep = bit_mask(mine[j], i);
+                    x[j][i] = __uint_as_float((__float_as_uint(x[j][i]) & keep) | (0xff800000u & ~keep));
                 }
+            }
+        };
+        if constexpr (EDGE) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j) {
+                const uint32_t all = seen_of_group(lo[j], hi[j], pg);
+                mine[j] = seen_by_lane(all);
+                seen |= all ? 1u << j : 0u;
             }
         } else {
             seen = ~0u;
         }
-        float mx[CB];
-        bool raise = false;
 #pragma unroll
         for (int j = 0; j < CB; ++j) {
-            mx[j] = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) mx[j] = fmaxf(mx[j], S[j][i >> 2][i & 3]);
-            mx[j] = quad_max(mx[j]) * scale2;
-            raise = raise || mx[j] > m[j] + 8.0f;
+            exponents(j);
+            top[j] = fmaxf(fmaxf(fmaxf(x[j][0], x[j][1]), fmaxf(x[j][2], x[j][3])), fmaxf(fmaxf(x[j][4], x[j][5]), fmaxf(x[j][6], x[j][7])));
+            raise = raise || top[j] > lim[j];
         }
         if (__any(raise)) {
 #pragma unroll
             for (int j = 0; j < CB; ++j) {
-                const float up = mx[j] > m[j] + 8.0f ? mx[j] : m[j], alpha = __builtin_amdgcn_exp2f(m[j] - reference(up));
-                l[j] *= up == m[j] ? 1.f : alpha;
+                const float t = quad_max(top[j]);
+                const bool up = t > lim[j];
+                const float to = up ? neg[j] - t : neg[j];
+                float alpha = __builtin_amdgcn_exp2f(to - neg[j]);
+                if (lim[j] == -INFINITY) alpha = 0.f;        // there is nothing yet
+                if (!up) alpha = 1.f;
+                neg[j] = to;
+                lim[j] = up ? 8.0f : lim[j];
+                l[j] *= alpha;
 #pragma unroll
-                for (int hb = 0; hb < 2 * NK; ++hb) O[j][hb] = O[j][hb] * (up == m[j] ? 1.f : alpha);
-                m[j] = up;
+                for (int hb = 0; hb < 2 * NK; ++hb) O[j][hb] = O[j][hb] * alpha;
+                exponents(j);
             }
         }
 #pragma unroll
         for (int j = 0; j < CB; ++j) {
             float e[8];
-            const float ref = reference(m[j]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(S[j][i >> 2][i & 3], scale2, -ref));
+            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(x[j][i]);
             l[j] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
             P[j] = make_uint4(bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7]));
+        }
+    }
+
+    // S^T = K Q^T of a group: kf[b NK + k] holds features 32 k .. of the 16 positions of half b
+    __device__ __forceinline__ void scores(const uint4 (&kf)[2 * NK], floatx4 (&S)[CB][2]) const {
+#pragma unroll
+        for (int j = 0; j < CB; ++j) S[j][0] = S[j][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int j = 0; j < CB; ++j) {
+                S[j][0] = mfma(kf[k], q[j][k], S[j][0]);
+                S[j][1] = mfma(kf[NK + k], q[j][k], S[j][1]);
+            }
+    }
+
+    // softmax and second product of a group at pg with the values vf
+    template <bool EDGE>
+    __device__ __forceinline__ void take(const floatx4 (&S)[CB][2], const uint4 (&vf)[2 * NK], float scale2, int pg, int min_lo, int max_hi) {
+        uint4 P[CB];
+        softmax<EDGE>(S, P, scale2, pg);
+        if constexpr (EDGE) {
+            weigh_edge(vf, P, pg, min_lo, max_hi);
+        } else {
+#pragma unroll
+            for (int hb = 0; hb < 2 * NK; ++hb) weigh(hb, vf[hb], P);
         }
     }
 
@@ -125,59 +191,63 @@ template <int NK, int CB> struct Columns {
         for (int j = 0; j < CB; ++j) O[j][hb] = mfma(v, P[j], O[j][hb]);
     }
 
-    // The same where some column does not see all positions: a probability of zero does not keep an infinity or NaN among the
+    // The same where some column does not see all positions.  A probability of zero does not keep an infinity or NaN among the
     // values out of the sum (0 x inf), so these are taken out of the operand, and the columns that see them get them by counting:
     // infinities of either sign met with a positive probability, NaN and everything non-finite met with a zero one.
-    // What no column sees (last_lo .. of the wave's columns) may be memory nobody has written: zero.
-    __device__ __forceinline__ void weigh_edge(int hb, uint4 v, const uint4 (&P)[CB], int pg, int min_lo, int max_hi) {
-        const int gq = (threadIdx.x & 63) >> 4;
-        uint32_t w[4] = {v.x, v.y, v.z, v.w}, pos[4], neg[4], nan[4], any = 0;
+    // What lies outside min_lo .. max_hi no column sees; it may be memory nobody has written, and counts as zero.
+    // Words hold two bf16; the tests work on both halves without a carry between.
+    __device__ __forceinline__ void weigh_edge(const uint4 (&vf)[2 * NK], const uint4 (&P)[CB], int pg, int min_lo, int max_hi) {
+        uint32_t in[4], any = 0;
+        seen_words(in, min_lo, max_hi, pg);
+        auto inside = [&](uint4 v) { return make_uint4(v.x & in[0], v.y & in[1], v.z & in[2], v.w & in[3]); };
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            pos[i] = neg[i] = nan[i] = 0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int e = 2 * i + h, p = pg + 16 * (e >> 2) + 4 * gq + (e & 3);
-                const uint32_t x = (w[i] >> (16 * h)) & 0xffffu, one = 0x3f80u << (16 * h), keep = ~(0xffffu << (16 * h));
-                const bool out = p < min_lo || p > max_hi, odd = !out && (x & 0x7f80u) == 0x7f80u;
-                if (out || odd) w[i] &= keep;
-                if (odd) {
-                    any = 1;
-                    if (x & 0x7fu) nan[i] |= one;
-                    else if (x >> 15) neg[i] |= one;
-                    else pos[i] |= one;
-                }
-            }
+        for (int hb = 0; hb < 2 * NK; ++hb) {
+            const uint4 v = inside(vf[hb]);
+            any |= odd_bits(v.x) | odd_bits(v.y) | odd_bits(v.z) | odd_bits(v.w);
         }
-        weigh(hb, make_uint4(w[0], w[1], w[2], w[3]), P);
-        if (!__any(any != 0)) return;
-        const uint4 vp = make_uint4(pos[0], pos[1], pos[2], pos[3]), vn = make_uint4(neg[0], neg[1], neg[2], neg[3]),
-                    vx = make_uint4(nan[0], nan[1], nan[2], nan[3]),
-                    va = make_uint4(pos[0] | neg[0] | nan[0], pos[1] | neg[1] | nan[1], pos[2] | neg[2] | nan[2], pos[3] | neg[3] | nan[3]);
-        const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (!__any(any != 0)) {
 #pragma unroll
-        for (int j = 0; j < CB; ++j) {
-            const uint32_t pw[4] = {P[j].x, P[j].y, P[j].z, P[j].w};
-            uint32_t some[4], none[4];                       // 1 where the column sees a position with P > 0, with P = 0
+            for (int hb = 0; hb < 2 * NK; ++hb) weigh(hb, inside(vf[hb]), P);
+            return;
+        }
+#pragma unroll
+        for (int hb = 0; hb < 2 * NK; ++hb) {
+            const uint4 v = inside(vf[hb]);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t fin[4], pos[4], neg[4], nan[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                some[i] = none[i] = 0;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int e = 2 * i + h, p = pg + 16 * (e >> 2) + 4 * gq + (e & 3);
-                    const bool sees = p >= lo[j] && p <= hi[j], positive = (pw[i] >> (16 * h)) & 0xffffu;
-                    const uint32_t one = 0x3f80u << (16 * h);
-                    if (sees && positive) some[i] |= one;
-                    if (sees && !positive) none[i] |= one;
-                }
+                const uint32_t odd = half_mask(odd_bits(w[i])), sign = half_mask(w[i] & 0x80008000u);
+                const uint32_t frac = half_mask(((((w[i] & 0x007f007fu) + 0x007f007fu) & 0x00800080u) << 8));
+                fin[i] = w[i] & ~odd;
+                nan[i] = odd & frac & 0x3f803f80u;
+                neg[i] = odd & ~frac & sign & 0x3f803f80u;
+                pos[i] = odd & ~frac & ~sign & 0x3f803f80u;
             }
-            const uint4 ps = make_uint4(some[0], some[1], some[2], some[3]), pz = make_uint4(none[0], none[1], none[2], none[3]);
-            const floatx4 up = mfma(vp, ps, zero), down = mfma(vn, ps, zero), bad = mfma(va, pz, mfma(vx, ps, zero));
+            weigh(hb, make_uint4(fin[0], fin[1], fin[2], fin[3]), P);
+            const uint4 vp = make_uint4(pos[0], pos[1], pos[2], pos[3]), vn = make_uint4(neg[0], neg[1], neg[2], neg[3]),
+                        vx = make_uint4(nan[0], nan[1], nan[2], nan[3]),
+                        va = make_uint4(pos[0] | neg[0] | nan[0], pos[1] | neg[1] | nan[1], pos[2] | neg[2] | nan[2], pos[3] | neg[3] | nan[3]);
+            const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (up[r] > 0.f) O[j][hb][r] += INFINITY;
-                if (down[r] > 0.f) O[j][hb][r] -= INFINITY;
-                if (bad[r] > 0.f) O[j][hb][r] = NAN;
+            for (int j = 0; j < CB; ++j) {
+                const uint32_t pw[4] = {P[j].x, P[j].y, P[j].z, P[j].w};
+                uint32_t sees[4], some[4], none[4];          // 1 where the column sees a position with P > 0, with P = 0
+                seen_words(sees, lo[j], hi[j], pg);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t positive = half_mask(((pw[i] & 0x7fff7fffu) + 0x7fff7fffu) & 0x80008000u);
+                    some[i] = sees[i] & positive & 0x3f803f80u;
+                    none[i] = sees[i] & ~positive & 0x3f803f80u;
+                }
+                const uint4 ps = make_uint4(some[0], some[1], some[2], some[3]), pz = make_uint4(none[0], none[1], none[2], none[3]);
+                const floatx4 up = mfma(vp, ps, zero), down = mfma(vn, ps, zero), bad = mfma(va, pz, mfma(vx, ps, zero));
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    O[j][hb][r] += up[r] > 0.f ? INFINITY : 0.f;
+                    O[j][hb][r] -= down[r] > 0.f ? INFINITY : 0.f;
+                    O[j][hb][r] = bad[r] > 0.f ? NAN : O[j][hb][r];
+                }
             }
         }
     }
@@ -223,44 +293,38 @@ k_bf16_paged_rows(AttnArgs a) {
     const char* pool = a.pv.pool;
     const int n_mine = max(0, (gb - ga - w + 3) >> 2);       // this wave's groups: ga + w, ga + w + 4, ..
     uint32_t where = 0;
-    for (int i = 0; i < n_mine; ++i) {
-        if ((i & 63) == 0) {
-            const int grp = ga + w + 4 * (i + lane);
-            where = grp < gb ? pool_group(a.pv, a.st, s, g, grp) : NO_GROUP;
-        }
-        const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)where, i & 63);
-        if (at == NO_GROUP) continue;
-        const uint4* kv = reinterpret_cast<const uint4*>(pool + (uint64_t)at * (HD * 128)) + lane;
-        const int pg = (ga + w + 4 * i) << 5;
-        const bool edge = pg + 31 > first || pg < max_lo;
-        constexpr int EARLY = NK > 6 ? NK / 2 : 2 * NK;          // values asked for before the scores: as many as fit the registers
-        uint4 kf[2 * NK], vf[2 * NK];
-#pragma unroll
-        for (int f = 0; f < 2 * NK; ++f) kf[f] = kv[f * 64];
-#pragma unroll
-        for (int f = 0; f < EARLY; ++f) vf[f] = kv[(2 * NK + f) * 64];
-        floatx4 S[CB][2];
-#pragma unroll
-        for (int j = 0; j < CB; ++j) S[j][0] = S[j][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < NK; ++k)
-#pragma unroll
-            for (int j = 0; j < CB; ++j) {
-                S[j][0] = mfma(kf[k], col.q[j][k], S[j][0]);
-                S[j][1] = mfma(kf[NK + k], col.q[j][k], S[j][1]);
+    // whether a column does not see all of a group is settled by range, so the loop over the groups that all see has no test:
+    // edge before a0 (the window's start) and from a1 on (the rows' own positions)
+    auto mine_from = [&](int grp) { return min(max((grp - ga - w + 3) >> 2, 0), n_mine); };
+    const int a0 = mine_from((max_lo + 31) >> 5), a1 = max(a0, mine_from((first + 1) >> 5));
+    auto run = [&](auto edge, int from, int to) {
+        for (int i = from; i < to; ++i) {
+            if ((i & 63) == 0 || i == from) {
+                const int grp = ga + w + 4 * ((i & ~63) + lane);
+                where = grp < gb ? pool_group(a.pv, a.st, s, g, grp) : NO_GROUP;
             }
-        if constexpr (EARLY < 2 * NK) __builtin_amdgcn_sched_barrier(0);
+            const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)where, i & 63);
+            if (at == NO_GROUP) continue;
+            const uint4* kv = reinterpret_cast<const uint4*>(pool + (uint64_t)at * (HD * 128)) + lane;
+            const int pg = (ga + w + 4 * i) << 5;
+            constexpr int EARLY = NK > 6 ? NK / 2 : 2 * NK;  // values asked for before the scores: as many as fit the registers
+            uint4 kf[2 * NK], vf[2 * NK];
 #pragma unroll
-        for (int f = EARLY; f < 2 * NK; ++f) vf[f] = kv[(2 * NK + f) * 64];
-        uint4 P[CB];
-        col.softmax(S, P, a.scale2, edge, pg);
-        if (edge) {
+            for (int f = 0; f < 2 * NK; ++f) kf[f] = kv[f * 64];
 #pragma unroll
-            for (int hb = 0; hb < 2 * NK; ++hb) col.weigh_edge(hb, vf[hb], P, pg, min_lo, sr.len - 1);
-        } else {
+            for (int f = 0; f < EARLY; ++f) vf[f] = kv[(2 * NK + f) * 64];
+            floatx4 S[CB][2];
+            col.scores(kf, S);
+            if constexpr (EARLY < 2 * NK) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int hb = 0; hb < 2 * NK; ++hb) col.weigh(hb, vf[hb], P);
+            for (int f = EARLY; f < 2 * NK; ++f) vf[f] = kv[(2 * NK + f) * 64];
+            col.template take<edge.value>(S, vf, a.scale2, pg, min_lo, sr.len - 1);
         }
+    };
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {
+        run(std::true_type{}, part == 0 ? 0 : a1, part == 0 ? a0 : n_mine);
+        if (part == 0) run(std::false_type{}, a0, a1);
     }
 
     // join the waves: maxima and sums first, then the weighted sums, a wave two features blocks of every four
@@ -268,7 +332,7 @@ k_bf16_paged_rows(AttnArgs a) {
     for (int j = 0; j < CB; ++j) {
         const float l = quad_sum(col.l[j]);
         if (lane < 16) {
-            sm[w][16 * j + n16] = col.m[j];
+            sm[w][16 * j + n16] = col.maximum(j);
             sl[w][16 * j + n16] = (col.seen >> j) & 1u ? l : -1.f;
         }
     }
@@ -339,7 +403,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
     const int lane = threadIdx.x & 63, n16 = lane & 15, w = to_scalar(threadIdx.x >> 6);
     const int cw = c0 + w * 16 * CB;                         // the wave's columns and the positions they see
     const int w_first = first + cw / a.G, w_last = cw < n_cols ? first + (min(cw + 16 * CB, n_cols) - 1) / a.G : -1;
-    const int min_lo = lowest_seen(w_first, a.window), max_lo = lowest_seen(w_last, a.window);
+    const int min_lo = lowest_seen(w_first, a.window);
 
     Columns<NK, CB> col;
     col.start(a, g, cw, n_cols, first, sr.row0);
@@ -366,46 +430,45 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
         asm volatile("" : "+v"(where));
         issue(0, where);
     }
-    for (int t = 0; t < n_st; ++t) {
-        // this wave's part of the stage has landed; after the barrier everybody's has, and the other buffer has been read
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        const int i0 = SG * t;
-        if (t + 1 < n_st) {
-            where_next = where;
-            if (((i0 + SG) & 63) == 0) where_next = look_up(i0 + SG);
-            issue(t + 1, where_next);
-        }
-#pragma unroll 1
-        for (int k = 0; k < SG; ++k) {
-            const int pg = (ga + i0 + k) << 5;
-            if (ga + i0 + k >= gb || pg > w_last) break;
-            if (pg + 31 < min_lo || (uint32_t)__builtin_amdgcn_readlane((int)where, (i0 + k) & 63) == NO_GROUP) continue;
-            const bool edge = pg + 31 > w_first || pg < max_lo || w_last < 0;
-            const uint4* kv = lds + ((t & 1) * SG + k) * KIB * 64 + lane;
-            uint4 kf[2 * NK];
-#pragma unroll
-            for (int f = 0; f < 2 * NK; ++f) kf[f] = kv[f * 64];
-            floatx4 S[CB][2];
-#pragma unroll
-            for (int j = 0; j < CB; ++j) S[j][0] = S[j][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int f = 0; f < NK; ++f)
-#pragma unroll
-                for (int j = 0; j < CB; ++j) {
-                    S[j][0] = mfma(kf[f], col.q[j][f], S[j][0]);
-                    S[j][1] = mfma(kf[NK + f], col.q[j][f], S[j][1]);
-                }
-            uint4 P[CB];
-            col.softmax(S, P, a.scale2, edge, pg);
-            if (edge) {
-#pragma unroll
-                for (int hb = 0; hb < 2 * NK; ++hb) col.weigh_edge(hb, kv[(2 * NK + hb) * 64], P, pg, min_lo, w_last);
-            } else {
-#pragma unroll
-                for (int hb = 0; hb < 2 * NK; ++hb) col.weigh(hb, kv[(2 * NK + hb) * 64], P);
+    // stages in which every column of the tile sees every position: from a0 to a1 (the window starts before, the rows' own
+    // positions come after); their loop tests nothing
+    const int a0 = min(max((lowest_seen(first + t1, a.window) + 31) / 32 - ga + SG - 1, 0) / SG, n_st);
+    const int a1 = max(a0, min(max(((first + t0 + 1) >> 5) - ga, 0) / SG, n_st));
+    auto run = [&](auto edge, int from, int to) {
+        for (int t = from; t < to; ++t) {
+            // this wave's part of the stage has landed; after the barrier everybody's has, and the other buffer has been read
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            const int i0 = SG * t;
+            if (t + 1 < n_st) {
+                where_next = where;
+                if (((i0 + SG) & 63) == 0) where_next = look_up(i0 + SG);
+                issue(t + 1, where_next);
             }
+#pragma unroll 1
+            for (int k = 0; k < SG; ++k) {
+                const int pg = (ga + i0 + k) << 5;
+                if (pg > w_last || (edge.value && ga + i0 + k >= gb)) break;
+                if ((edge.value && pg + 31 < min_lo) || (uint32_t)__builtin_amdgcn_readlane((int)where, (i0 + k) & 63) == NO_GROUP) continue;
+                const uint4* kv = lds + ((t & 1) * SG + k) * KIB * 64 + lane;
+                uint4 kf[2 * NK], vf[2 * NK];
+#pragma unroll
+                for (int f = 0; f < 2 * NK; ++f) kf[f] = kv[f * 64];
+                floatx4 S[CB][2];
+                __builtin_amdgcn_sched_barrier(0);           // all keys are under way before the first MFMA ...
+                col.scores(kf, S);
+                __builtin_amdgcn_sched_barrier(0);           // ... and the values during the softmax
+#pragma unroll
+                for (int f = 0; f < 2 * NK; ++f) vf[f] = kv[(2 * NK + f) * 64];
+                __builtin_amdgcn_sched_barrier(0);
+                col.template take<edge.value>(S, vf, a.scale2, pg, min_lo, w_last);
+            }
+            where = where_next;
         }
-        where = where_next;
+    };
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {
+        run(std::true_type{}, part == 0 ? 0 : a1, part == 0 ? a0 : n_st);
+        if (part == 0) run(std::false_type{}, a0, a1);
     }
 
     const bool last = n_shares == 1, wide = wide_o(a.out);
@@ -418,7 +481,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
         if (c >= n_cols) continue;
         const int64_t at = block + c - c0;
         const ColumnOut dst{last ? out_row(a, g, c, sr.row0) : nullptr, last ? nullptr : a.part + at * HD, wide};
-        if (!last && lane < 16) a.stat[at] = make_float2(col.m[j], seen ? l : -1.f);
+        if (!last && lane < 16) a.stat[at] = make_float2(col.maximum(j), seen ? l : -1.f);
         const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
 #pragma unroll
         for (int hb = 0; hb < 2 * NK; ++hb) dst.put(16 * hb + 4 * (lane >> 4), seen ? col.O[j][hb] * inv : floatx4{0.f, 0.f, 0.f, 0.f});
