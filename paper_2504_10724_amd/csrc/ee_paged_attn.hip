@@ -172,11 +172,9 @@ template <int NK, int CB> struct Columns {
             }
     }
 
-    // softmax and second product of a group at pg with the values vf
+    // second product of a group at pg with the values vf
     template <bool EDGE>
-    __device__ __forceinline__ void take(const floatx4 (&S)[CB][2], const uint4 (&vf)[2 * NK], float scale2, int pg, int min_lo, int max_hi) {
-        uint4 P[CB];
-        softmax<EDGE>(S, P, scale2, pg);
+    __device__ __forceinline__ void weigh_group(const uint4 (&vf)[2 * NK], const uint4 (&P)[CB], int pg, int min_lo, int max_hi) {
         if constexpr (EDGE) {
             weigh_edge(vf, P, pg, min_lo, max_hi);
         } else {
@@ -318,7 +316,9 @@ k_bf16_paged_rows(AttnArgs a) {
             if constexpr (EARLY < 2 * NK) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int f = EARLY; f < 2 * NK; ++f) vf[f] = kv[(2 * NK + f) * 64];
-            col.template take<edge.value>(S, vf, a.scale2, pg, min_lo, sr.len - 1);
+            uint4 P[CB];
+            col.template softmax<edge.value>(S, P, a.scale2, pg);
+            col.template weigh_group<edge.value>(vf, P, pg, min_lo, sr.len - 1);
         }
     };
 #pragma unroll 1
@@ -413,61 +413,71 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
         for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(col.q[j][k].x), "+v"(col.q[j][k].y), "+v"(col.q[j][k].z), "+v"(col.q[j][k].w));
 
     const unsigned lane_bytes = (unsigned)lane * 16u, lds0 = (unsigned)(size_t)lds;
-    const int n_st = (gb - ga + SG - 1) / SG;
-    uint32_t where = NO_GROUP, where_next = NO_GROUP;        // of the 64 groups around the current stage, and of the next 64
+    const int n = gb - ga, n_st = (n + SG - 1) / SG;
+    uint32_t now = NO_GROUP, then = NO_GROUP;                // pool groups of the 64 groups around the one at work, around the one asked for
     auto look_up = [&](int i) { return ga + i + lane < gb ? pool_group(a.pv, a.st, s, g, ga + i + lane) : NO_GROUP; };
-    // a wave sends SG NK of the SG 4 NK KiB of a stage; a group that is not there is replaced by the pool's first
-    auto issue = [&](int t, uint32_t known) {
-        const int k = w * SG / 4, i = (SG * t + k) & 63;
-        const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)known, i);
-        const char* src = a.pv.pool + (at == NO_GROUP ? 0ull : (uint64_t)at * (HD * 128)) + (w * SG % 4) * NK * 1024;
-        const unsigned dst = lds0 + (unsigned)((t & 1) * SG * KIB + w * SG * NK) * 1024u;
+    // a wave sends SG NK of the SG 4 NK KiB of stage t; a group that is not there is replaced by the pool's first
+    auto issue = [&](int t) {
+        const int part = w * SG;
+        if ((SG * t & 63) == 0) {
+            then = look_up(SG * t);
+            asm volatile("" : "+v"(then));                   // arrived before the stage is under way
+        }
+        const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)then, (SG * t + part / 4) & 63);
+        const char* src = a.pv.pool + (at == NO_GROUP ? 0ull : (uint64_t)at * (HD * 128)) + part % 4 * NK * 1024;
+        const unsigned dst = lds0 + (unsigned)((t & 1) * SG * KIB + part * NK) * 1024u;
 #pragma unroll
         for (int p = 0; p < SG * NK; ++p) load_kib(src + p * 1024, lane_bytes, dst + (unsigned)p * 1024u);
     };
-    if (n_st > 0) {
-        where = look_up(0);
-        asm volatile("" : "+v"(where));
-        issue(0, where);
+    // this wave's part of a stage has landed and it has read the one before; after the barrier so has everybody's and everybody
+    auto meet = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    uint4 kf[2 * NK];
+    auto group = [&](int i) { return lds + i % (2 * SG) * KIB * 64 + lane; };
+    auto load_keys = [&](int i) {
+#pragma unroll
+        for (int f = 0; f < 2 * NK; ++f) kf[f] = group(i)[f * 64];
+    };
+    if (n > 0) {
+        issue(0);
+        now = then;
+        meet();
+        if (n_st > 1) issue(1);
+        load_keys(0);
     }
-    // stages in which every column of the tile sees every position: from a0 to a1 (the window starts before, the rows' own
-    // positions come after); their loop tests nothing
-    const int a0 = min(max((lowest_seen(first + t1, a.window) + 31) / 32 - ga + SG - 1, 0) / SG, n_st);
-    const int a1 = max(a0, min(max(((first + t0 + 1) >> 5) - ga, 0) / SG, n_st));
+    // groups that every column of the tile sees whole: from a0 to a1 (the window starts before, the rows' own positions come after);
+    // their loop tests nothing
+    const int a0 = min(max((lowest_seen(first + t1, a.window) + 31) / 32 - ga, 0), n), a1 = max(a0, min(((first + t0 + 1) >> 5) - ga, n));
     auto run = [&](auto edge, int from, int to) {
-        for (int t = from; t < to; ++t) {
-            // this wave's part of the stage has landed; after the barrier everybody's has, and the other buffer has been read
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            const int i0 = SG * t;
-            if (t + 1 < n_st) {
-                where_next = where;
-                if (((i0 + SG) & 63) == 0) where_next = look_up(i0 + SG);
-                issue(t + 1, where_next);
-            }
-#pragma unroll 1
-            for (int k = 0; k < SG; ++k) {
-                const int pg = (ga + i0 + k) << 5;
-                if (pg > w_last || (edge.value && ga + i0 + k >= gb)) break;
-                if ((edge.value && pg + 31 < min_lo) || (uint32_t)__builtin_amdgcn_readlane((int)where, (i0 + k) & 63) == NO_GROUP) continue;
-                const uint4* kv = lds + ((t & 1) * SG + k) * KIB * 64 + lane;
-                uint4 kf[2 * NK], vf[2 * NK];
-#pragma unroll
-                for (int f = 0; f < 2 * NK; ++f) kf[f] = kv[f * 64];
+        for (int i = from; i < to; ++i) {
+            const int pg = (ga + i) << 5;
+            if ((i & 63) == 0 && i > 0) now = then;
+            const bool works = pg <= w_last && (!edge.value || pg + 31 >= min_lo) &&
+                               (uint32_t)__builtin_amdgcn_readlane((int)now, i & 63) != NO_GROUP;
+            uint4 vf[2 * NK], P[CB];
+            if (works) {
                 floatx4 S[CB][2];
-                __builtin_amdgcn_sched_barrier(0);           // all keys are under way before the first MFMA ...
                 col.scores(kf, S);
-                __builtin_amdgcn_sched_barrier(0);           // ... and the values during the softmax
+                __builtin_amdgcn_sched_barrier(0);           // the values are under way during the softmax
 #pragma unroll
-                for (int f = 0; f < 2 * NK; ++f) vf[f] = kv[(2 * NK + f) * 64];
+                for (int f = 0; f < 2 * NK; ++f) vf[f] = group(i)[(2 * NK + f) * 64];
                 __builtin_amdgcn_sched_barrier(0);
-                col.template take<edge.value>(S, vf, a.scale2, pg, min_lo, w_last);
+                col.template softmax<edge.value>(S, P, a.scale2, pg);
             }
-            where = where_next;
+            if (i + 1 < n) {
+                if ((i + 1) % SG == 0) {                     // the stage is in registers: its buffer is free
+                    meet();
+                    if ((i + 1) / SG + 1 < n_st) issue((i + 1) / SG + 1);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                load_keys(i + 1);                            // the next keys during the second product
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (works) col.template weigh_group<edge.value>(vf, P, pg, min_lo, w_last);
         }
     };
 #pragma unroll 1
     for (int part = 0; part < 2; ++part) {
-        run(std::true_type{}, part == 0 ? 0 : a1, part == 0 ? a0 : n_st);
+        run(std::true_type{}, part == 0 ? 0 : a1, part == 0 ? a0 : n);
         if (part == 0) run(std::false_type{}, a0, a1);
     }
 
