@@ -48,7 +48,7 @@ class ee_rope_config(C.Structure):
                 ("low", C.c_float), ("high", C.c_float), ("magnitude", C.c_float)]
 
 
-class ee_heads(C.Structure):
+class ee_heads(C.Structure):      # arguments of this type are declared as void pointers: ee_heads by reference, or its bytes
     _fields_ = [("dev", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
@@ -112,15 +112,13 @@ _SIGS = {
     "ee_pht_push_step": (_i, [_vp, _vp, _vp, _vp]),
     "ee_rope_create": (_i, [C.POINTER(ee_rope_config), C.POINTER(_vp)]),
     "ee_rope_destroy": (_i, [_vp]),
-    "ee_rope_apply": (_i, [_vp, _i, C.POINTER(ee_heads), C.POINTER(ee_heads), _vp, _i, _i, _i, _vp, _vp]),
+    "ee_rope_apply": (_i, [_vp, _i, _vp, _vp, _vp, _i, _i, _i, _vp, _vp]),
     "ee_paged_pool_bytes": (_sz, [C.POINTER(ee_paged_config)]),
     "ee_paged_bind": (_i, [C.POINTER(ee_paged_config), _vp, _sz, C.POINTER(_vp)]),
     "ee_paged_destroy": (_i, [_vp]),
-    "ee_paged_append": (_i, [_vp, _i, C.POINTER(ee_paged_step), _vp, C.POINTER(ee_heads), C.POINTER(ee_heads),
-                             C.POINTER(ee_heads), C.POINTER(ee_heads), _i, _vp]),
+    "ee_paged_append": (_i, [_vp, _i, C.POINTER(ee_paged_step), _vp, _vp, _vp, _vp, _vp, _i, _vp]),
     "ee_paged_attention_workspace": (_sz, [_vp, _i, C.POINTER(ee_paged_step)]),
-    "ee_paged_attention": (_i, [_vp, _i, C.POINTER(ee_paged_step), C.POINTER(ee_heads), C.POINTER(ee_heads), _i, _f, _i,
-                                _vp, _sz, _vp]),
+    "ee_paged_attention": (_i, [_vp, _i, C.POINTER(ee_paged_step), _vp, _vp, _i, _f, _i, _vp, _sz, _vp]),
     "ee_timing_enable": (_i, [_i]),
     "ee_timing_reset": (_i, []),
     "ee_timing_read": (_i, [_i, C.POINTER(_i), C.POINTER(_f)]),

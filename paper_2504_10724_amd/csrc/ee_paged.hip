@@ -53,6 +53,8 @@ template <int V> __device__ __forceinline__ Item<V> make_item(const RopeView& ro
     const float2* t = reinterpret_cast<const float2*>(rope.table) + (int64_t)pos * (rope.rot >> 1);
     it.partner = -1;
     it.turns = false;
+#pragma unroll
+    for (int e = 0; e < V; ++e) { it.c[e] = 1.f; it.s[e] = 0.f; }
     if (u < np) {
         it.turns = true;
         it.at = rope.interleaved ? 2 * u : V * u;
@@ -124,12 +126,10 @@ __global__ void __launch_bounds__(256)
 k_rope_apply(RopeView rope, int hd, HeadsView x, HeadsView y, const int32_t* __restrict__ pos, int n_tokens, int n_heads, int n_slices,
              int32_t* status) {
     const int items = items_per_head(V, hd, rope.rot, rope.interleaved);
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t rest = i / items;
-    const int u = (int)(i - rest * items);
-    const int64_t t64 = rest / n_slices;
-    if (t64 >= n_tokens) return;
-    const int t = (int)t64, p = pos[t];
+    const unsigned i = blockIdx.x * 256u + threadIdx.x;      // the launch holds 2^31 threads at most
+    const unsigned rest = i / (unsigned)items, t = rest / (unsigned)n_slices;
+    if (t >= (unsigned)n_tokens) return;
+    const int u = (int)(i - rest * items), p = pos[t];
     if (p < 0 || p >= rope.max_pos) {
         if (status) atomicOr(status, 1);
         return;
@@ -137,7 +137,8 @@ k_rope_apply(RopeView rope, int hd, HeadsView x, HeadsView y, const int32_t* __r
     const Item<V> it = make_item<V>(rope, p, u);
     const T* xr = (const T*)x.p + t * x.ts;
     T* yr = (T*)y.p + t * y.ts;
-    for (int h = (int)(rest - t64 * n_slices); h < n_heads; h += n_slices) {
+#pragma unroll 4
+    for (int h = (int)(rest - t * n_slices); h < n_heads; h += n_slices) {
         T* yh = yr + h * y.hs;
         turn_item<V>(it, xr + h * x.hs, [&](int at, const float (&v)[V]) { store_row<V>(yh + at, v); });
     }
@@ -166,8 +167,12 @@ int launch_rope_apply(int dtype, const RopeView& rope, int hd, const HeadsView& 
 
 // ------------------------------------------------------------------ append
 // A workgroup takes the new rows of one sequence that fall into one group of 32 positions (a page is whole groups), and `heads`
-// kv heads with the query heads that go with them.  unit = sequence slot: sequence s has the units from q_start[s]/32 + 2 s on
-// (two more than its whole groups of 32 rows: the first and the last may be partial), or `per_seq` each where that is at most 2.
+// kv heads with the query heads that go with them.  Units: sequence s has the ones from q_start[s]/32 + 2 s on (two more than its
+// whole groups of 32 rows: the first and the last may be partial), or `per_seq` each where that is at most 2.
+//
+// Keys and queries: thread = (item of a head, row, first head); it keeps the row's cos and sin over its heads.  A wave's 16-byte
+// items of eight rows fill whole 128-byte lines of the keys' order.  Values (bf16): 16 bytes of a group hold eight positions of
+// one feature, so a thread reads two features of eight rows and writes 32 bytes; positions that are not new keep their bytes.
 template <class T, int V>
 __global__ void __launch_bounds__(256)
 k_paged_append(PagedView pv, StepView st, RopeView rope, HeadsView k, HeadsView v, HeadsView q, HeadsView qo, int G, int heads, int per_seq) {
@@ -176,61 +181,103 @@ k_paged_append(PagedView pv, StepView st, RopeView rope, HeadsView k, HeadsView 
     const int unit = (int)blockIdx.x - (per_seq <= 2 ? s * per_seq : slot_base(st.q_start, st.n_tokens, s, 32, 2));
     const int first = sr.len - sr.n;                         // position of the sequence's first new row
     if (unit == 0 && first < 0 && sr.n > 0 && threadIdx.x == 0 && st.status) atomicOr(st.status, 1);
-    const int grp = (max(first, 0) >> 5) + unit;
-    const int p0 = grp << 5, r0 = max(max(first, 0) - p0, 0), r1 = min(sr.len - p0, 32);
+    const int p0 = ((max(first, 0) >> 5) + unit) << 5, r0 = max(max(first, 0) - p0, 0);
+    int r1 = min(sr.len - p0, 32);
     if (sr.n == 0 || r0 >= r1) return;
     const int page = st.pages[(int64_t)s * st.pages_per_seq + p0 / pv.page_size];
-    const bool mapped = page >= 0 && page < pv.n_pages;
-    const int g0 = blockIdx.y * heads, ng = min(heads, pv.n_kv_heads - g0);
-    const int at0 = p0 % pv.page_size;                       // of the group in its page
+    const bool beyond = p0 + r1 > rope.max_pos;              // rows that are not in the rotary table
+    r1 = min(r1, rope.max_pos - p0);
+    const int g0 = blockIdx.y * heads, ng = min(heads, pv.n_kv_heads - g0), hd = pv.hd, ps = pv.page_size, nr = r1 - r0;
+    const int at0 = p0 % ps;                                 // of the group in its page
     const int64_t row0 = (int64_t)sr.row0 + p0 - first;      // of position p0 (its own row may not exist)
-    const int hd = pv.hd, nr = r1 - r0;
-    if (threadIdx.x == 0 && st.status && (!mapped || p0 + r1 > rope.max_pos)) atomicOr(st.status, 1);
-    T* pool = (T*)pv.pool + ((int64_t)page * pv.n_kv_heads + g0) * (2LL * pv.page_size * hd);
-    const int64_t block = 2LL * pv.page_size * hd;
+    const int64_t block = 2LL * ps * hd;
+    T* pool = (T*)pv.pool + ((int64_t)page * pv.n_kv_heads + g0) * block;
 
-    const int items = items_per_head(V, hd, rope.rot, rope.interleaved);
-    const int n_k = mapped ? ng * nr * items : 0, n_v = mapped ? ng * nr * (hd / V) : 0, n_q = ng * G * nr * items;
-    for (int i = threadIdx.x; i < n_k + n_v + n_q; i += 256) {
-        if (i < n_k) {
-            const int r = r0 + i % nr, rest = i / nr, u = rest % items, g = rest / items, p = p0 + r;
-            if (p >= rope.max_pos) continue;
-            const Item<V> it = make_item<V>(rope, p, u);
-            T* dst = pool + g * block;
-            turn_item<V>(it, (const T*)k.p + (row0 + r) * k.ts + (g0 + g) * k.hs,
-                         [&](int at, const float (&x)[V]) { store_row<V>(dst + page_k<T>(at0 + r, at, hd, pv.page_size), x); });
-        } else if (i < n_k + n_v) {
-            const int j = i - n_k, n_i = hd / V, u = j % n_i, rest = j / n_i, r = r0 + rest % nr, g = rest / nr;
-            if (p0 + r >= rope.max_pos) continue;
-            const T* src = (const T*)v.p + (row0 + r) * v.ts + (g0 + g) * v.hs + V * u;
-            T* dst = pool + g * block;
-            float x[V];
-            load_row<V>(src, x);
-#pragma unroll
-            for (int e = 0; e < V; ++e) dst[page_v<T>(at0 + r, V * u + e, hd, pv.page_size)] = from_f32<T>(x[e]);
-        } else {
-            const int j = i - n_k - n_v, u = j % items, rest = j / items, h = rest % (ng * G), r = r0 + rest / (ng * G), p = p0 + r;
-            if (p >= rope.max_pos) continue;
-            const Item<V> it = make_item<V>(rope, p, u);
-            T* dst = (T*)qo.p + (row0 + r) * qo.ts + (g0 * G + h) * qo.hs;
-            turn_item<V>(it, (const T*)q.p + (row0 + r) * q.ts + (g0 * G + h) * q.hs,
-                         [&](int at, const float (&x)[V]) { store_row<V>(dst + at, x); });
+    const bool mapped = page >= 0 && page < pv.n_pages;      // looked at when the rows are there: the page comes in beside them
+    const int items = items_per_head(V, hd, rope.rot, rope.interleaved), nh = ng * (G + 1);
+    const int slots = 256 / items, slot = (int)threadIdx.x / items, u = (int)threadIdx.x - slot * items;    // items <= hd <= 256
+    const int rows = min(nr, slots), steps = slots / rows;   // rows and heads at a time
+    if (slot < rows * steps) {
+        for (int r = r0 + slot % rows; r < r1; r += rows) {
+            const Item<V> it = make_item<V>(rope, p0 + r, u);
+            const int64_t t = row0 + r;
+#pragma unroll 4
+            for (int h = slot / rows; h < nh; h += steps) {
+                if (h < nh - ng) {
+                    const int hq = g0 * G + h;
+                    T* dst = (T*)qo.p + t * qo.ts + hq * qo.hs;
+                    turn_item<V>(it, (const T*)q.p + t * q.ts + hq * q.hs, [&](int at, const float (&x)[V]) { store_row<V>(dst + at, x); });
+                } else {
+                    const int g = h - (nh - ng);
+                    T* dst = pool + g * block;
+                    turn_item<V>(it, (const T*)k.p + t * k.ts + (g0 + g) * k.hs, [&](int at, const float (&x)[V]) {
+                        if (mapped) store_row<V>(dst + page_k<T>(at0 + r, at, hd, ps), x);
+                    });
+                }
+            }
         }
     }
+
+    const int back = 255 - (int)threadIdx.x;                 // a single row leaves threads without keys or queries: they start here
+    if constexpr (sizeof(T) == 2 && V > 1) {
+        // quads of positions 4 d + i and 16 + 4 d + i; a single row is in one of them
+        const int d0 = nr == 1 ? (r0 & 15) >> 2 : 0, nd = nr == 1 ? 1 : 4, pairs = hd / 2;
+        for (int i = back; i < ng * nd * pairs; i += 256) {
+            const int f = i % pairs, rest = i / pairs, d = d0 + rest % nd, g = rest / nd;
+            const bf16_t* src = (const bf16_t*)v.p + (g0 + g) * v.hs + 2 * f;
+            uint32_t w[8];
+            bool all = true;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int r = 4 * d + 16 * (e >> 2) + (e & 3);
+                const bool in = r >= r0 && r < r1;
+                all = all && in;
+                w[e] = in ? *reinterpret_cast<const uint32_t*>(src + (row0 + r) * v.ts) : 0u;
+            }
+            bf16_t* dst = (bf16_t*)pool + g * block + page_v<bf16_t>(at0 + 4 * d, 2 * f, hd, ps);
+            if (!mapped) continue;
+            if (all) {
+                uint32_t lo[4], hi[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    lo[e] = (w[2 * e] & 0xffffu) | (w[2 * e + 1] << 16);
+                    hi[e] = (w[2 * e] >> 16) | (w[2 * e + 1] & 0xffff0000u);
+                }
+                reinterpret_cast<uint4*>(dst)[0] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                reinterpret_cast<uint4*>(dst)[1] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int r = 4 * d + 16 * (e >> 2) + (e & 3);
+                    if (r >= r0 && r < r1) { dst[e] = (bf16_t)w[e]; dst[8 + e] = (bf16_t)(w[e] >> 16); }
+                }
+            }
+        }
+    } else {
+        const int n_i = hd / V;
+        for (int i = back; i < ng * nr * n_i; i += 256) {
+            const int u = i % n_i, rest = i / n_i, r = r0 + rest % nr, g = rest / nr;
+            float x[V];
+            load_row<V>((const T*)v.p + (row0 + r) * v.ts + (g0 + g) * v.hs + V * u, x);
+            if (mapped) store_row<V>(pool + g * block + page_v<T>(at0 + r, V * u, hd, ps), x);
+        }
+    }
+    if (threadIdx.x == 0 && st.status && (!mapped || beyond)) atomicOr(st.status, 1);
 }
 
 int launch_paged_append(int dtype, const PagedView& pv, const StepView& st, const RopeView& rope, const HeadsView& k, const HeadsView& v,
                         const HeadsView& q, const HeadsView& q_out, int n_q_heads, hipStream_t s) {
     const int W = dtype == EE_BF16 ? 8 : 4;
     const bool wide = wide_rope(W, rope, pv.hd) && wide_rows(k, W) && wide_rows(v, W) && wide_rows(q, W) && wide_rows(q_out, W);
-    const int most = (st.max_q_len + 30) / 32 + 1;           // groups of 32 positions that max_q_len rows touch
+    const int most = (int)(((int64_t)st.max_q_len + 30) / 32 + 1);   // groups of 32 positions that max_q_len rows touch
     const int per_seq = most <= 2 ? most : 3;
     const int64_t units = per_seq <= 2 ? (int64_t)st.n_seqs * per_seq : (int64_t)st.n_tokens / 32 + 2LL * st.n_seqs;
-    const int G = n_q_heads / pv.n_kv_heads, heads = 1;
+    // one kv head a workgroup until there are eight workgroups a CU, then as many as keep that number
+    const int heads = (int)std::max<int64_t>(1, std::min<int64_t>(pv.n_kv_heads, units * pv.n_kv_heads / 2048));
     const dim3 grid((unsigned)units, (unsigned)((pv.n_kv_heads + heads - 1) / heads));
     auto kern = dtype == EE_BF16 ? (wide ? k_paged_append<bf16_t, 8> : k_paged_append<bf16_t, 1>)
                                  : (wide ? k_paged_append<float, 4> : k_paged_append<float, 1>);
-    hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, pv, st, rope, k, v, q, q_out, G, heads, per_seq);
+    hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, pv, st, rope, k, v, q, q_out, n_q_heads / pv.n_kv_heads, heads, per_seq);
     EE_LAUNCH_CHECK();
     return EE_OK;
 }

@@ -8,11 +8,12 @@ stream, libee does all the work.  What a server does with them, per layer and st
     out = attend(kv, layer, step, q)
 """
 import ctypes as C
+import struct
 
 import torch
 
 from . import capi as ee
-from .session import _ptr, _stream
+from .session import _stream
 
 _PAIRINGS = {"half": ee.EE_ROPE_HALF, "interleaved": ee.EE_ROPE_INTERLEAVED}
 _SCALINGS = {"none": ee.EE_ROPE_UNSCALED, "linear": ee.EE_ROPE_LINEAR, "base": ee.EE_ROPE_BASE, "bands": ee.EE_ROPE_BANDS}
@@ -23,19 +24,22 @@ def _refuse(what):
     raise ee.EEError(ee.EE_ERR_INVALID_ARG, what)
 
 
-def _heads(t, what, n_tokens, n_heads, hd, dtype):
-    """ee_heads of a tensor [n_tokens][n_heads][hd] whose features are contiguous"""
-    if tuple(t.shape) != (n_tokens, n_heads, hd) or t.dtype != dtype or not t.is_cuda:
-        _refuse(f"{what}: expected a device tensor {(n_tokens, n_heads, hd)} of {dtype}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    st = t.stride()
-    if st[2] != 1 and hd > 1:
+_pack_heads = struct.Struct("Pqq").pack      # an ee_heads as bytes, a fifth of the time a ctypes structure takes
+
+
+def _heads(t, what, shape, dtype):
+    """ee_heads of a device tensor [n_tokens][n_heads][hd] whose features are contiguous"""
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
+        _refuse(f"{what}: expected a device tensor {shape} of {dtype}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    token, head, feature = t.stride()
+    if feature != 1 and shape[2] > 1:
         _refuse(f"{what}: the features of a head must be contiguous")
-    return ee.ee_heads(t.data_ptr(), st[0], st[1])
+    return _pack_heads(t.data_ptr(), token, head)
 
 
 def _int32(t, what, n):
     """a contiguous int32 device tensor of n values"""
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or t.numel() != n:
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
         _refuse(f"{what}: expected a contiguous int32 device tensor of {n} values, got {t.numel()} of {t.dtype} on {t.device}")
     return t
 
@@ -68,14 +72,15 @@ class Rope:
     def apply(self, x, pos, *, out=None, inverse=False, status=None):
         """x [n][heads][head_dim] (float32 or bfloat16, any token and head stride) rotated at pos (int32 [n]); out may be x.
         inverse: by the negative angle, which is the gradient with respect to x of a result's gradient."""
-        if x.dim() != 3 or x.dtype not in _DTYPES:
-            _refuse(f"Rope.apply: x must be [tokens][heads][features] of float32 or bfloat16, got {tuple(x.shape)} of {x.dtype}")
-        n, heads, hd = x.shape
+        dtype, shape = x.dtype, x.shape
+        if len(shape) != 3 or dtype not in _DTYPES or shape[2] != self.cfg.head_dim:
+            _refuse(f"Rope.apply: x must be [tokens][heads][{self.cfg.head_dim}] of float32 or bfloat16, got {tuple(shape)} of {dtype}")
         if out is None:
-            out = torch.empty((n, heads, hd), dtype=x.dtype, device=x.device)
-        xh, yh = (_heads(t, "Rope.apply", n, heads, self.cfg.head_dim, x.dtype) for t in (x, out))
-        ee.check(self.lib.ee_rope_apply(self.h, _DTYPES[x.dtype], C.byref(xh), C.byref(yh), _ptr(_int32(pos, "Rope.apply: pos", n)), n, heads,
-                                        int(inverse), None if status is None else _ptr(_int32(status, "Rope.apply: status", 1)), _stream()))
+            out = torch.empty(shape, dtype=dtype, device=x.device)
+        n, heads, _ = shape
+        ee.check(self.lib.ee_rope_apply(self.h, _DTYPES[dtype], _heads(x, "Rope.apply", shape, dtype), _heads(out, "Rope.apply", shape, dtype),
+                                        _int32(pos, "Rope.apply: pos", n).data_ptr(), n, heads, inverse,
+                                        None if status is None else _int32(status, "Rope.apply: status", 1).data_ptr(), _stream()))
         return out
 
 
@@ -85,13 +90,13 @@ class PagedCache:
     def __init__(self, n_layers, n_pages, n_kv_heads, head_dim, page_size, dtype="bf16"):
         self.lib = ee.load()
         self.cfg = ee.ee_paged_config(n_layers, n_pages, n_kv_heads, head_dim, page_size, ee.EE_BF16 if dtype == "bf16" else ee.EE_F32)
-        self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.dtype, self.n_kv_heads, self.head_dim = (torch.bfloat16 if dtype == "bf16" else torch.float32), n_kv_heads, head_dim
         nbytes = self.lib.ee_paged_pool_bytes(C.byref(self.cfg))
         if nbytes == 0:
             raise ee.EEError(ee.EE_ERR_SHAPE, self.lib.ee_last_error().decode())
         self.pool = torch.empty(nbytes // self.dtype.itemsize, dtype=self.dtype, device="cuda")
         self.h = C.c_void_p()
-        ee.check(self.lib.ee_paged_bind(C.byref(self.cfg), _ptr(self.pool), nbytes, C.byref(self.h)))
+        ee.check(self.lib.ee_paged_bind(C.byref(self.cfg), self.pool.data_ptr(), nbytes, C.byref(self.h)))
 
     def close(self):
         if self.h:
@@ -106,7 +111,7 @@ class PagedCache:
 
     def workspace(self, step, n_q_heads):
         """what attend needs for this step and every step whose host figures are at most its; keep one per stream"""
-        nbytes = self.lib.ee_paged_attention_workspace(self.h, n_q_heads, C.byref(step.c))
+        nbytes = self.lib.ee_paged_attention_workspace(self.h, n_q_heads, step.ref)
         return torch.empty(max(nbytes, 1), dtype=torch.uint8, device="cuda")
 
 
@@ -122,39 +127,38 @@ class PagedStep:
         self.tensors = (_int32(q_start, "PagedStep: q_start", n + 1), _int32(kv_len, "PagedStep: kv_len", n),
                         _int32(pages, "PagedStep: pages", pages.numel()), None if status is None else _int32(status, "PagedStep: status", 1))
         self.c = ee.ee_paged_step(n, n_tokens, max_q_len, max_kv_len, pages.shape[1], *(None if t is None else t.data_ptr() for t in self.tensors))
-        self.n_tokens = n_tokens
+        self.n_tokens, self.ref = n_tokens, C.byref(self.c)
 
 
 def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
     """Keys (rotated by rope) and values [n_tokens][n_kv_heads][head_dim] to the rows' positions of `layer`; with q
     [n_tokens][n_q_heads][head_dim] also the rotated queries to q_out (default: a new tensor, which is returned)."""
-    n, c = step.n_tokens, kv.cfg
-    kh, vh = (_heads(t, "append", n, c.n_kv_heads, c.head_dim, kv.dtype) for t in (k, v))
+    dtype, shape = kv.dtype, (step.n_tokens, kv.n_kv_heads, kv.head_dim)
+    kh, vh = _heads(k, "append", shape, dtype), _heads(v, "append", shape, dtype)
     qh = qo = None
     n_q = 0
     if q is not None:
         n_q = q.shape[1]
+        shape = (step.n_tokens, n_q, kv.head_dim)
         if q_out is None:
-            q_out = torch.empty((n, n_q, c.head_dim), dtype=q.dtype, device=q.device)
-        qh, qo = (_heads(t, "append", n, n_q, c.head_dim, kv.dtype) for t in (q, q_out))
-        qh, qo = C.byref(qh), C.byref(qo)
-    ee.check(kv.lib.ee_paged_append(kv.h, layer, C.byref(step.c), None if rope is None else rope.h, C.byref(kh), C.byref(vh), qh, qo, n_q,
-                                    _stream()))
+            q_out = torch.empty(shape, dtype=dtype, device=q.device)
+        qh, qo = _heads(q, "append", shape, dtype), _heads(q_out, "append", shape, dtype)
+    ee.check(kv.lib.ee_paged_append(kv.h, layer, step.ref, None if rope is None else rope.h, kh, vh, qh, qo, n_q, _stream()))
     return q_out
 
 
 def attend(kv, layer, step, q, *, out=None, scale=None, window=0, workspace=None):
     """Attention of the step's rows q [n_tokens][n_q_heads][head_dim] over the cached positions of `layer`; scale defaults to
     1/sqrt(head_dim), window 0 is all earlier positions, workspace is kv.workspace's."""
-    n, c = step.n_tokens, kv.cfg
     if q.dim() != 3:
         _refuse(f"attend: q must be [tokens][heads][features], got {tuple(q.shape)}")
     heads = q.shape[1]
+    shape, dtype = (step.n_tokens, heads, kv.head_dim), kv.dtype
     if out is None:
-        out = torch.empty((n, heads, c.head_dim), dtype=kv.dtype, device=q.device)
+        out = torch.empty(shape, dtype=dtype, device=q.device)
     if workspace is None:
         workspace = kv.workspace(step, heads)
-    qh, oh = (_heads(t, "attend", n, heads, c.head_dim, kv.dtype) for t in (q, out))
-    ee.check(kv.lib.ee_paged_attention(kv.h, layer, C.byref(step.c), C.byref(qh), C.byref(oh), heads,
-                                       c.head_dim ** -0.5 if scale is None else scale, window, _ptr(workspace), workspace.numel(), _stream()))
+    ee.check(kv.lib.ee_paged_attention(kv.h, layer, step.ref, _heads(q, "attend", shape, dtype), _heads(out, "attend", shape, dtype), heads,
+                                       kv.head_dim ** -0.5 if scale is None else scale, window, workspace.data_ptr(), workspace.numel(),
+                                       _stream()))
     return out
