@@ -62,6 +62,136 @@ __device__ __forceinline__ float quad_sum(float v) {
 // what a maximum of -inf (nothing seen yet, or only scores of -inf) is replaced by in exponents
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
 
+// Positions lo .. hi of the group at pg as bits (bit r: position pg + r); of these the eight a lane holds (bit e: 16 (e / 4) + 4 gq +
+// e % 4); one of them as a mask.
+__device__ __forceinline__ uint32_t seen_of_group(int lo, int hi, int pg) {
+    const int a = max(lo - pg, 0), e = min(hi - pg, 31);
+    return a > e ? 0u : (0xffffffffu >> (31 - e)) & (0xffffffffu << a);
+}
+__device__ __forceinline__ uint32_t seen_by_lane(uint32_t group) {
+    const uint32_t g = group >> (4 * ((threadIdx.x & 63) >> 4));
+    return (g & 15u) | ((g >> 12) & 0xf0u);
+}
+__device__ __forceinline__ uint32_t bit_mask(uint32_t bits, int i) { return (uint32_t)((int)(bits << (31 - i)) >> 31); }
+// The softmax of CB blocks of 16 columns: lane (n16, gq) of a wave holds column n16 of a block and, of a group of 32 positions, the
+// positions 16 b + 4 gq + r.  NO sums of four features a lane and block, which the kernel's second product adds to.
+template <int NO, int CB> struct ColumnState {
+    int   hi[CB];                  // the last position the lane's column sees (-1: none); the first is lowest_seen(hi, window)
+    float neg[CB], lim[CB], l[CB]; // minus the exponents' reference (log2 units); how far above it a score may lie (see softmax); the
+                                   // lane's part of the sum
+    uint32_t seen;                 // bit j: the column of block j has seen a position
+    floatx4 O[CB][NO];
+
+    // columns c0 .. of the n_cols of the rows at positions first + c / G
+    __device__ __forceinline__ void begin(const AttnArgs& a, int c0, int n_cols, int first) {
+        seen = 0;
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+            const int c = c0 + 16 * j + (threadIdx.x & 15);
+            hi[j] = c < n_cols ? first + c / a.G : -1;
+            neg[j] = 0.f;
+            lim[j] = -INFINITY;
+            l[j] = 0.f;
+#pragma unroll
+            for (int o = 0; o < NO; ++o) O[j][o] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+
+    __device__ __forceinline__ float maximum(int j) const { return lim[j] == -INFINITY ? -INFINITY : -neg[j]; }
+
+    // Scores S[j][b][r] of positions pg + 16 b + 4 gq + r -> probabilities P[j][4 b + r]; EDGE: some column does not see all.
+    // A column's reference is its largest score when it was last moved: it moves when a score exceeds it by more than lim = 8, or,
+    // while nothing but -inf has been seen (lim = -inf), when any does.  A lane looks at its own eight scores only; the four lanes
+    // of a column meet when one of the wave's references has to move.
+    template <bool EDGE> __device__ __forceinline__ void softmax(const floatx4 (&S)[CB][2], float (&P)[CB][8], float scale2, int pg, int window) {
+        float x[CB][8], top[CB];
+        uint32_t mine[CB];
+        bool raise = false;
+        auto exponents = [&](int j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[j][i] = fmaf(S[j][i >> 2][i & 3], scale2, neg[j]);
+            if constexpr (EDGE) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t keep = bit_mask(mine[j], i);
+                    x[j][i] = __uint_as_float((__float_as_uint(x[j][i]) & keep) | (0xff800000u & ~keep));
+                }
+            }
+        };
+        if constexpr (EDGE) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j) {
+                const uint32_t all = seen_of_group(lowest_seen(hi[j], window), hi[j], pg);
+                mine[j] = seen_by_lane(all);
+                seen |= all ? 1u << j : 0u;
+            }
+        } else {
+            seen = ~0u;
+        }
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+            exponents(j);
+            top[j] = fmaxf(fmaxf(fmaxf(x[j][0], x[j][1]), fmaxf(x[j][2], x[j][3])), fmaxf(fmaxf(x[j][4], x[j][5]), fmaxf(x[j][6], x[j][7])));
+            raise = raise || top[j] > lim[j];
+        }
+        if (__any(raise)) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j) {
+                const float t = quad_max(top[j]);
+                const bool up = t > lim[j];
+                const float to = up ? neg[j] - t : neg[j];
+                float alpha = __builtin_amdgcn_exp2f(to - neg[j]);
+                if (lim[j] == -INFINITY) alpha = 0.f;        // there is nothing yet
+                if (!up) alpha = 1.f;
+                neg[j] = to;
+                lim[j] = up ? 8.0f : lim[j];
+                l[j] *= alpha;
+#pragma unroll
+                for (int hb = 0; hb < NO; ++hb) O[j][hb] = O[j][hb] * alpha;
+                exponents(j);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+            float (&e)[8] = P[j];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(x[j][i]);
+            l[j] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+        }
+    }
+};
+
+// Four features of a result, and where a column's result lies
+__device__ __forceinline__ void store_o4(bf16_t* p, bool wide, float a, float b, float c, float d) {
+    const uint2 v = make_uint2(bf16_pair(a, b), bf16_pair(c, d));
+    if (wide) {
+        *reinterpret_cast<uint2*>(p) = v;
+    } else {
+        p[0] = (bf16_t)v.x; p[1] = (bf16_t)(v.x >> 16); p[2] = (bf16_t)v.y; p[3] = (bf16_t)(v.y >> 16);
+    }
+}
+__device__ __forceinline__ void store_o4(float* p, bool wide, float a, float b, float c, float d) {
+    if (wide) *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+    else { p[0] = a; p[1] = b; p[2] = c; p[3] = d; }
+}
+template <class T> __device__ __forceinline__ bool wide_o(const HeadsView& h) {
+    return (uintptr_t)h.p % (4 * sizeof(T)) == 0 && h.ts % 4 == 0 && h.hs % 4 == 0;
+}
+template <class T> __device__ __forceinline__ T* out_row(const AttnArgs& a, int g, int c, int row0) {
+    const int t = c / a.G;
+    return (T*)a.out.p + (int64_t)(row0 + t) * a.out.ts + (int64_t)(g * a.G + c - t * a.G) * a.out.hs;
+}
+// sums of four features to the result (one share) or to the shares' buffer
+template <class T> struct ColumnOut {
+    T*     row;                    // of the result, or null
+    float* part;
+    bool   wide;
+    __device__ __forceinline__ void put(int f, floatx4 o) const {
+        if (row) store_o4(row + f, wide, o[0], o[1], o[2], o[3]);
+        else *reinterpret_cast<floatx4*>(part + f) = o;
+    }
+};
+
 // Tiles of C columns: sequence s has the slots from floor(q_start[s] G / C) + s on (see seq_of_slot).  By all lanes of a wave.
 struct Tile { int s, tile; };
 __device__ __forceinline__ Tile tile_of_slot(const StepView& st, int G, int C, int slot) {
@@ -78,5 +208,14 @@ __device__ __forceinline__ Tile tile_of_slot(const StepView& st, int G, int C, i
     return Tile{lo, slot - to_scalar(base(lo))};
 }
 
-int f32_paged_attention(const PagedView& pv, const StepView& st, const HeadsView& q, const HeadsView& out, int n_q_heads, float scale,
-                        int window, hipStream_t s);
+// Host side.  blocks workgroups before any split, of `groups` groups of 32 positions at most; the split's workgroups are fewer than
+// target + blocks, and none of them is split where there are target already.
+struct Split { int share = 1, shares = 1; };
+Split split_groups(int64_t blocks, int groups, int target, int least);
+// groups of 32 positions that `rows` neighbouring rows see together at most
+int groups_seen(const StepView& st, int64_t rows, int window);
+static inline size_t share_bytes(int hd) { return (size_t)hd * sizeof(float) + sizeof(float2); }      // of a column
+
+size_t f32_paged_workspace(int hd, int64_t most_cols, int groups);
+int f32_paged_attention(AttnArgs a, char* ws, hipStream_t s);
+int launch_join(int dtype, const AttnArgs& a, int C, int64_t slots, hipStream_t s);

@@ -32,28 +32,9 @@ __device__ __forceinline__ uint4 load_q8(const bf16_t* p, bool wide, uint32_t ke
     }
     return make_uint4((v.x & keep) ^ flip, (v.y & keep) ^ flip, (v.z & keep) ^ flip, (v.w & keep) ^ flip);
 }
-__device__ __forceinline__ void store_o4(bf16_t* p, bool wide, float a, float b, float c, float d) {
-    const uint2 v = make_uint2(bf16_pair(a, b), bf16_pair(c, d));
-    if (wide) {
-        *reinterpret_cast<uint2*>(p) = v;
-    } else {
-        p[0] = (bf16_t)v.x; p[1] = (bf16_t)(v.x >> 16); p[2] = (bf16_t)v.y; p[3] = (bf16_t)(v.y >> 16);
-    }
-}
 __device__ __forceinline__ bool wide_q(const HeadsView& h) { return (uintptr_t)h.p % 16 == 0 && h.ts % 8 == 0 && h.hs % 8 == 0; }
-__device__ __forceinline__ bool wide_o(const HeadsView& h) { return (uintptr_t)h.p % 8 == 0 && h.ts % 4 == 0 && h.hs % 4 == 0; }
 
-// Positions lo .. hi of the group at pg as bits (bit r: position pg + r); of these the eight a lane holds (bit e: 16 (e / 4) + 4 gq +
-// e % 4); one of them as a mask; and all eight as masks of the halves of an operand's four words.
-__device__ __forceinline__ uint32_t seen_of_group(int lo, int hi, int pg) {
-    const int a = max(lo - pg, 0), e = min(hi - pg, 31);
-    return a > e ? 0u : (0xffffffffu >> (31 - e)) & (0xffffffffu << a);
-}
-__device__ __forceinline__ uint32_t seen_by_lane(uint32_t group) {
-    const uint32_t g = group >> (4 * ((threadIdx.x & 63) >> 4));
-    return (g & 15u) | ((g >> 12) & 0xf0u);
-}
-__device__ __forceinline__ uint32_t bit_mask(uint32_t bits, int i) { return (uint32_t)((int)(bits << (31 - i)) >> 31); }
+// the lane's eight positions as masks of the halves of an operand's four words
 __device__ __forceinline__ void seen_words(uint32_t (&w)[4], int lo, int hi, int pg) {
     const uint32_t mine = seen_by_lane(seen_of_group(lo, hi, pg));
 #pragma unroll
@@ -65,98 +46,33 @@ __device__ __forceinline__ uint32_t half_mask(uint32_t bits) { bits >>= 15; retu
 
 // ------------------------------------------------------------------ the columns of a wave
 // CB blocks of 16 columns of a (sequence, kv head), and what the softmax and the second product keep for them
-template <int NK, int CB> struct Columns {
-    int   lo[CB], hi[CB];          // positions the lane's column sees; hi < lo: none
-    float neg[CB], lim[CB], l[CB]; // minus the exponents' reference (log2 units); how far above it a score may lie (see softmax); the
-                                   // lane's part of the sum
-    uint32_t seen;                 // bit j: the column of block j has seen a position
-    floatx4 O[CB][2 * NK];         // [hb][r]: feature 16 hb + 4 gq + r
+template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[j][hb][r]: feature 16 hb + 4 gq + r
+    using State = ColumnState<2 * NK, CB>;
+    using State::hi; using State::O;
     uint4 q[CB][NK];
 
-    // columns c0 .. of the n_cols of rows at positions first + c / G, token rows row0 + c / G
+    // columns c0 .. of the n_cols of a sequence whose first row is row0, at position first
     __device__ __forceinline__ void start(const AttnArgs& a, int g, int c0, int n_cols, int first, int row0) {
         const int lane = threadIdx.x & 63, n16 = lane & 15, gq = lane >> 4;
         const bool wide = wide_q(a.q);
-        seen = 0;
+        State::begin(a, c0, n_cols, first);
 #pragma unroll
         for (int j = 0; j < CB; ++j) {
             const int c = c0 + 16 * j + n16, t = c / a.G;
             const bool live = c < n_cols;
-            hi[j] = live ? first + t : -1;
-            lo[j] = lowest_seen(hi[j], a.window);
-            neg[j] = 0.f;
-            lim[j] = -INFINITY;
-            l[j] = 0.f;
-#pragma unroll
-            for (int hb = 0; hb < 2 * NK; ++hb) O[j][hb] = floatx4{0.f, 0.f, 0.f, 0.f};
             const bf16_t* p = (const bf16_t*)a.q.p + (int64_t)(row0 + t) * a.q.ts + (int64_t)(g * a.G + c - t * a.G) * a.q.hs + 8 * gq;
 #pragma unroll
             for (int k = 0; k < NK; ++k) q[j][k] = live ? load_q8(p + 32 * k, wide, a.keep, a.flip) : make_uint4(0, 0, 0, 0);
         }
     }
 
-    __device__ __forceinline__ float maximum(int j) const { return lim[j] == -INFINITY ? -INFINITY : -neg[j]; }
-
-    // Scores S[j][b][r] of positions pg + 16 b + 4 gq + r -> probabilities as right operands; EDGE: some column does not see all.
-    // A column's reference is its largest score when it was last moved: it moves when a score exceeds it by more than lim = 8, or,
-    // while nothing but -inf has been seen (lim = -inf), when any does.  A lane looks at its own eight scores only; the four lanes
-    // of a column meet when one of the wave's references has to move.
-    template <bool EDGE> __device__ __forceinline__ void softmax(const floatx4 (&S)[CB][2], uint4 (&P)[CB], float scale2, int pg) {
-        float x[CB][8], top[CB];
-        uint32_t mine[CB];
-        bool raise = false;
-        auto exponents = [&](int j) {
+    // the probabilities of a group as right operands
+    template <bool EDGE> __device__ __forceinline__ void weights(const floatx4 (&S)[CB][2], uint4 (&P)[CB], float scale2, int pg, int window) {
+        float e[CB][8];
+        State::template softmax<EDGE>(S, e, scale2, pg, window);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[j][i] = fmaf(S[j][i >> 2][i & 3], scale2, neg[j]);
-            if constexpr (EDGE) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t keep = bit_mask(mine[j], i);
-                    x[j][i] = __uint_as_float((__float_as_uint(x[j][i]) & keep) | (0xff800000u & ~keep));
-                }
-            }
-        };
-        if constexpr (EDGE) {
-#pragma unroll
-            for (int j = 0; j < CB; ++j) {
-                const uint32_t all = seen_of_group(lo[j], hi[j], pg);
-                mine[j] = seen_by_lane(all);
-                seen |= all ? 1u << j : 0u;
-            }
-        } else {
-            seen = ~0u;
-        }
-#pragma unroll
-        for (int j = 0; j < CB; ++j) {
-            exponents(j);
-            top[j] = fmaxf(fmaxf(fmaxf(x[j][0], x[j][1]), fmaxf(x[j][2], x[j][3])), fmaxf(fmaxf(x[j][4], x[j][5]), fmaxf(x[j][6], x[j][7])));
-            raise = raise || top[j] > lim[j];
-        }
-        if (__any(raise)) {
-#pragma unroll
-            for (int j = 0; j < CB; ++j) {
-                const float t = quad_max(top[j]);
-                const bool up = t > lim[j];
-                const float to = up ? neg[j] - t : neg[j];
-                float alpha = __builtin_amdgcn_exp2f(to - neg[j]);
-                if (lim[j] == -INFINITY) alpha = 0.f;        // there is nothing yet
-                if (!up) alpha = 1.f;
-                neg[j] = to;
-                lim[j] = up ? 8.0f : lim[j];
-                l[j] *= alpha;
-#pragma unroll
-                for (int hb = 0; hb < 2 * NK; ++hb) O[j][hb] = O[j][hb] * alpha;
-                exponents(j);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < CB; ++j) {
-            float e[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(x[j][i]);
-            l[j] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-            P[j] = make_uint4(bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7]));
-        }
+        for (int j = 0; j < CB; ++j)
+            P[j] = make_uint4(bf16_pair(e[j][0], e[j][1]), bf16_pair(e[j][2], e[j][3]), bf16_pair(e[j][4], e[j][5]), bf16_pair(e[j][6], e[j][7]));
     }
 
     // S^T = K Q^T of a group: kf[b NK + k] holds features 32 k .. of the 16 positions of half b
@@ -174,9 +90,9 @@ template <int NK, int CB> struct Columns {
 
     // second product of a group at pg with the values vf
     template <bool EDGE>
-    __device__ __forceinline__ void weigh_group(const uint4 (&vf)[2 * NK], const uint4 (&P)[CB], int pg, int min_lo, int max_hi) {
+    __device__ __forceinline__ void weigh_group(const uint4 (&vf)[2 * NK], const uint4 (&P)[CB], int pg, int min_lo, int max_hi, int window) {
         if constexpr (EDGE) {
-            weigh_edge(vf, P, pg, min_lo, max_hi);
+            weigh_edge(vf, P, pg, min_lo, max_hi, window);
         } else {
 #pragma unroll
             for (int hb = 0; hb < 2 * NK; ++hb) weigh(hb, vf[hb], P);
@@ -194,7 +110,7 @@ template <int NK, int CB> struct Columns {
     // infinities of either sign met with a positive probability, NaN and everything non-finite met with a zero one.
     // What lies outside min_lo .. max_hi no column sees; it may be memory nobody has written, and counts as zero.
     // Words hold two bf16; the tests work on both halves without a carry between.
-    __device__ __forceinline__ void weigh_edge(const uint4 (&vf)[2 * NK], const uint4 (&P)[CB], int pg, int min_lo, int max_hi) {
+    __device__ __forceinline__ void weigh_edge(const uint4 (&vf)[2 * NK], const uint4 (&P)[CB], int pg, int min_lo, int max_hi, int window) {
         uint32_t in[4], any = 0;
         seen_words(in, min_lo, max_hi, pg);
         auto inside = [&](uint4 v) { return make_uint4(v.x & in[0], v.y & in[1], v.z & in[2], v.w & in[3]); };
@@ -203,13 +119,14 @@ template <int NK, int CB> struct Columns {
             const uint4 v = inside(vf[hb]);
             any |= odd_bits(v.x) | odd_bits(v.y) | odd_bits(v.z) | odd_bits(v.w);
         }
-        if (!__any(any != 0)) {
+        if (__builtin_expect(!__any(any != 0), 1)) {
 #pragma unroll
             for (int hb = 0; hb < 2 * NK; ++hb) weigh(hb, inside(vf[hb]), P);
             return;
         }
 #pragma unroll
         for (int hb = 0; hb < 2 * NK; ++hb) {
+            __builtin_amdgcn_sched_barrier(0);               // rare: one block at a time, few registers
             const uint4 v = inside(vf[hb]);
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
             uint32_t fin[4], pos[4], neg[4], nan[4];
@@ -231,7 +148,7 @@ template <int NK, int CB> struct Columns {
             for (int j = 0; j < CB; ++j) {
                 const uint32_t pw[4] = {P[j].x, P[j].y, P[j].z, P[j].w};
                 uint32_t sees[4], some[4], none[4];          // 1 where the column sees a position with P > 0, with P = 0
-                seen_words(sees, lo[j], hi[j], pg);
+                seen_words(sees, lowest_seen(hi[j], window), hi[j], pg);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t positive = half_mask(((pw[i] & 0x7fff7fffu) + 0x7fff7fffu) & 0x80008000u);
@@ -250,21 +167,6 @@ template <int NK, int CB> struct Columns {
         }
     }
 };
-
-// sums of four features to the result (one share) or to the shares' buffer
-struct ColumnOut {
-    bf16_t* row;                   // of the result, or null
-    float*  part;
-    bool    wide;
-    __device__ __forceinline__ void put(int f, floatx4 o) const {
-        if (row) store_o4(row + f, wide, o[0], o[1], o[2], o[3]);
-        else *reinterpret_cast<floatx4*>(part + f) = o;
-    }
-};
-__device__ __forceinline__ bf16_t* out_row(const AttnArgs& a, int g, int c, int row0) {
-    const int t = c / a.G;
-    return (bf16_t*)a.out.p + (int64_t)(row0 + t) * a.out.ts + (int64_t)(g * a.G + c - t * a.G) * a.out.hs;
-}
 
 // ------------------------------------------------------------------ sequences of few columns
 // One workgroup per (sequence, kv head, share of the positions); its four waves take the share's groups in turn, straight from
@@ -317,8 +219,8 @@ k_bf16_paged_rows(AttnArgs a) {
 #pragma unroll
             for (int f = EARLY; f < 2 * NK; ++f) vf[f] = kv[(2 * NK + f) * 64];
             uint4 P[CB];
-            col.template softmax<edge.value>(S, P, a.scale2, pg);
-            col.template weigh_group<edge.value>(vf, P, pg, min_lo, sr.len - 1);
+            col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
+            col.template weigh_group<edge.value>(vf, P, pg, min_lo, sr.len - 1, a.window);
         }
     };
 #pragma unroll 1
@@ -356,7 +258,7 @@ k_bf16_paged_rows(AttnArgs a) {
         if (c >= n_cols) continue;
         const int64_t slot = ((int64_t)blockIdx.x * a.shares + blockIdx.y) * a.rows_cols + c;
         const bool last = n_shares == 1;
-        const ColumnOut dst{last ? out_row(a, g, c, sr.row0) : nullptr, last ? nullptr : a.part + slot * HD, wide_o(a.out)};
+        const ColumnOut<bf16_t> dst{last ? out_row<bf16_t>(a, g, c, sr.row0) : nullptr, last ? nullptr : a.part + slot * HD, wide_o<bf16_t>(a.out)};
         if (!last && w == 0 && lane < 16) a.stat[slot] = make_float2(m, seen ? l : -1.f);
         const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
         for (int hb = w; hb < 2 * NK; hb += 4) {
@@ -461,7 +363,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
 #pragma unroll
                 for (int f = 0; f < 2 * NK; ++f) vf[f] = group(i)[(2 * NK + f) * 64];
                 __builtin_amdgcn_sched_barrier(0);
-                col.template softmax<edge.value>(S, P, a.scale2, pg);
+                col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
             }
             if (i + 1 < n) {
                 if ((i + 1) % SG == 0) {                     // the stage is in registers: its buffer is free
@@ -472,7 +374,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
                 load_keys(i + 1);                            // the next keys during the second product
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (works) col.template weigh_group<edge.value>(vf, P, pg, min_lo, w_last);
+            if (works) col.template weigh_group<edge.value>(vf, P, pg, min_lo, w_last, a.window);
         }
     };
 #pragma unroll 1
@@ -481,7 +383,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
         if (part == 0) run(std::false_type{}, a0, a1);
     }
 
-    const bool last = n_shares == 1, wide = wide_o(a.out);
+    const bool last = n_shares == 1, wide = wide_o<bf16_t>(a.out);
     const int64_t block = ((int64_t)(slot * (int64_t)a.pv.n_kv_heads + g) * a.shares + blockIdx.y) * C;
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
@@ -490,7 +392,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
         const bool seen = (col.seen >> j) & 1u;
         if (c >= n_cols) continue;
         const int64_t at = block + c - c0;
-        const ColumnOut dst{last ? out_row(a, g, c, sr.row0) : nullptr, last ? nullptr : a.part + at * HD, wide};
+        const ColumnOut<bf16_t> dst{last ? out_row<bf16_t>(a, g, c, sr.row0) : nullptr, last ? nullptr : a.part + at * HD, wide};
         if (!last && lane < 16) a.stat[at] = make_float2(col.maximum(j), seen ? l : -1.f);
         const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
 #pragma unroll
@@ -501,8 +403,9 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
 // ------------------------------------------------------------------ join of the shares
 // A wave per column: the shares' maxima and sums, then their weighted sums, in share order (the same bits every time).
 // C = 0: sequences of few columns, blockIdx.x = (sequence, kv head); else tiles of C columns, blockIdx.x = (slot, kv head).
+template <class T>
 __global__ void __launch_bounds__(256)
-k_bf16_paged_join(AttnArgs a, int C, int n_slots) {
+k_paged_join(AttnArgs a, int C, int n_slots) {
     const int x = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - x * a.pv.n_kv_heads;
     const int slot = C > 0 ? n_slots - 1 - x : x;
     Tile tl{x, 0};
@@ -539,7 +442,7 @@ k_bf16_paged_join(AttnArgs a, int C, int n_slots) {
     }
     if (f >= hd) return;
     const float inv = seen ? 1.0f / l : 0.f;
-    store_o4(out_row(a, g, c, sr.row0) + f, wide_o(a.out), o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    store_o4(out_row<T>(a, g, c, sr.row0) + f, wide_o<T>(a.out), o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 }
 
 // ------------------------------------------------------------------ host side
@@ -548,13 +451,20 @@ namespace {
 constexpr int ROWS_TARGET = 1024, ROWS_LEAST = 8;            // workgroups wanted; groups of 32 positions a share has at least
 constexpr int TILE_TARGET = 512, TILE_LEAST = 16;
 
-struct Split { int share = 1, shares = 1; };
-Split split(int64_t blocks, int groups, int target, int least) {
+}  // namespace
+
+Split split_groups(int64_t blocks, int groups, int target, int least) {
     const int64_t want = std::max<int64_t>(1, (target + blocks - 1) / blocks);
     const int share = (int)std::max<int64_t>(least, (groups + want - 1) / want);
     return Split{share, std::max(1, (groups + share - 1) / share)};
 }
 
+int groups_seen(const StepView& st, int64_t rows, int window) {
+    const int all = (st.max_kv_len + 31) / 32;
+    return window > 0 ? (int)std::min<int64_t>(all, (std::min<int64_t>(window, st.max_kv_len) + rows + 29) / 32 + 1) : all;
+}
+
+namespace {
 int rows_limit(int hd) { return hd <= 128 ? 32 : 16; }       // columns that k_bf16_paged_rows holds
 constexpr int TILE_MOST = 128;                               // columns of the widest tile
 
@@ -564,11 +474,6 @@ struct Plan {
     int64_t rows_blocks = 0, n_slots = 0;
     Split r, t;
 };
-// groups of 32 positions that `rows` neighbouring rows see together at most
-int groups_seen(const StepView& st, int64_t rows, int window) {
-    const int all = (st.max_kv_len + 31) / 32;
-    return window > 0 ? (int)std::min<int64_t>(all, (std::min<int64_t>(window, st.max_kv_len) + rows + 29) / 32 + 1) : all;
-}
 Plan make_plan(int hd, int Hkv, int G, const StepView& st, int window) {
     Plan p;
     const int64_t most = (int64_t)st.max_q_len * G;
@@ -584,28 +489,35 @@ Plan make_plan(int hd, int Hkv, int G, const StepView& st, int window) {
         p.tile_cb = most <= 64 ? 1 : 2;
         const int C = 64 * p.tile_cb;
         p.n_slots = (int64_t)st.n_tokens * G / C + st.n_seqs;
-        p.t = split(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window), TILE_TARGET, TILE_LEAST);
+        p.t = split_groups(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window), TILE_TARGET, TILE_LEAST);
     }
     while (16 * p.rows_cb < p.rows_cols) p.rows_cb *= 2;
     p.rows_cols = std::min(p.rows_cols, 16 * p.rows_cb);
     if (p.rows) {
         p.rows_blocks = (int64_t)st.n_seqs * Hkv;
-        p.r = split(p.rows_blocks, groups_seen(st, (p.rows_cols + G - 1) / G, window), ROWS_TARGET, ROWS_LEAST);
+        p.r = split_groups(p.rows_blocks, groups_seen(st, (p.rows_cols + G - 1) / G, window), ROWS_TARGET, ROWS_LEAST);
     }
     return p;
 }
-size_t share_bytes(int hd) { return (size_t)hd * sizeof(float) + sizeof(float2); }     // of a column
 }  // namespace
 
-// split() makes at most target + blocks workgroups of fewer than target blocks, whatever the other figures are
+// Split workgroups are fewer than target + blocks of fewer than target blocks, whatever the other figures are.
 size_t paged_attention_workspace(int dtype, int hd, int Hkv, int n_q_heads, const StepView& st) {
-    if (dtype != EE_BF16) return 0;
     const int64_t most = (int64_t)st.max_q_len * (n_q_heads / Hkv);
     const int groups = (st.max_kv_len + 31) / 32, limit = rows_limit(hd);
+    if (dtype != EE_BF16) return f32_paged_workspace(hd, most, groups);
     size_t n = 0;
     if (groups > ROWS_LEAST) n += (size_t)2 * ROWS_TARGET * std::min<int64_t>(limit, (most + 15) / 16 * 16) * share_bytes(hd);
     if (groups > TILE_LEAST && most > limit) n += (size_t)2 * TILE_TARGET * TILE_MOST * share_bytes(hd);
     return n;
+}
+
+int launch_join(int dtype, const AttnArgs& a, int C, int64_t slots, hipStream_t s) {
+    const int64_t blocks = (C > 0 ? slots : a.st.n_seqs) * a.pv.n_kv_heads;
+    const dim3 grid((unsigned)blocks, ((C > 0 ? C : a.rows_cols) + 3) / 4);
+    hipLaunchKernelGGL(dtype == EE_BF16 ? k_paged_join<bf16_t> : k_paged_join<float>, grid, dim3(256), 0, s, a, C, (int)slots);
+    EE_LAUNCH_CHECK();
+    return EE_OK;
 }
 
 template <int NK>
@@ -625,8 +537,8 @@ static int run_bf16(const Plan& p, AttnArgs a, char* ws, hipStream_t s) {
         hipLaunchKernelGGL(kern, dim3((unsigned)(p.n_slots * Hkv), a.shares), dim3(256), 0, s, a, (int)p.n_slots);
         EE_LAUNCH_CHECK();
         if (a.shares > 1) {
-            hipLaunchKernelGGL(k_bf16_paged_join, dim3((unsigned)(p.n_slots * Hkv), C / 4), dim3(256), 0, s, a, C, (int)p.n_slots);
-            EE_LAUNCH_CHECK();
+            const int rc = launch_join(EE_BF16, a, C, p.n_slots, s);
+            if (rc != EE_OK) return rc;
         }
     }
     if (p.rows) {
@@ -636,17 +548,13 @@ static int run_bf16(const Plan& p, AttnArgs a, char* ws, hipStream_t s) {
         if (p.rows_cb == 1) hipLaunchKernelGGL((k_bf16_paged_rows<NK, 1>), grid, dim3(256), 0, s, a);
         else if constexpr (NK <= 4) hipLaunchKernelGGL((k_bf16_paged_rows<NK, 2>), grid, dim3(256), 0, s, a);
         EE_LAUNCH_CHECK();
-        if (a.shares > 1) {
-            hipLaunchKernelGGL(k_bf16_paged_join, dim3((unsigned)p.rows_blocks, (a.rows_cols + 3) / 4), dim3(256), 0, s, a, 0, 0);
-            EE_LAUNCH_CHECK();
-        }
+        if (a.shares > 1) return launch_join(EE_BF16, a, 0, 0, s);
     }
     return EE_OK;
 }
 
 int launch_paged_attention(int dtype, const PagedView& pv, const StepView& st, const HeadsView& q, const HeadsView& out, int n_q_heads,
                            float scale, int window, char* ws, hipStream_t s) {
-    if (dtype != EE_BF16) return f32_paged_attention(pv, st, q, out, n_q_heads, scale, window, s);
     AttnArgs a{};
     a.pv = pv; a.st = st; a.q = q; a.out = out;
     a.G = n_q_heads / pv.n_kv_heads;
@@ -654,6 +562,7 @@ int launch_paged_attention(int dtype, const PagedView& pv, const StepView& st, c
     a.flip = scale < 0.f ? 0x80008000u : 0u;
     a.keep = scale == 0.f ? 0u : 0xffffffffu;
     a.window = window;
+    if (dtype != EE_BF16) return f32_paged_attention(a, ws, s);
     const Plan p = make_plan(pv.hd, pv.n_kv_heads, a.G, st, window);
     switch (pv.hd) {
         case 64: return run_bf16<2>(p, a, ws, s);

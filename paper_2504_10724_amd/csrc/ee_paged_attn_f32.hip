@@ -1,67 +1,265 @@
 // ee_paged_attn_f32.hip -- attention of new rows over the paged cache, fp32.
+//
+// The same scheme on 16x16x4 fp32 MFMAs: S^T = K Q^T, O^T = V^T P^T, nothing rounded below fp32.  Four products of depth 4 take 16
+// features (or 16 positions) in any order, as long as both operands use the same one, so a lane loads 16 bytes of a key (features
+// 16 c + 4 gq ..) and of a value (features 64 c + 4 n16 ..) and feeds their four elements to four products.  What bounds it: the MFMAs
+// of a chunk, at 157 TFLOP/s a fifteenth of bf16's rate; the cache's bytes for single tokens.
 #include "ee_paged_attn.h"
 
-// One wave per (row, query head): 64 positions at a time, a lane each for the scores, then the lanes share out the features.
-template <class T>
-__global__ void __launch_bounds__(256)
-k_paged_attn(PagedView pv, StepView st, HeadsView q, HeadsView out, int Hq, float scale, int window) {
-    __shared__ float qs[4][256];
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, hd = pv.hd, ps = pv.page_size;
-    const int64_t id = (int64_t)blockIdx.x * 4 + w;
-    const int t = (int)(id / Hq), h = (int)(id % Hq);
-    if (t >= st.n_tokens) return;
-    const int s = seq_of_slot(st, t, 1, 0);
-    const SeqRows sr = seq_rows(st, s);
-    if (t < sr.row0 || t >= sr.row0 + sr.n) return;
-    const int p = sr.len - sr.n + t - sr.row0;
-    const T* qr = (const T*)q.p + t * q.ts + h * q.hs;
-    for (int i = lane; i < hd; i += 64) qs[w][i] = to_f32(qr[i]) * scale;
-    __builtin_amdgcn_wave_barrier();
-    const int lo = window > 0 ? max(0, p - window + 1) : 0, g = h / (Hq / pv.n_kv_heads);
-    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    bool seen = false;
-    for (int c = lo; c <= p; c += 64) {
-        const int j = c + lane;
-        const T* blk = nullptr;
-        if (j <= p) {
-            const int page = st.pages[(int64_t)s * st.pages_per_seq + j / ps];
-            if (page >= 0 && page < pv.n_pages) blk = (const T*)pv.pool + ((int64_t)page * pv.n_kv_heads + g) * (2LL * ps * hd);
-            else if (st.status) atomicOr(st.status, 1);
-        }
-        float x = -INFINITY;
-        if (blk) {
-            x = 0.f;
-            for (int i = 0; i < hd; ++i) x = fmaf(qs[w][i], to_f32(blk[page_k<T>(j % ps, i, hd, ps)]), x);
-        }
-        seen = seen || __any(blk != nullptr);
-        float mx = x;
-        for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
-        mx = fmaxf(mx, m);
-        const float ref = mx == -INFINITY ? 0.f : mx, a = expf(m - ref);
-        const float e = blk ? expf(x - ref) : 0.f;
-        float sum = e;
-        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-        l = l * a + sum;
-        m = mx;
-        for (int k = 0; k < 4; ++k) o[k] *= a;
-        for (int jj = 0; jj < 64; ++jj) {
-            const uint64_t b = (uint64_t)blk;
-            const uint64_t at = ((uint64_t)(uint32_t)__shfl((int)(b >> 32), jj, 64) << 32) | (uint32_t)__shfl((int)b, jj, 64);
-            if (at == 0) continue;
-            const float ej = __shfl(e, jj, 64);
-            for (int k = 0; k < 4; ++k)
-                if (lane + 64 * k < hd) o[k] = fmaf(ej, to_f32(((const T*)at)[page_v<T>((c + jj) % ps, lane + 64 * k, hd, ps)]), o[k]);
-        }
-    }
-    T* dst = (T*)out.p + t * out.ts + h * out.hs;
-    for (int k = 0; k < 4; ++k)
-        if (lane + 64 * k < hd) dst[lane + 64 * k] = from_f32<T>(seen ? o[k] / l : 0.f);
+#include <algorithm>
+#include <type_traits>
+
+__device__ __forceinline__ floatx4 mfma(float a, float b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ float4 load4(const float* p, bool wide) {
+    return wide ? *reinterpret_cast<const float4*>(p) : make_float4(p[0], p[1], p[2], p[3]);
 }
 
-int f32_paged_attention(const PagedView& pv, const StepView& st, const HeadsView& q, const HeadsView& out, int n_q_heads, float scale,
-                        int window, hipStream_t s) {
-    const int64_t waves = (int64_t)st.n_tokens * n_q_heads;
-    hipLaunchKernelGGL(k_paged_attn<float>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, pv, st, q, out, n_q_heads, scale, window);
+// features f .. f + 3 of a cached row, zeros beyond its hd (a load and selects, no branch)
+__device__ __forceinline__ floatx4 features(const float* row, int f, int hd) {
+    const bool in = f < hd;
+    floatx4 x = *reinterpret_cast<const floatx4*>(row + (in ? f : 0));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = in ? x[e] : 0.f;
+    return x;
+}
+
+// O[j][4 c + e][r]: feature 64 c + 16 gq + 4 r + e
+template <int HD, int CB> struct ColumnsF32 : ColumnState<HD / 16, CB> {
+    using State = ColumnState<HD / 16, CB>;
+    using State::hi; using State::O;
+
+    // values v[4 b + r][c] (of positions 16 b + 4 gq + r), probabilities P[j][4 b + r]
+    __device__ __forceinline__ void weigh(const floatx4 (&v)[8][HD / 64], const float (&P)[CB][8], int hd) {
+#pragma unroll
+        for (int c = 0; c < HD / 64; ++c)
+            if (64 * c < hd)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int j = 0; j < CB; ++j) O[j][4 * c + e] = mfma(v[i][c][e], P[j][i], O[j][4 * c + e]);
+    }
+
+    // As in the bf16 kernels: infinities and NaN at positions that some column does not see leave the operand and are counted for the
+    // columns that see them; what no column sees (outside min_lo .. max_hi) is zero.
+    __device__ __forceinline__ void weigh_edge(floatx4 (&v)[8][HD / 64], const float (&P)[CB][8], int hd, int pg, int min_lo, int max_hi, int window) {
+        const uint32_t in = seen_by_lane(seen_of_group(min_lo, max_hi, pg));
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int c = 0; c < HD / 64; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[i][c][e] = __uint_as_float(__float_as_uint(v[i][c][e]) & bit_mask(in, i));
+                    odd = odd || !(fabsf(v[i][c][e]) < INFINITY);
+                }
+        if (__builtin_expect(!__any(odd), 1)) {
+            weigh(v, P, hd);
+            return;
+        }
+        const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+            const uint32_t sees = seen_by_lane(seen_of_group(lowest_seen(hi[j], window), hi[j], pg));
+#pragma unroll
+            for (int c = 0; c < HD / 64; ++c) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    floatx4 up = zero, down = zero, bad = zero;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float x = v[i][c][e], p = P[j][i];
+                        const bool some = ((sees >> i) & 1u) && !(p == 0.f), none = ((sees >> i) & 1u) && p == 0.f;
+                        const bool nan = x != x, plus = x == INFINITY, minus = x == -INFINITY;
+                        up = mfma(plus ? 1.f : 0.f, some ? 1.f : 0.f, up);
+                        down = mfma(minus ? 1.f : 0.f, some ? 1.f : 0.f, down);
+                        bad = mfma(nan ? 1.f : 0.f, some ? 1.f : 0.f, bad);
+                        bad = mfma(nan || plus || minus ? 1.f : 0.f, none ? 1.f : 0.f, bad);
+                        O[j][4 * c + e] = mfma(nan || plus || minus ? 0.f : x, p, O[j][4 * c + e]);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        O[j][4 * c + e][r] += up[r] > 0.f ? INFINITY : 0.f;
+                        O[j][4 * c + e][r] -= down[r] > 0.f ? INFINITY : 0.f;
+                        O[j][4 * c + e][r] = bad[r] > 0.f ? NAN : O[j][4 * c + e][r];
+                    }
+                }
+            }
+        }
+    }
+};
+
+// One workgroup per (16 CB columns of a sequence, kv head, share of the positions); its waves take the share's groups in turn, from
+// memory into registers, and join their sums through LDS.  one_tile: no sequence has more columns, the slots are the sequences.
+// WHOLE: the heads are HD wide, else less.
+template <int HD, int CB, bool WHOLE>
+__global__ void __launch_bounds__(256, HD <= 128 ? 2 : 1)
+k_f32_paged(AttnArgs a, int n_slots, int one_tile) {
+    constexpr int C = 16 * CB, NC = HD / 64;
+    __shared__ float4 so[4][HD / 16][64];
+    __shared__ float sm[4][C], sl[4][C];
+    const int sx = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - sx * a.pv.n_kv_heads;
+    const int slot = n_slots - 1 - sx;                       // later rows see more positions: they start first
+    Tile tl{slot, 0};
+    if (!one_tile) tl = tile_of_slot(a.st, a.G, C, slot);
+    const SeqRows sr = seq_rows(a.st, tl.s);
+    const int n_cols = sr.n * a.G, c0 = tl.tile * C, hd = WHOLE ? HD : a.pv.hd;
+    if (sr.n == 0 || tl.tile < 0 || c0 >= n_cols) return;
+    const int first = sr.len - sr.n, t0 = c0 / a.G, t1 = (min(c0 + C, n_cols) - 1) / a.G;
+    const int min_lo = lowest_seen(first + t0, a.window), max_hi = first + t1;
+    const GroupRange all = groups_of(min_lo, max_hi);
+    const int n_shares = shares_of(all.n, a.share);
+    if ((int)blockIdx.y >= n_shares) return;
+    const int lane = threadIdx.x & 63, n16 = lane & 15, gq = lane >> 4, w = to_scalar(threadIdx.x >> 6);
+    const int ga = all.g0 + blockIdx.y * a.share, gb = min(ga + a.share, all.g0 + all.n);
+
+    ColumnsF32<HD, CB> col;
+    col.begin(a, c0, n_cols, first);
+    floatx4 q[CB][HD / 16];                                  // features 16 k + 4 gq + e
+    const bool wide = (uintptr_t)a.q.p % 16 == 0 && a.q.ts % 4 == 0 && a.q.hs % 4 == 0;
+#pragma unroll
+    for (int j = 0; j < CB; ++j) {
+        const int c = c0 + 16 * j + n16, t = c / a.G;
+        const float* p = (const float*)a.q.p + (int64_t)(sr.row0 + t) * a.q.ts + (int64_t)(g * a.G + c - t * a.G) * a.q.hs + 4 * gq;
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+            const float4 x = c < n_cols && 16 * k + 4 * gq < hd ? load4(p + 16 * k, wide) : make_float4(0.f, 0.f, 0.f, 0.f);
+            const float y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[j][k][e] = __uint_as_float((__float_as_uint(y[e]) & a.keep) ^ (a.flip & 0x80000000u));
+        }
+    }
+
+    const int ps = a.pv.page_size, per = ps >> 5;
+    const int n_mine = max(0, (gb - ga - w + 3) >> 2);       // this wave's groups: ga + w, ga + w + 4, ..
+    auto mine_from = [&](int grp) { return min(max((grp - ga - w + 3) >> 2, 0), n_mine); };
+    // groups that every column sees whole: from a0 to a1 of the wave's
+    const int a0 = mine_from((lowest_seen(max_hi, a.window) + 31) >> 5), a1 = max(a0, mine_from((first + t0 + 1) >> 5));
+    uint32_t where = 0;
+    auto run = [&](auto edge, int from, int to) {
+        for (int i = from; i < to; ++i) {
+            if ((i & 63) == 0 || i == from) {
+                const int grp = ga + w + 4 * ((i & ~63) + lane);
+                where = grp < gb ? pool_group(a.pv, a.st, tl.s, g, grp) : NO_GROUP;
+            }
+            const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)where, i & 63);
+            if (at == NO_GROUP) continue;
+            // of the block's keys, then its values: the group's offset in both
+            const uint32_t blk = at / (uint32_t)per;
+            const float* kp = (const float*)a.pv.pool + (int64_t)blk * (2 * ps * hd) + (int64_t)(at - blk * per) * (32 * hd);
+            const float* vp = kp + (int64_t)ps * hd;
+            const int pg = (ga + w + 4 * i) << 5;
+            floatx4 S[CB][2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                floatx4 kf[HD / 16];
+#pragma unroll
+                for (int k = 0; k < HD / 16; ++k) kf[k] = features(kp + (16 * b + n16) * hd, 16 * k + 4 * gq, hd);
+#pragma unroll
+                for (int j = 0; j < CB; ++j) S[j][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < HD / 16; ++k)
+                    if (16 * k < hd)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+#pragma unroll
+                            for (int j = 0; j < CB; ++j) S[j][b] = mfma(kf[k][e], q[j][k][e], S[j][b]);
+            }
+            floatx4 v[8][NC];
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+                    v[r][c] = features(vp + (16 * (r >> 2) + 4 * gq + (r & 3)) * hd, 64 * c + 4 * n16, hd);
+            float P[CB][8];
+            col.template softmax<edge.value>(S, P, a.scale2, pg, a.window);
+            if constexpr (edge.value) col.weigh_edge(v, P, hd, pg, min_lo, max_hi, a.window);
+            else col.weigh(v, P, hd);
+        }
+    };
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {
+        run(std::true_type{}, part == 0 ? 0 : a1, part == 0 ? a0 : n_mine);
+        if (part == 0) run(std::false_type{}, a0, a1);
+    }
+
+#pragma unroll
+    for (int j = 0; j < CB; ++j) {
+        const float l = quad_sum(col.l[j]);
+        if (lane < 16) {
+            sm[w][16 * j + n16] = col.maximum(j);
+            sl[w][16 * j + n16] = (col.seen >> j) & 1u ? l : -1.f;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < CB; ++j) {
+        if (c0 + 16 * j >= n_cols) break;
+        __syncthreads();                                     // the statistics are there; the last block's sums have been read
+#pragma unroll
+        for (int o = 0; o < HD / 16; ++o) *reinterpret_cast<floatx4*>(&so[w][o][lane]) = col.O[j][o];
+        __syncthreads();
+        const int cl = 16 * j + n16, c = c0 + cl;
+        float m = -INFINITY, l = 0.f, wt[4];
+        bool seen = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { m = fmaxf(m, sm[i][cl]); seen = seen || !(sl[i][cl] < 0.f); }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            wt[i] = __builtin_amdgcn_exp2f(sm[i][cl] - reference(m));
+            if (!(sl[i][cl] < 0.f)) l += wt[i] * sl[i][cl];
+        }
+        if (c >= n_cols) continue;
+        const bool last = n_shares == 1;
+        const int64_t at = (((int64_t)slot * a.pv.n_kv_heads + g) * a.shares + blockIdx.y) * C + cl;
+        const ColumnOut<float> dst{last ? out_row<float>(a, g, c, sr.row0) : nullptr, last ? nullptr : a.part + at * hd, wide_o<float>(a.out)};
+        if (!last && w == 0 && lane < 16) a.stat[at] = make_float2(m, seen ? l : -1.f);
+        const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {                       // wave w: row w of the four sums, four neighbouring features
+            const int f = 64 * k + 16 * gq + 4 * w;
+            if (f >= hd) continue;
+            floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (sl[i][cl] < 0.f) continue;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] += reinterpret_cast<const float*>(&so[i][4 * k + e][lane])[w] * wt[i];
+            }
+            dst.put(f, o * inv);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ host side
+namespace {
+constexpr int TARGET = 1024, LEAST = 8;                      // workgroups wanted; groups of 32 positions a share has at least
+int column_blocks(int hd, int64_t most_cols) { return hd <= 64 && most_cols > 16 ? 2 : 1; }
+}
+
+size_t f32_paged_workspace(int hd, int64_t most_cols, int groups) {
+    return groups > LEAST ? (size_t)2 * TARGET * 16 * column_blocks(hd, most_cols) * share_bytes(hd) : 0;
+}
+
+int f32_paged_attention(AttnArgs a, char* ws, hipStream_t s) {
+    const int hd = a.pv.hd, Hkv = a.pv.n_kv_heads;
+    const int64_t most = (int64_t)a.st.max_q_len * a.G;
+    const int cb = column_blocks(hd, most), C = 16 * cb, one_tile = most <= C;
+    const int64_t slots = one_tile ? a.st.n_seqs : (int64_t)a.st.n_tokens * a.G / C + a.st.n_seqs;
+    const Split sp = split_groups(slots * Hkv, groups_seen(a.st, (C + a.G - 1) / a.G + 1, a.window), TARGET, LEAST);
+    a.share = sp.share;
+    a.shares = sp.shares;
+    a.rows_cols = 0;                                         // all sequences are tiled
+    a.part = (float*)ws;
+    a.stat = (float2*)(ws + (size_t)(slots * Hkv * a.shares * C) * hd * sizeof(float));
+    auto kern = hd == 64    ? (cb == 1 ? k_f32_paged<64, 1, true> : k_f32_paged<64, 2, true>)
+                : hd < 64   ? (cb == 1 ? k_f32_paged<64, 1, false> : k_f32_paged<64, 2, false>)
+                : hd <= 128 ? (hd == 128 ? k_f32_paged<128, 1, true> : k_f32_paged<128, 1, false>)
+                            : (hd == 256 ? k_f32_paged<256, 1, true> : k_f32_paged<256, 1, false>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(slots * Hkv), a.shares), dim3(256), 0, s, a, (int)slots, one_tile);
     EE_LAUNCH_CHECK();
-    return EE_OK;
+    return a.shares > 1 ? launch_join(EE_F32, a, C, slots, s) : EE_OK;
 }

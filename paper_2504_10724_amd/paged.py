@@ -88,6 +88,8 @@ class PagedCache:
     """A pool of pages (see ee_paged_config) and its allocation; .pool is the whole pool, flat, in the cache's type."""
 
     def __init__(self, n_layers, n_pages, n_kv_heads, head_dim, page_size, dtype="bf16"):
+        if dtype not in ("bf16", "f32"):
+            raise ee.EEError(ee.EE_ERR_DTYPE, f"PagedCache: unknown dtype {dtype!r}")
         self.lib = ee.load()
         self.cfg = ee.ee_paged_config(n_layers, n_pages, n_kv_heads, head_dim, page_size, ee.EE_BF16 if dtype == "bf16" else ee.EE_F32)
         self.dtype, self.n_kv_heads, self.head_dim = (torch.bfloat16 if dtype == "bf16" else torch.float32), n_kv_heads, head_dim
