@@ -6,6 +6,25 @@
 typedef float  floatx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
+// How the positions of a workgroup's columns are split, and where the shares leave their sums.
+struct Split { int share = 1, shares = 1; };
+struct Shares {
+    int share = 1;                 // groups of 32 positions that a workgroup takes at most ...
+    int shares = 1;                // ... and how many of them the longest sequence has
+    float*  part = nullptr;        // sums of the shares, unnormalised [workgroup][share][column][hd]
+    float2* stat = nullptr;        // (maximum in log2 units, sum; sum < 0: no position seen) [workgroup][share][column]
+    // columns: of all workgroups, before the split; returns what follows in the workspace
+    char* place(const Split& sp, char* ws, int64_t columns, int hd) {
+        share = sp.share;
+        shares = sp.shares;
+        if (shares == 1) return ws;
+        columns *= shares;
+        part = (float*)ws;
+        stat = (float2*)(ws + (size_t)columns * hd * sizeof(float));
+        return (char*)(stat + columns);
+    }
+};
+
 // Columns: a sequence's n rows and the G query heads of a kv head make n G columns, column c = row c / G, head c % G.  All
 // columns of a (sequence, kv head) read the same keys and values.  Two kernels share the sequences of a call out:
 // one of few columns (at most rows_cols) streams its positions through the waves of a workgroup, one of many is cut into tiles.
@@ -17,11 +36,8 @@ struct AttnArgs {
     float scale2;                  // |scale| log2 e: exp(x) = 2^(x log2 e)
     uint32_t flip, keep;           // what a negative scale puts into q (its signs), and a scale of zero leaves of it
     int   window;                  // 0: none
-    int   share;                   // groups of 32 positions that a workgroup takes at most ...
-    int   shares;                  // ... and how many of them the longest sequence has
     int   rows_cols;
-    float*  part;                  // sums of the shares, unnormalised [workgroup][column][hd]
-    float2* stat;                  // (maximum in log2 units, sum; sum < 0: no position seen) [workgroup][column]
+    Shares tiles, rows;
 };
 
 // positions lo .. hi that the rows of a sequence see together, by groups of 32
@@ -192,25 +208,34 @@ template <class T> struct ColumnOut {
     }
 };
 
-// Tiles of C columns: sequence s has the slots from floor(q_start[s] G / C) + s on (see seq_of_slot).  By all lanes of a wave.
+// Tiles of C columns: sequence s has the slots from floor(q_start[s] G / C) + s on (see seq_of_slot).  By all lanes of a wave; sr is
+// what seq_rows gives for the sequence, of up to 64 sequences from the loads that found it.
 struct Tile { int s, tile; };
-__device__ __forceinline__ Tile tile_of_slot(const StepView& st, int G, int C, int slot) {
+__device__ __forceinline__ Tile tile_of_slot(const StepView& st, int G, int C, int slot, SeqRows& sr) {
     const int lane = threadIdx.x & 63;
-    auto base = [&](int i) { return (int)((int64_t)min(max(st.q_start[i], 0), st.n_tokens) * G / C) + i; };
+    auto base = [&](int start, int s) { return (int)((int64_t)min(max(start, 0), st.n_tokens) * G / C) + s; };
+    if (st.n_seqs <= 64) {
+        const bool there = lane < st.n_seqs;
+        const int start = there ? st.q_start[lane] : 0, end = there ? st.q_start[lane + 1] : 0, len = there ? st.kv_len[lane] : 0;
+        const int s = max(__popcll(__ballot(there && base(start, lane) <= slot)), 1) - 1;
+        const int a = __builtin_amdgcn_readlane(start, s);
+        sr = checked_rows(st, a, __builtin_amdgcn_readlane(end, s), __builtin_amdgcn_readlane(len, s));
+        return Tile{s, slot - base(a, s)};
+    }
     int lo = 0, n = st.n_seqs;
     while (n > 1) {
         const int step = (n + 63) >> 6, i = lane * step;
-        const int k = max(__popcll(__ballot(i < n && base(lo + i) <= slot)), 1) - 1;
+        const int k = max(__popcll(__ballot(i < n && base(st.q_start[lo + min(i, n - 1)], lo + i) <= slot)), 1) - 1;
         lo += k * step;
         n = min(step, n - k * step);
     }
     lo = to_scalar(lo);
-    return Tile{lo, slot - to_scalar(base(lo))};
+    sr = seq_rows(st, lo);
+    return Tile{lo, slot - to_scalar(base(st.q_start[lo], lo))};
 }
 
 // Host side.  blocks workgroups before any split, of `groups` groups of 32 positions at most; the split's workgroups are fewer than
 // target + blocks, and none of them is split where there are target already.
-struct Split { int share = 1, shares = 1; };
 Split split_groups(int64_t blocks, int groups, int target, int least);
 // groups of 32 positions that `rows` neighbouring rows see together at most
 int groups_seen(const StepView& st, int64_t rows, int window);

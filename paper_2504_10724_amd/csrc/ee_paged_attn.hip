@@ -171,22 +171,24 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
 // ------------------------------------------------------------------ sequences of few columns
 // One workgroup per (sequence, kv head, share of the positions); its four waves take the share's groups in turn, straight from
 // memory into registers, and join their sums through LDS at the end.
-template <int NK, int CB>
-__global__ void __launch_bounds__(256, 2)
-k_bf16_paged_rows(AttnArgs a) {
-    constexpr int HD = 32 * NK;
-    __shared__ float4 so[4][2 * NK][64];
-    __shared__ float sm[4][16 * CB], sl[4][16 * CB];
-    const int s = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - s * a.pv.n_kv_heads;
+template <int NK> struct RowsShared {
+    float4 so[4][2 * NK][64];
+    float  sm[4][16], sl[4][16];
+};
+template <int NK>
+__device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh, int pair, int share) {
+    constexpr int HD = 32 * NK, CB = 1;
+    auto& [so, sm, sl] = sh;
+    const int s = pair / a.pv.n_kv_heads, g = pair - s * a.pv.n_kv_heads;
     const SeqRows sr = seq_rows(a.st, s);
     const int n_cols = sr.n * a.G;
     if (sr.n == 0 || n_cols > a.rows_cols) return;
     const int first = sr.len - sr.n, min_lo = lowest_seen(first, a.window), max_lo = lowest_seen(sr.len - 1, a.window);
     const GroupRange all = groups_of(min_lo, sr.len - 1);
-    const int n_shares = shares_of(all.n, a.share);
-    if ((int)blockIdx.y >= n_shares) return;
+    const int n_shares = shares_of(all.n, a.rows.share);
+    if (share >= n_shares) return;
     const int lane = threadIdx.x & 63, n16 = lane & 15, w = to_scalar(threadIdx.x >> 6);
-    const int ga = all.g0 + blockIdx.y * a.share, gb = min(ga + a.share, all.g0 + all.n);
+    const int ga = all.g0 + share * a.rows.share, gb = min(ga + a.rows.share, all.g0 + all.n);
 
     Columns<NK, CB> col;
     col.start(a, g, 0, n_cols, first, sr.row0);
@@ -229,48 +231,47 @@ k_bf16_paged_rows(AttnArgs a) {
         if (part == 0) run(std::false_type{}, a0, a1);
     }
 
-    // join the waves: maxima and sums first, then the weighted sums, a wave two features blocks of every four
-#pragma unroll
-    for (int j = 0; j < CB; ++j) {
-        const float l = quad_sum(col.l[j]);
-        if (lane < 16) {
-            sm[w][16 * j + n16] = col.maximum(j);
-            sl[w][16 * j + n16] = (col.seen >> j) & 1u ? l : -1.f;
-        }
+    // join the waves: maxima and sums, then the weighted sums, a wave every fourth block of 16 features
+    const float part_l = quad_sum(col.l[0]);
+    if (lane < 16) {
+        sm[w][n16] = col.maximum(0);
+        sl[w][n16] = col.seen & 1u ? part_l : -1.f;
     }
 #pragma unroll
-    for (int j = 0; j < CB; ++j) {
-        if (16 * j >= n_cols) break;
-        __syncthreads();                                     // the statistics are there; the last block's sums have been read
+    for (int hb = 0; hb < 2 * NK; ++hb) *reinterpret_cast<floatx4*>(&so[w][hb][lane]) = col.O[0][hb];
+    __syncthreads();
+    float m = -INFINITY, l = 0.f, wt[4];
+    bool seen = false;
 #pragma unroll
-        for (int hb = 0; hb < 2 * NK; ++hb) *reinterpret_cast<floatx4*>(&so[w][hb][lane]) = col.O[j][hb];
-        __syncthreads();
-        const int c = 16 * j + n16;
-        float m = -INFINITY, l = 0.f, wt[4];
-        bool seen = false;
+    for (int i = 0; i < 4; ++i) { m = fmaxf(m, sm[i][n16]); seen = seen || !(sl[i][n16] < 0.f); }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { m = fmaxf(m, sm[i][c]); seen = seen || !(sl[i][c] < 0.f); }
+    for (int i = 0; i < 4; ++i) {
+        wt[i] = __builtin_amdgcn_exp2f(sm[i][n16] - reference(m));
+        if (!(sl[i][n16] < 0.f)) l += wt[i] * sl[i][n16];
+    }
+    if (n16 >= n_cols) return;
+    const int64_t slot = ((int64_t)pair * a.rows.shares + share) * a.rows_cols + n16;
+    const bool last = n_shares == 1;
+    const ColumnOut<bf16_t> dst{last ? out_row<bf16_t>(a, g, n16, sr.row0) : nullptr, last ? nullptr : a.rows.part + slot * HD,
+                                wide_o<bf16_t>(a.out)};
+    if (!last && w == 0 && lane < 16) a.rows.stat[slot] = make_float2(m, seen ? l : -1.f);
+    const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
+    for (int hb = w; hb < 2 * NK; hb += 4) {
+        floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            wt[i] = __builtin_amdgcn_exp2f(sm[i][c] - reference(m));
-            if (!(sl[i][c] < 0.f)) l += wt[i] * sl[i][c];
+            const floatx4 x = *reinterpret_cast<const floatx4*>(&so[i][hb][lane]);
+            if (!(sl[i][n16] < 0.f)) o += x * wt[i];
         }
-        if (c >= n_cols) continue;
-        const int64_t slot = ((int64_t)blockIdx.x * a.shares + blockIdx.y) * a.rows_cols + c;
-        const bool last = n_shares == 1;
-        const ColumnOut<bf16_t> dst{last ? out_row<bf16_t>(a, g, c, sr.row0) : nullptr, last ? nullptr : a.part + slot * HD, wide_o<bf16_t>(a.out)};
-        if (!last && w == 0 && lane < 16) a.stat[slot] = make_float2(m, seen ? l : -1.f);
-        const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
-        for (int hb = w; hb < 2 * NK; hb += 4) {
-            floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const floatx4 x = *reinterpret_cast<const floatx4*>(&so[i][hb][lane]);
-                if (!(sl[i][c] < 0.f)) o += x * wt[i];
-            }
-            dst.put(16 * hb + 4 * (lane >> 4), o * inv);
-        }
+        dst.put(16 * hb + 4 * (lane >> 4), o * inv);
     }
+}
+
+template <int NK>
+__global__ void __launch_bounds__(256, 2)
+k_bf16_paged_rows(AttnArgs a) {
+    __shared__ RowsShared<NK> sh;
+    rows_block<NK>(a, sh, blockIdx.x, blockIdx.y);
 }
 
 // ------------------------------------------------------------------ sequences of many columns
@@ -283,36 +284,40 @@ __device__ __forceinline__ void load_kib(const char* src, unsigned lane_bytes, u
 }
 
 // One workgroup per (tile of 64 CB columns, kv head, share): the four waves take 16 CB columns each and share the keys and values,
-// which go through LDS SG groups at a time, the next stage under way while one is worked on.
-template <int NK, int CB>
+// which go through LDS SG groups at a time, the next stage under way while one is worked on.  The workgroups from n_tiles on serve the
+// sequences of few columns (ROWS): in one launch they run beside the tiles and fill its tail.
+template <int NK, int CB, bool ROWS>
 __global__ void __launch_bounds__(256, NK <= 4 ? 2 : 1)
-k_bf16_paged_tile(AttnArgs a, int n_slots) {
+k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
     constexpr int HD = 32 * NK, C = 64 * CB, SG = NK <= 4 ? 2 : 1, KIB = 4 * NK;   // KiB of a group
-    __shared__ uint4 lds[2 * SG * KIB * 64];
-    const int sx = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - sx * a.pv.n_kv_heads;
+    constexpr int STAGES = 2 * SG * KIB * 64, SUMS = ROWS ? (int)sizeof(RowsShared<NK>) / 16 : 0;
+    __shared__ uint4 lds[STAGES > SUMS ? STAGES : SUMS];
+    if constexpr (ROWS) {
+        if (blockIdx.x >= n_tiles) {
+            const unsigned i = blockIdx.x - n_tiles, pairs = (unsigned)(a.st.n_seqs * a.pv.n_kv_heads);
+            rows_block<NK>(a, *reinterpret_cast<RowsShared<NK>*>(lds), (int)(i % pairs), (int)(i / pairs));
+            return;
+        }
+    }
+    const unsigned blocks = (unsigned)n_slots * a.pv.n_kv_heads;
+    const int share = (int)(blockIdx.x / blocks), x = (int)(blockIdx.x - share * blocks);
+    const int sx = x / a.pv.n_kv_heads, g = x - sx * a.pv.n_kv_heads;
     const int slot = n_slots - 1 - sx;                       // later rows see more positions: they start first
-    const Tile tl = tile_of_slot(a.st, a.G, C, slot);
+    SeqRows sr;
+    const Tile tl = tile_of_slot(a.st, a.G, C, slot, sr);
     const int s = tl.s, tile = tl.tile;
-    const SeqRows sr = seq_rows(a.st, s);
     const int n_cols = sr.n * a.G, c0 = tile * C;
     if (sr.n == 0 || n_cols <= a.rows_cols || tile < 0 || c0 >= n_cols) return;
     const int first = sr.len - sr.n;
     const int t0 = c0 / a.G, t1 = (min(c0 + C, n_cols) - 1) / a.G;
     const GroupRange all = groups_of(lowest_seen(first + t0, a.window), first + t1);
-    const int n_shares = shares_of(all.n, a.share);
-    if ((int)blockIdx.y >= n_shares) return;
-    const int ga = all.g0 + blockIdx.y * a.share, gb = min(ga + a.share, all.g0 + all.n);
+    const int n_shares = shares_of(all.n, a.tiles.share);
+    if (share >= n_shares) return;
+    const int ga = all.g0 + share * a.tiles.share, gb = min(ga + a.tiles.share, all.g0 + all.n);
     const int lane = threadIdx.x & 63, n16 = lane & 15, w = to_scalar(threadIdx.x >> 6);
     const int cw = c0 + w * 16 * CB;                         // the wave's columns and the positions they see
     const int w_first = first + cw / a.G, w_last = cw < n_cols ? first + (min(cw + 16 * CB, n_cols) - 1) / a.G : -1;
     const int min_lo = lowest_seen(w_first, a.window);
-
-    Columns<NK, CB> col;
-    col.start(a, g, cw, n_cols, first, sr.row0);
-#pragma unroll
-    for (int j = 0; j < CB; ++j)                             // in registers before the first load into LDS is under way
-#pragma unroll
-        for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(col.q[j][k].x), "+v"(col.q[j][k].y), "+v"(col.q[j][k].z), "+v"(col.q[j][k].w));
 
     const unsigned lane_bytes = (unsigned)lane * 16u, lds0 = (unsigned)(size_t)lds;
     const int n = gb - ga, n_st = (n + SG - 1) / SG;
@@ -321,7 +326,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
     // a wave sends SG NK of the SG 4 NK KiB of stage t; a group that is not there is replaced by the pool's first
     auto issue = [&](int t) {
         const int part = w * SG;
-        if ((SG * t & 63) == 0) {
+        if (t > 0 && (SG * t & 63) == 0) {
             then = look_up(SG * t);
             asm volatile("" : "+v"(then));                   // arrived before the stage is under way
         }
@@ -333,18 +338,27 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
     };
     // this wave's part of a stage has landed and it has read the one before; after the barrier so has everybody's and everybody
     auto meet = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    constexpr bool AHEAD = NK <= 4;                          // wider heads leave no registers for the next group's keys
     uint4 kf[2 * NK];
     auto group = [&](int i) { return lds + i % (2 * SG) * KIB * 64 + lane; };
     auto load_keys = [&](int i) {
 #pragma unroll
         for (int f = 0; f < 2 * NK; ++f) kf[f] = group(i)[f * 64];
     };
+    if (n > 0) then = now = look_up(0);
+    Columns<NK, CB> col;
+    col.start(a, g, cw, n_cols, first, sr.row0);             // the queries come in beside the page numbers and the first stage
     if (n > 0) {
         issue(0);
-        now = then;
         meet();
+    }
+#pragma unroll
+    for (int j = 0; j < CB; ++j)                             // in registers: a wait for them in the loop would wait for its stages
+#pragma unroll
+        for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(col.q[j][k].x), "+v"(col.q[j][k].y), "+v"(col.q[j][k].z), "+v"(col.q[j][k].w));
+    if (n > 0) {
         if (n_st > 1) issue(1);
-        load_keys(0);
+        if constexpr (AHEAD) load_keys(0);
     }
     // groups that every column of the tile sees whole: from a0 to a1 (the window starts before, the rows' own positions come after);
     // their loop tests nothing
@@ -358,6 +372,10 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
             uint4 vf[2 * NK], P[CB];
             if (works) {
                 floatx4 S[CB][2];
+                if constexpr (!AHEAD) {
+                    load_keys(i);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
                 col.scores(kf, S);
                 __builtin_amdgcn_sched_barrier(0);           // the values are under way during the softmax
 #pragma unroll
@@ -370,9 +388,11 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
                     meet();
                     if ((i + 1) / SG + 1 < n_st) issue((i + 1) / SG + 1);
                 }
-                __builtin_amdgcn_sched_barrier(0);
-                load_keys(i + 1);                            // the next keys during the second product
-                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (AHEAD) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    load_keys(i + 1);                        // the next keys during the second product
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
             if (works) col.template weigh_group<edge.value>(vf, P, pg, min_lo, w_last, a.window);
         }
@@ -384,7 +404,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
     }
 
     const bool last = n_shares == 1, wide = wide_o<bf16_t>(a.out);
-    const int64_t block = ((int64_t)(slot * (int64_t)a.pv.n_kv_heads + g) * a.shares + blockIdx.y) * C;
+    const int64_t block = (((int64_t)slot * a.pv.n_kv_heads + g) * a.tiles.shares + share) * C;
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
         const int c = cw + 16 * j + n16;
@@ -392,8 +412,8 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
         const bool seen = (col.seen >> j) & 1u;
         if (c >= n_cols) continue;
         const int64_t at = block + c - c0;
-        const ColumnOut<bf16_t> dst{last ? out_row<bf16_t>(a, g, c, sr.row0) : nullptr, last ? nullptr : a.part + at * HD, wide};
-        if (!last && lane < 16) a.stat[at] = make_float2(col.maximum(j), seen ? l : -1.f);
+        const ColumnOut<bf16_t> dst{last ? out_row<bf16_t>(a, g, c, sr.row0) : nullptr, last ? nullptr : a.tiles.part + at * HD, wide};
+        if (!last && lane < 16) a.tiles.stat[at] = make_float2(col.maximum(j), seen ? l : -1.f);
         const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
 #pragma unroll
         for (int hb = 0; hb < 2 * NK; ++hb) dst.put(16 * hb + 4 * (lane >> 4), seen ? col.O[j][hb] * inv : floatx4{0.f, 0.f, 0.f, 0.f});
@@ -401,48 +421,75 @@ k_bf16_paged_tile(AttnArgs a, int n_slots) {
 }
 
 // ------------------------------------------------------------------ join of the shares
-// A wave per column: the shares' maxima and sums, then their weighted sums, in share order (the same bits every time).
-// C = 0: sequences of few columns, blockIdx.x = (sequence, kv head); else tiles of C columns, blockIdx.x = (slot, kv head).
+// A wave per column and `cols` columns a wave: the shares' maxima and sums, a share a lane, then their weighted sums in share order
+// (the same bits every time), the two halves of the wave a share each where a half holds the features.  The sums of the first shares
+// are asked for beside the statistics.  blockIdx.x < n_tiles: (slot, kv head) of the tiles of C columns; then (sequence, kv head) of the
+// sequences of few columns.
 template <class T>
 __global__ void __launch_bounds__(256)
-k_paged_join(AttnArgs a, int C, int n_slots) {
-    const int x = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - x * a.pv.n_kv_heads;
-    const int slot = C > 0 ? n_slots - 1 - x : x;
+k_paged_join(AttnArgs a, int C, int n_slots, int n_tiles, int cols) {
+    constexpr int AT_ONCE = 4;
+    const bool tiled = (int)blockIdx.x < n_tiles;
+    const int bx = tiled ? blockIdx.x : blockIdx.x - n_tiles, x = bx / a.pv.n_kv_heads, g = bx - x * a.pv.n_kv_heads;
+    const Shares& sh = tiled ? a.tiles : a.rows;
+    const int slot = tiled ? n_slots - 1 - x : x, width = tiled ? C : a.rows_cols;
     Tile tl{x, 0};
-    if (C > 0) tl = tile_of_slot(a.st, a.G, C, slot);
-    const SeqRows sr = seq_rows(a.st, tl.s);
-    const int n_cols = sr.n * a.G, first = sr.len - sr.n, width = C > 0 ? C : a.rows_cols;
-    const int i = blockIdx.y * 4 + to_scalar(threadIdx.x >> 6), c0 = tl.tile * C, c = c0 + i;
-    if (sr.n == 0 || tl.tile < 0 || (C > 0) != (n_cols > a.rows_cols) || i >= width || c >= n_cols) return;
-    const int t0 = C > 0 ? c0 / a.G : 0, t1 = C > 0 ? (min(c0 + C, n_cols) - 1) / a.G : sr.n - 1;
-    const int shares = shares_of(groups_of(lowest_seen(first + t0, a.window), first + t1).n, a.share);
+    SeqRows sr;
+    if (tiled) tl = tile_of_slot(a.st, a.G, C, slot, sr);
+    else sr = seq_rows(a.st, x);
+    const int n_cols = sr.n * a.G, first = sr.len - sr.n, c0 = tl.tile * C, wave = to_scalar(threadIdx.x >> 6);
+    if (sr.n == 0 || tl.tile < 0 || tiled != (n_cols > a.rows_cols) || c0 >= n_cols) return;
+    const int t0 = tiled ? c0 / a.G : 0, t1 = tiled ? (min(c0 + C, n_cols) - 1) / a.G : sr.n - 1;
+    const int shares = shares_of(groups_of(lowest_seen(first + t0, a.window), first + t1).n, sh.share);
     if (shares == 1) return;                                 // its workgroup has written the result
-    const int64_t at = ((int64_t)slot * a.pv.n_kv_heads + g) * a.shares * width + i;
-    const int lane = threadIdx.x & 63, hd = a.pv.hd, f = 4 * lane;
-    float m = -INFINITY;
-    bool seen = false;
-    for (int k = lane; k < shares; k += 64) {
-        const float2 st = a.stat[at + (int64_t)k * width];
-        m = fmaxf(m, st.x);
-        seen = seen || !(st.y < 0.f);
-    }
+    const int lane = threadIdx.x & 63, hd = a.pv.hd, halves = hd <= 128 ? 2 : 1, step = AT_ONCE * halves;
+    const int half = halves == 2 ? lane >> 5 : 0, f = 4 * (halves == 2 ? lane & 31 : lane);
+    const bool wide = wide_o<T>(a.out);
+    const int64_t block = ((int64_t)slot * a.pv.n_kv_heads + g) * sh.shares * width;
+    for (int k = 0; k < cols; ++k) {
+        const int i = (blockIdx.y * 4 + wave) * cols + k, c = c0 + i;
+        if (i >= width || c >= n_cols) break;
+        const int64_t at = block + i;
+        floatx4 v[AT_ONCE];
+        auto ask = [&](int s0) {                             // sums of shares s0 + half, s0 + half + halves, ..
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-    seen = __any(seen);
-    float l = 0.f;
-    floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int k = 0; k < shares; ++k) {
-        const float2 st = a.stat[at + (int64_t)k * width];
-        const floatx4 v = f < hd ? *reinterpret_cast<const floatx4*>(a.part + (at + (int64_t)k * width) * hd + f) : floatx4{0.f, 0.f, 0.f, 0.f};
-        if (st.y < 0.f) continue;
-        const float wt = __builtin_amdgcn_exp2f(st.x - reference(m));
-        l += wt * st.y;
-        o += v * wt;
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int q = s0 + half + u * halves;
+                v[u] = q < shares && f < hd ? *reinterpret_cast<const floatx4*>(sh.part + (at + (int64_t)q * width) * hd + f) : floatx4{0.f, 0.f, 0.f, 0.f};
+            }
+        };
+        ask(0);
+        float m = -INFINITY;
+        bool seen = false;
+        float2 st = make_float2(-INFINITY, -1.f);
+        for (int q = lane; q < shares; q += 64) {
+            st = sh.stat[at + (int64_t)q * width];
+            m = fmaxf(m, st.x);
+            seen = seen || !(st.y < 0.f);
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+        seen = __any(seen);
+        float l = 0.f;
+        floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int s64 = 0; s64 < shares; s64 += 64) {
+            if (shares > 64) st = s64 + lane < shares ? sh.stat[at + (int64_t)(s64 + lane) * width] : make_float2(-INFINITY, -1.f);
+            const float wt = st.y < 0.f ? 0.f : __builtin_amdgcn_exp2f(st.x - reference(m));   // of share s64 + lane
+            if (!(st.y < 0.f)) l += wt * st.y;
+            for (int s0 = s64; s0 < min(shares, s64 + 64); s0 += step) {
+                if (s0 > 0) ask(s0);
+#pragma unroll
+                for (int u = 0; u < AT_ONCE; ++u) o += v[u] * __shfl(wt, (s0 + half + u * halves) & 63, 64);
+            }
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) l += __shfl_xor(l, d, 64);
+        if (halves == 2)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] += __shfl_xor(o[r], 32, 64);
+        const float inv = seen ? 1.0f / l : 0.f;
+        if (f < hd && half == 0) store_o4(out_row<T>(a, g, c, sr.row0) + f, wide, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
     }
-    if (f >= hd) return;
-    const float inv = seen ? 1.0f / l : 0.f;
-    store_o4(out_row<T>(a, g, c, sr.row0) + f, wide_o<T>(a.out), o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 }
 
 // ------------------------------------------------------------------ host side
@@ -465,34 +512,31 @@ int groups_seen(const StepView& st, int64_t rows, int window) {
 }
 
 namespace {
-int rows_limit(int hd) { return hd <= 128 ? 32 : 16; }       // columns that k_bf16_paged_rows holds
+constexpr int ROWS_MOST = 16;                                // columns that k_bf16_paged_rows holds
 constexpr int TILE_MOST = 128;                               // columns of the widest tile
 
 struct Plan {
     bool rows = false, tile = false;
-    int rows_cols = 0, rows_cb = 1, tile_cb = 2;
+    int rows_cols = 0, tile_cb = 2;
     int64_t rows_blocks = 0, n_slots = 0;
     Split r, t;
 };
-Plan make_plan(int hd, int Hkv, int G, const StepView& st, int window) {
+Plan make_plan(int Hkv, int G, const StepView& st, int window) {
     Plan p;
     const int64_t most = (int64_t)st.max_q_len * G;
-    const int limit = rows_limit(hd);
-    if (most <= limit) {
+    if (most <= ROWS_MOST) {
         p.rows = true;
         p.rows_cols = (int)most;
     } else {
         p.tile = true;
         // single tokens beside longer sequences; if every sequence brings max_q_len rows there are none
-        p.rows = G <= limit && (int64_t)st.n_seqs * st.max_q_len != st.n_tokens;
-        p.rows_cols = p.rows ? (G + 15) / 16 * 16 : 0;
+        p.rows = G <= ROWS_MOST && (int64_t)st.n_seqs * st.max_q_len != st.n_tokens;
+        p.rows_cols = p.rows ? ROWS_MOST : 0;
         p.tile_cb = most <= 64 ? 1 : 2;
         const int C = 64 * p.tile_cb;
         p.n_slots = (int64_t)st.n_tokens * G / C + st.n_seqs;
         p.t = split_groups(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window), TILE_TARGET, TILE_LEAST);
     }
-    while (16 * p.rows_cb < p.rows_cols) p.rows_cb *= 2;
-    p.rows_cols = std::min(p.rows_cols, 16 * p.rows_cb);
     if (p.rows) {
         p.rows_blocks = (int64_t)st.n_seqs * Hkv;
         p.r = split_groups(p.rows_blocks, groups_seen(st, (p.rows_cols + G - 1) / G, window), ROWS_TARGET, ROWS_LEAST);
@@ -504,53 +548,48 @@ Plan make_plan(int hd, int Hkv, int G, const StepView& st, int window) {
 // Split workgroups are fewer than target + blocks of fewer than target blocks, whatever the other figures are.
 size_t paged_attention_workspace(int dtype, int hd, int Hkv, int n_q_heads, const StepView& st) {
     const int64_t most = (int64_t)st.max_q_len * (n_q_heads / Hkv);
-    const int groups = (st.max_kv_len + 31) / 32, limit = rows_limit(hd);
+    const int groups = (st.max_kv_len + 31) / 32;
     if (dtype != EE_BF16) return f32_paged_workspace(hd, most, groups);
     size_t n = 0;
-    if (groups > ROWS_LEAST) n += (size_t)2 * ROWS_TARGET * std::min<int64_t>(limit, (most + 15) / 16 * 16) * share_bytes(hd);
-    if (groups > TILE_LEAST && most > limit) n += (size_t)2 * TILE_TARGET * TILE_MOST * share_bytes(hd);
+    if (groups > ROWS_LEAST) n += (size_t)2 * ROWS_TARGET * std::min<int64_t>(ROWS_MOST, most) * share_bytes(hd);
+    if (groups > TILE_LEAST && most > ROWS_MOST) n += (size_t)2 * TILE_TARGET * TILE_MOST * share_bytes(hd);
     return n;
 }
 
 int launch_join(int dtype, const AttnArgs& a, int C, int64_t slots, hipStream_t s) {
-    const int64_t blocks = (C > 0 ? slots : a.st.n_seqs) * a.pv.n_kv_heads;
-    const dim3 grid((unsigned)blocks, ((C > 0 ? C : a.rows_cols) + 3) / 4);
-    hipLaunchKernelGGL(dtype == EE_BF16 ? k_paged_join<bf16_t> : k_paged_join<float>, grid, dim3(256), 0, s, a, C, (int)slots);
+    const int64_t tiles = a.tiles.shares > 1 ? slots * a.pv.n_kv_heads : 0, pairs = a.rows.shares > 1 ? (int64_t)a.st.n_seqs * a.pv.n_kv_heads : 0;
+    if (tiles + pairs == 0) return EE_OK;
+    const int width = std::max(tiles > 0 ? C : 0, pairs > 0 ? a.rows_cols : 0);
+    // a wave takes one column until there are 32 waves a CU: 32 columns of 32 shares 6.5 us (12.8 with eight a wave for 512 x 8 columns of
+    // two), 32768 columns of two shares 29 us with one and 20 with eight
+    const int cols = (int)std::min<int64_t>(8, std::max<int64_t>(1, (tiles + pairs) * width / 8192));
+    hipLaunchKernelGGL(dtype == EE_BF16 ? k_paged_join<bf16_t> : k_paged_join<float>,
+                       dim3((unsigned)(tiles + pairs), (width + 4 * cols - 1) / (4 * cols)), dim3(256), 0, s, a, C, (int)slots, (int)tiles, cols);
     EE_LAUNCH_CHECK();
     return EE_OK;
 }
 
+template <int NK, int CB>
+static void launch_tile(const Plan& p, const AttnArgs& a, hipStream_t s) {
+    const unsigned tiles = (unsigned)(p.n_slots * a.pv.n_kv_heads * a.tiles.shares), rows = p.rows ? (unsigned)(p.rows_blocks * a.rows.shares) : 0;
+    auto kern = p.rows ? k_bf16_paged_tile<NK, CB, true> : k_bf16_paged_tile<NK, CB, false>;
+    hipLaunchKernelGGL(kern, dim3(tiles + rows), dim3(256), 0, s, a, (int)p.n_slots, tiles);
+}
+
 template <int NK>
 static int run_bf16(const Plan& p, AttnArgs a, char* ws, hipStream_t s) {
-    const int Hkv = a.pv.n_kv_heads, hd = a.pv.hd;
-    auto place = [&](int64_t columns) {                      // sums and statistics of a kernel's shares
-        a.part = (float*)ws;
-        a.stat = (float2*)(ws + (size_t)columns * hd * sizeof(float));
-        ws += (size_t)columns * share_bytes(hd);
-    };
+    const int Hkv = a.pv.n_kv_heads, C = 64 * p.tile_cb;
     a.rows_cols = p.rows_cols;
+    if (p.tile) ws = a.tiles.place(p.t, ws, p.n_slots * Hkv * C, a.pv.hd);
+    if (p.rows) a.rows.place(p.r, ws, p.rows_blocks * a.rows_cols, a.pv.hd);
     if (p.tile) {
-        a.share = p.t.share; a.shares = p.t.shares;
-        const int C = 64 * p.tile_cb;
-        if (a.shares > 1) place(p.n_slots * Hkv * a.shares * C);
-        auto kern = p.tile_cb == 1 ? k_bf16_paged_tile<NK, 1> : k_bf16_paged_tile<NK, 2>;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(p.n_slots * Hkv), a.shares), dim3(256), 0, s, a, (int)p.n_slots);
-        EE_LAUNCH_CHECK();
-        if (a.shares > 1) {
-            const int rc = launch_join(EE_BF16, a, C, p.n_slots, s);
-            if (rc != EE_OK) return rc;
-        }
+        if (p.tile_cb == 1) launch_tile<NK, 1>(p, a, s);
+        else launch_tile<NK, 2>(p, a, s);
+    } else {
+        hipLaunchKernelGGL(k_bf16_paged_rows<NK>, dim3((unsigned)p.rows_blocks, a.rows.shares), dim3(256), 0, s, a);
     }
-    if (p.rows) {
-        a.share = p.r.share; a.shares = p.r.shares;
-        if (a.shares > 1) place(p.rows_blocks * a.shares * a.rows_cols);
-        const dim3 grid((unsigned)p.rows_blocks, a.shares);
-        if (p.rows_cb == 1) hipLaunchKernelGGL((k_bf16_paged_rows<NK, 1>), grid, dim3(256), 0, s, a);
-        else if constexpr (NK <= 4) hipLaunchKernelGGL((k_bf16_paged_rows<NK, 2>), grid, dim3(256), 0, s, a);
-        EE_LAUNCH_CHECK();
-        if (a.shares > 1) return launch_join(EE_BF16, a, 0, 0, s);
-    }
-    return EE_OK;
+    EE_LAUNCH_CHECK();
+    return launch_join(EE_BF16, a, C, p.n_slots, s);
 }
 
 int launch_paged_attention(int dtype, const PagedView& pv, const StepView& st, const HeadsView& q, const HeadsView& out, int n_q_heads,
@@ -563,7 +602,7 @@ int launch_paged_attention(int dtype, const PagedView& pv, const StepView& st, c
     a.keep = scale == 0.f ? 0u : 0xffffffffu;
     a.window = window;
     if (dtype != EE_BF16) return f32_paged_attention(a, ws, s);
-    const Plan p = make_plan(pv.hd, pv.n_kv_heads, a.G, st, window);
+    const Plan p = make_plan(pv.n_kv_heads, a.G, st, window);
     switch (pv.hd) {
         case 64: return run_bf16<2>(p, a, ws, s);
         case 96: return run_bf16<3>(p, a, ws, s);

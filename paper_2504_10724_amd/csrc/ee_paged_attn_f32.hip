@@ -105,17 +105,18 @@ k_f32_paged(AttnArgs a, int n_slots, int one_tile) {
     const int sx = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - sx * a.pv.n_kv_heads;
     const int slot = n_slots - 1 - sx;                       // later rows see more positions: they start first
     Tile tl{slot, 0};
-    if (!one_tile) tl = tile_of_slot(a.st, a.G, C, slot);
-    const SeqRows sr = seq_rows(a.st, tl.s);
+    SeqRows sr;
+    if (one_tile) sr = seq_rows(a.st, slot);
+    else tl = tile_of_slot(a.st, a.G, C, slot, sr);
     const int n_cols = sr.n * a.G, c0 = tl.tile * C, hd = WHOLE ? HD : a.pv.hd;
     if (sr.n == 0 || tl.tile < 0 || c0 >= n_cols) return;
     const int first = sr.len - sr.n, t0 = c0 / a.G, t1 = (min(c0 + C, n_cols) - 1) / a.G;
     const int min_lo = lowest_seen(first + t0, a.window), max_hi = first + t1;
     const GroupRange all = groups_of(min_lo, max_hi);
-    const int n_shares = shares_of(all.n, a.share);
+    const int n_shares = shares_of(all.n, a.tiles.share);
     if ((int)blockIdx.y >= n_shares) return;
     const int lane = threadIdx.x & 63, n16 = lane & 15, gq = lane >> 4, w = to_scalar(threadIdx.x >> 6);
-    const int ga = all.g0 + blockIdx.y * a.share, gb = min(ga + a.share, all.g0 + all.n);
+    const int ga = all.g0 + blockIdx.y * a.tiles.share, gb = min(ga + a.tiles.share, all.g0 + all.n);
 
     ColumnsF32<HD, CB> col;
     col.begin(a, c0, n_cols, first);
@@ -214,9 +215,9 @@ k_f32_paged(AttnArgs a, int n_slots, int one_tile) {
         }
         if (c >= n_cols) continue;
         const bool last = n_shares == 1;
-        const int64_t at = (((int64_t)slot * a.pv.n_kv_heads + g) * a.shares + blockIdx.y) * C + cl;
-        const ColumnOut<float> dst{last ? out_row<float>(a, g, c, sr.row0) : nullptr, last ? nullptr : a.part + at * hd, wide_o<float>(a.out)};
-        if (!last && w == 0 && lane < 16) a.stat[at] = make_float2(m, seen ? l : -1.f);
+        const int64_t at = (((int64_t)slot * a.pv.n_kv_heads + g) * a.tiles.shares + blockIdx.y) * C + cl;
+        const ColumnOut<float> dst{last ? out_row<float>(a, g, c, sr.row0) : nullptr, last ? nullptr : a.tiles.part + at * hd, wide_o<float>(a.out)};
+        if (!last && w == 0 && lane < 16) a.tiles.stat[at] = make_float2(m, seen ? l : -1.f);
         const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
 #pragma unroll
         for (int k = 0; k < NC; ++k) {                       // wave w: row w of the four sums, four neighbouring features
@@ -250,16 +251,13 @@ int f32_paged_attention(AttnArgs a, char* ws, hipStream_t s) {
     const int cb = column_blocks(hd, most), C = 16 * cb, one_tile = most <= C;
     const int64_t slots = one_tile ? a.st.n_seqs : (int64_t)a.st.n_tokens * a.G / C + a.st.n_seqs;
     const Split sp = split_groups(slots * Hkv, groups_seen(a.st, (C + a.G - 1) / a.G + 1, a.window), TARGET, LEAST);
-    a.share = sp.share;
-    a.shares = sp.shares;
     a.rows_cols = 0;                                         // all sequences are tiled
-    a.part = (float*)ws;
-    a.stat = (float2*)(ws + (size_t)(slots * Hkv * a.shares * C) * hd * sizeof(float));
+    a.tiles.place(sp, ws, slots * Hkv * C, hd);
     auto kern = hd == 64    ? (cb == 1 ? k_f32_paged<64, 1, true> : k_f32_paged<64, 2, true>)
                 : hd < 64   ? (cb == 1 ? k_f32_paged<64, 1, false> : k_f32_paged<64, 2, false>)
                 : hd <= 128 ? (hd == 128 ? k_f32_paged<128, 1, true> : k_f32_paged<128, 1, false>)
                             : (hd == 256 ? k_f32_paged<256, 1, true> : k_f32_paged<256, 1, false>);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(slots * Hkv), a.shares), dim3(256), 0, s, a, (int)slots, one_tile);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(slots * Hkv), a.tiles.shares), dim3(256), 0, s, a, (int)slots, one_tile);
     EE_LAUNCH_CHECK();
-    return a.shares > 1 ? launch_join(EE_F32, a, C, slots, s) : EE_OK;
+    return launch_join(EE_F32, a, C, slots, s);
 }

@@ -78,11 +78,11 @@ __device__ __forceinline__ int seq_of_slot(const StepView& st, int slot, int T, 
 
 // rows and positions of a sequence; n = 0 if it brings none or lies outside the host's figures (status bit 2)
 struct SeqRows { int row0, n, len; };
-__device__ __forceinline__ SeqRows seq_rows(const StepView& st, int s) {
-    const int a = st.q_start[s], e = st.q_start[s + 1], len = st.kv_len[s];
+__device__ __forceinline__ SeqRows checked_rows(const StepView& st, int a, int e, int len) {
     if (a < 0 || e < a || e > st.n_tokens || e - a > st.max_q_len || len < 0 || len > st.max_kv_len) {
         if (threadIdx.x == 0 && st.status) atomicOr(st.status, 2);
         return SeqRows{0, 0, 0};
     }
     return SeqRows{a, e - a, len};
 }
+__device__ __forceinline__ SeqRows seq_rows(const StepView& st, int s) { return checked_rows(st, st.q_start[s], st.q_start[s + 1], st.kv_len[s]); }
