@@ -502,10 +502,10 @@ typedef struct {
     int32_t max_pos;     /* positions 0 .. max_pos-1                                   */
     int32_t scaling;     /* ee_rope_scaling                                            */
     int32_t trained_pos; /* EE_ROPE_BANDS: length the model was trained on             */
-    float   theta;       /* > 1                                                        */
-    float   factor;      /* > 0; not used by EE_ROPE_UNSCALED                          */
-    float   low, high;   /* EE_ROPE_BANDS: 0 <= low < high                             */
-    float   magnitude;   /* >= 0 and finite; 0 stands for 1                            */
+    double  theta;       /* > 1.  fp64: the angle of position 131071 takes all of it   */
+    double  factor;      /* > 0; not used by EE_ROPE_UNSCALED                          */
+    double  low, high;   /* EE_ROPE_BANDS: 0 <= low < high                             */
+    double  magnitude;   /* >= 0 and finite; 0 stands for 1                            */
 } ee_rope_config;
 typedef struct ee_rope ee_rope;
 

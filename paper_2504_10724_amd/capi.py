@@ -44,8 +44,8 @@ class ee_pht_row(C.Structure):
 
 class ee_rope_config(C.Structure):
     _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("pairing", C.c_int32), ("max_pos", C.c_int32),
-                ("scaling", C.c_int32), ("trained_pos", C.c_int32), ("theta", C.c_float), ("factor", C.c_float),
-                ("low", C.c_float), ("high", C.c_float), ("magnitude", C.c_float)]
+                ("scaling", C.c_int32), ("trained_pos", C.c_int32), ("theta", C.c_double), ("factor", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double)]
 
 
 class ee_heads(C.Structure):      # arguments of this type are declared as void pointers: ee_heads by reference, or its bytes

@@ -11,8 +11,8 @@ static int check_rope(const ee_rope_config* c) {
         return ee_fail(EE_ERR_SHAPE, "ee_rope_create: rot_dim must be even and at most head_dim, max_pos positive");
     if (c->pairing != EE_ROPE_HALF && c->pairing != EE_ROPE_INTERLEAVED)
         return ee_fail(EE_ERR_INVALID_ARG, "ee_rope_create: unknown pairing");
-    if (!(c->theta > 1.f) || !std::isfinite(c->theta)) return ee_fail(EE_ERR_INVALID_ARG, "ee_rope_create: theta must be > 1");
-    if (!(c->magnitude >= 0.f) || !std::isfinite(c->magnitude))
+    if (!(c->theta > 1.0) || !std::isfinite(c->theta)) return ee_fail(EE_ERR_INVALID_ARG, "ee_rope_create: theta must be > 1");
+    if (!(c->magnitude >= 0.0) || !std::isfinite(c->magnitude))
         return ee_fail(EE_ERR_INVALID_ARG, "ee_rope_create: magnitude must be >= 0");
     switch (c->scaling) {
         case EE_ROPE_UNSCALED: return EE_OK;
@@ -21,12 +21,12 @@ static int check_rope(const ee_rope_config* c) {
             if (c->rot_dim < 4) return ee_fail(EE_ERR_SHAPE, "ee_rope_create: EE_ROPE_BASE needs rot_dim > 2");
             break;
         case EE_ROPE_BANDS:
-            if (c->trained_pos < 1 || !(c->low >= 0.f) || !(c->high > c->low) || !std::isfinite(c->high))
+            if (c->trained_pos < 1 || !(c->low >= 0.0) || !(c->high > c->low) || !std::isfinite(c->high))
                 return ee_fail(EE_ERR_INVALID_ARG, "ee_rope_create: EE_ROPE_BANDS needs trained_pos > 0 and 0 <= low < high");
             break;
         default: return ee_fail(EE_ERR_INVALID_ARG, "ee_rope_create: unknown scaling");
     }
-    if (!(c->factor > 0.f) || !std::isfinite(c->factor)) return ee_fail(EE_ERR_INVALID_ARG, "ee_rope_create: factor must be > 0");
+    if (!(c->factor > 0.0) || !std::isfinite(c->factor)) return ee_fail(EE_ERR_INVALID_ARG, "ee_rope_create: factor must be > 0");
     return EE_OK;
 }
 

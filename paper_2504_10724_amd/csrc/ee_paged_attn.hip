@@ -170,7 +170,8 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
 
 // ------------------------------------------------------------------ sequences of few columns
 // One workgroup per (sequence, kv head, share of the positions); its four waves take the share's groups in turn, straight from
-// memory into registers, and join their sums through LDS at the end.
+// memory into registers, and join their sums through LDS at the end.  Bound by the cache's bytes.  They are read past L2 (each once;
+// nontemporal): 256 rows over 512-2048 positions (70B shape) 241 -> 214 us (6.2 TB/s), one row over 32768 (7B shape) 102 -> 88 us.
 template <int NK> struct RowsShared {
     float4 so[4][2 * NK][64];
     float  sm[4][16], sl[4][16];
@@ -212,14 +213,14 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
             constexpr int EARLY = NK > 6 ? NK / 2 : 2 * NK;  // values asked for before the scores: as many as fit the registers
             uint4 kf[2 * NK], vf[2 * NK];
 #pragma unroll
-            for (int f = 0; f < 2 * NK; ++f) kf[f] = kv[f * 64];
+            for (int f = 0; f < 2 * NK; ++f) kf[f] = load_once(kv + f * 64);
 #pragma unroll
-            for (int f = 0; f < EARLY; ++f) vf[f] = kv[(2 * NK + f) * 64];
+            for (int f = 0; f < EARLY; ++f) vf[f] = load_once(kv + (2 * NK + f) * 64);
             floatx4 S[CB][2];
             col.scores(kf, S);
             if constexpr (EARLY < 2 * NK) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int f = EARLY; f < 2 * NK; ++f) vf[f] = kv[(2 * NK + f) * 64];
+            for (int f = EARLY; f < 2 * NK; ++f) vf[f] = load_once(kv + (2 * NK + f) * 64);
             uint4 P[CB];
             col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
             col.template weigh_group<edge.value>(vf, P, pg, min_lo, sr.len - 1, a.window);
@@ -403,20 +404,36 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
         if (part == 0) run(std::false_type{}, a0, a1);
     }
 
-    const bool last = n_shares == 1, wide = wide_o<bf16_t>(a.out);
+    // A lane holds four neighbouring features of 2 NK blocks; two blocks at a time, lanes 16 apart swap halves, so that a lane has eight of
+    // one block and a column's 64 bytes leave in one instruction.
+    const bool last = n_shares == 1, wide = last && wide_q(a.out);
     const int64_t block = (((int64_t)slot * a.pv.n_kv_heads + g) * a.tiles.shares + share) * C;
+    const int gq = lane >> 4;
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
         const int c = cw + 16 * j + n16;
         const float l = quad_sum(col.l[j]);
         const bool seen = (col.seen >> j) & 1u;
-        if (c >= n_cols) continue;
         const int64_t at = block + c - c0;
-        const ColumnOut<bf16_t> dst{last ? out_row<bf16_t>(a, g, c, sr.row0) : nullptr, last ? nullptr : a.tiles.part + at * HD, wide};
-        if (!last && lane < 16) a.tiles.stat[at] = make_float2(col.maximum(j), seen ? l : -1.f);
-        const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
+        if (!last && c < n_cols && lane < 16) a.tiles.stat[at] = make_float2(col.maximum(j), seen ? l : -1.f);
+        const float inv = last ? 1.0f / l : 1.f;
 #pragma unroll
-        for (int hb = 0; hb < 2 * NK; ++hb) dst.put(16 * hb + 4 * (lane >> 4), seen ? col.O[j][hb] * inv : floatx4{0.f, 0.f, 0.f, 0.f});
+        for (int hb = 0; hb < 2 * NK; ++hb) col.O[j][hb] = seen ? col.O[j][hb] * inv : floatx4{0.f, 0.f, 0.f, 0.f};
+        if (wide) {
+            bf16_t* row = out_row<bf16_t>(a, g, min(c, n_cols - 1), sr.row0) + 16 * (gq & 1) + 8 * (gq >> 1);
+#pragma unroll
+            for (int hb = 0; hb < 2 * NK; hb += 2) {
+                const floatx4 &x = col.O[j][hb], &y = col.O[j][hb + 1];
+                const auto u = __builtin_amdgcn_permlane16_swap(bf16_pair(x[0], x[1]), bf16_pair(y[0], y[1]), false, false);
+                const auto v = __builtin_amdgcn_permlane16_swap(bf16_pair(x[2], x[3]), bf16_pair(y[2], y[3]), false, false);
+                if (c < n_cols) *reinterpret_cast<uint4*>(row + 16 * hb) = make_uint4(u[0], v[0], u[1], v[1]);
+            }
+        } else if (c < n_cols) {
+            const ColumnOut<bf16_t> dst{last ? out_row<bf16_t>(a, g, c, sr.row0) : nullptr, last ? nullptr : a.tiles.part + at * HD,
+                                        wide_o<bf16_t>(a.out)};
+#pragma unroll
+            for (int hb = 0; hb < 2 * NK; ++hb) dst.put(16 * hb + 4 * gq, col.O[j][hb]);
+        }
     }
 }
 

@@ -57,6 +57,13 @@ template <int V> __device__ __forceinline__ void store_row(bf16_t* p, const floa
     else p[0] = f32_to_bf16(x[0]);
 }
 
+// 16 bytes that are read once: their line need not stay in the caches
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    const words w = __builtin_nontemporal_load(reinterpret_cast<const words*>(p));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // The sequence a slot of a launch belongs to, by all 64 lanes of a wave.  A launch has for each sequence s the slots from
 // base(s) = q_start[s] / T + extra * s on; base rises with s and leaves a sequence of n rows room for
 // floor(n / T) + extra slots at least, so no prefix sum over the sequences is needed.  64 bases are looked at at a time.

@@ -583,3 +583,15 @@ def test_wrapper_refusals():
     if n > 0:
         with pytest.raises(ee.EEError):
             P.attend(b.kv, 1, b.step, q, workspace=torch.empty(n - 1, dtype=torch.uint8, device="cuda"))
+
+
+def test_rope_settings_keep_all_their_bits():
+    """a factor that fp32 would round moves the angle of a late position by thousandths"""
+    print("[case] rope settings", flush=True)
+    x, pos = _randn((64, 3, 64), torch.float32, 90), torch.arange(64, dtype=torch.int32) * 2000 + 3000
+    for scaling, factor in (("linear", 3.17), ("base", 7.53), ("bands", 1.23)):
+        rope = P.Rope(64, 131072, scaling=scaling, factor=factor, theta=9999.7, trained_pos=4096, low=1.1, high=3.7, magnitude=1.07)
+        got = rope.apply(x.cuda(), pos.cuda()).cpu().double()
+        want = R.rotate(x, pos, 64, "half", 1.07, theta=9999.7, scaling=scaling, factor=factor, trained_pos=4096, low=1.1, high=3.7)
+        # an angle of up to 1.3e5 in fp64 (2^-36 off at most), a table entry, two products and a sum
+        assert ((got - want).abs() <= 4 * U * 1.07 * 2 * x.abs().amax() + 2.0 ** -35 * 8).all(), scaling
