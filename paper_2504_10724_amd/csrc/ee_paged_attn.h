@@ -234,13 +234,14 @@ __device__ __forceinline__ Tile tile_of_slot(const StepView& st, int G, int C, i
     return Tile{lo, slot - to_scalar(base(st.q_start[lo], lo))};
 }
 
-// Host side.  blocks workgroups before any split, of `groups` groups of 32 positions at most; the split's workgroups are fewer than
-// target + blocks, and none of them is split where there are target already.
-Split split_groups(int64_t blocks, int groups, int target, int least);
+// Host side.  How to split the positions of `blocks` workgroups, of up to `groups` groups of 32: the workgroups after it are fewer than
+// SPLIT_TARGET + blocks, and nothing is split that has SPLIT_TARGET workgroups already or WHOLE_GROUPS groups at most.
+constexpr int SPLIT_TARGET = 512, WHOLE_GROUPS = 48;
+Split split_groups(int64_t blocks, int groups);
 // groups of 32 positions that `rows` neighbouring rows see together at most
 int groups_seen(const StepView& st, int64_t rows, int window);
 static inline size_t share_bytes(int hd) { return (size_t)hd * sizeof(float) + sizeof(float2); }      // of a column
 
-size_t f32_paged_workspace(int hd, int64_t most_cols, int groups);
+int64_t f32_paged_columns(int hd, int64_t most_cols);       // of a workgroup
 int f32_paged_attention(AttnArgs a, char* ws, hipStream_t s);
 int launch_join(int dtype, const AttnArgs& a, int C, int64_t slots, hipStream_t s);

@@ -178,7 +178,7 @@ template <int NK> struct RowsShared {
 };
 template <int NK>
 __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh, int pair, int share) {
-    constexpr int HD = 32 * NK, CB = 1;
+    constexpr int HD = 32 * NK, CB = 1, WAVES = 4;
     auto& [so, sm, sl] = sh;
     const int s = pair / a.pv.n_kv_heads, g = pair - s * a.pv.n_kv_heads;
     const SeqRows sr = seq_rows(a.st, s);
@@ -191,39 +191,58 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
     const int lane = threadIdx.x & 63, n16 = lane & 15, w = to_scalar(threadIdx.x >> 6);
     const int ga = all.g0 + share * a.rows.share, gb = min(ga + a.rows.share, all.g0 + all.n);
 
+    const char* pool = a.pv.pool;
+    const int n_mine = max(0, (gb - ga - w + WAVES - 1) / WAVES);        // this wave's groups: ga + w, ga + w + WAVES, ..
+    uint32_t now = NO_GROUP, then = NO_GROUP;                // pool groups of the 64 around the one at work, around the next one
+    auto look_up = [&](int i) {
+        const int grp = ga + w + WAVES * (i + lane);
+        return grp < gb ? pool_group(a.pv, a.st, s, g, grp) : NO_GROUP;
+    };
+    if (n_mine > 0) now = then = look_up(0);
     Columns<NK, CB> col;
     col.start(a, g, 0, n_cols, first, sr.row0);
-    const char* pool = a.pv.pool;
-    const int n_mine = max(0, (gb - ga - w + 3) >> 2);       // this wave's groups: ga + w, ga + w + 4, ..
-    uint32_t where = 0;
+    // keys and values of a group each have registers of their own, which are asked for again as soon as a product has used them;
+    // a group that is not there is replaced by the pool's first
+    uint4 kf[2 * NK], vf[2 * NK];
+    auto place = [&](int i) {
+        const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)then, i & 63);
+        return reinterpret_cast<const uint4*>(pool + (at == NO_GROUP ? 0ull : (uint64_t)at * (HD * 128))) + lane;
+    };
+    auto load_keys = [&](const uint4* kv) {
+#pragma unroll
+        for (int f = 0; f < 2 * NK; ++f) kf[f] = load_once(kv + f * 64);
+    };
+    auto load_values = [&](const uint4* kv) {
+#pragma unroll
+        for (int f = 0; f < 2 * NK; ++f) vf[f] = load_once(kv + (2 * NK + f) * 64);
+    };
+    if (n_mine > 0) {
+        load_keys(place(0));
+        load_values(place(0));
+    }
     // whether a column does not see all of a group is settled by range, so the loop over the groups that all see has no test:
     // edge before a0 (the window's start) and from a1 on (the rows' own positions)
-    auto mine_from = [&](int grp) { return min(max((grp - ga - w + 3) >> 2, 0), n_mine); };
-    const int a0 = mine_from((max_lo + 31) >> 5), a1 = max(a0, mine_from((first + 1) >> 5));
+    auto mine_from = [&](int grp) { return min(max((grp - ga - w + WAVES - 1) / WAVES, 0), n_mine); };
+    const int a0 = max_lo > 0 ? mine_from((max_lo + 31) >> 5) : 0, a1 = max(a0, first < 31 ? 0 : mine_from((first + 1) >> 5));
     auto run = [&](auto edge, int from, int to) {
         for (int i = from; i < to; ++i) {
-            if ((i & 63) == 0 || i == from) {
-                const int grp = ga + w + 4 * ((i & ~63) + lane);
-                where = grp < gb ? pool_group(a.pv, a.st, s, g, grp) : NO_GROUP;
-            }
-            const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)where, i & 63);
-            if (at == NO_GROUP) continue;
-            const uint4* kv = reinterpret_cast<const uint4*>(pool + (uint64_t)at * (HD * 128)) + lane;
-            const int pg = (ga + w + 4 * i) << 5;
-            constexpr int EARLY = NK > 6 ? NK / 2 : 2 * NK;  // values asked for before the scores: as many as fit the registers
-            uint4 kf[2 * NK], vf[2 * NK];
-#pragma unroll
-            for (int f = 0; f < 2 * NK; ++f) kf[f] = load_once(kv + f * 64);
-#pragma unroll
-            for (int f = 0; f < EARLY; ++f) vf[f] = load_once(kv + (2 * NK + f) * 64);
-            floatx4 S[CB][2];
-            col.scores(kf, S);
-            if constexpr (EARLY < 2 * NK) __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int f = EARLY; f < 2 * NK; ++f) vf[f] = load_once(kv + (2 * NK + f) * 64);
+            if ((i & 63) == 0 && i > 0) now = then;
+            const bool works = (uint32_t)__builtin_amdgcn_readlane((int)now, i & 63) != NO_GROUP;
+            const int pg = (ga + w + WAVES * i) << 5;
+            if (i + 1 < n_mine && ((i + 1) & 63) == 0) then = look_up(i + 1);
+            const uint4* next = place(min(i + 1, n_mine - 1));
             uint4 P[CB];
-            col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
-            col.template weigh_group<edge.value>(vf, P, pg, min_lo, sr.len - 1, a.window);
+            floatx4 S[CB][2];
+            if (works) col.scores(kf, S);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + 1 < n_mine) load_keys(next);
+            __builtin_amdgcn_sched_barrier(0);
+            if (works) {
+                col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
+                col.template weigh_group<edge.value>(vf, P, pg, min_lo, sr.len - 1, a.window);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + 1 < n_mine) load_values(next);
         }
     };
 #pragma unroll 1
@@ -232,7 +251,7 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
         if (part == 0) run(std::false_type{}, a0, a1);
     }
 
-    // join the waves: maxima and sums, then the weighted sums, a wave every fourth block of 16 features
+    // join the waves: maxima and sums, then the weighted sums, the blocks of 16 features in turn
     const float part_l = quad_sum(col.l[0]);
     if (lane < 16) {
         sm[w][n16] = col.maximum(0);
@@ -241,12 +260,12 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
 #pragma unroll
     for (int hb = 0; hb < 2 * NK; ++hb) *reinterpret_cast<floatx4*>(&so[w][hb][lane]) = col.O[0][hb];
     __syncthreads();
-    float m = -INFINITY, l = 0.f, wt[4];
+    float m = -INFINITY, l = 0.f, wt[WAVES];
     bool seen = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { m = fmaxf(m, sm[i][n16]); seen = seen || !(sl[i][n16] < 0.f); }
+    for (int i = 0; i < WAVES; ++i) { m = fmaxf(m, sm[i][n16]); seen = seen || !(sl[i][n16] < 0.f); }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < WAVES; ++i) {
         wt[i] = __builtin_amdgcn_exp2f(sm[i][n16] - reference(m));
         if (!(sl[i][n16] < 0.f)) l += wt[i] * sl[i][n16];
     }
@@ -257,10 +276,10 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
                                 wide_o<bf16_t>(a.out)};
     if (!last && w == 0 && lane < 16) a.rows.stat[slot] = make_float2(m, seen ? l : -1.f);
     const float inv = last ? (seen ? 1.0f / l : 0.f) : 1.f;
-    for (int hb = w; hb < 2 * NK; hb += 4) {
+    for (int hb = w; hb < 2 * NK; hb += WAVES) {
         floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < WAVES; ++i) {
             const floatx4 x = *reinterpret_cast<const floatx4*>(&so[i][hb][lane]);
             if (!(sl[i][n16] < 0.f)) o += x * wt[i];
         }
@@ -269,7 +288,7 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
 }
 
 template <int NK>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, NK <= 4 ? 2 : 1)
 k_bf16_paged_rows(AttnArgs a) {
     __shared__ RowsShared<NK> sh;
     rows_block<NK>(a, sh, blockIdx.x, blockIdx.y);
@@ -511,16 +530,16 @@ k_paged_join(AttnArgs a, int C, int n_slots, int n_tiles, int cols) {
 
 // ------------------------------------------------------------------ host side
 // Who serves what, and in how many shares.  From the host's figures alone: the device's are not known here.
-namespace {
-constexpr int ROWS_TARGET = 1024, ROWS_LEAST = 8;            // workgroups wanted; groups of 32 positions a share has at least
-constexpr int TILE_TARGET = 512, TILE_LEAST = 16;
-
-}  // namespace
-
-Split split_groups(int64_t blocks, int groups, int target, int least) {
-    const int64_t want = std::max<int64_t>(1, (target + blocks - 1) / blocks);
-    const int share = (int)std::max<int64_t>(least, (groups + want - 1) / want);
-    return Split{share, std::max(1, (groups + share - 1) / share)};
+// The join of shares is a launch of its own and takes 4 to 5 us, what 48 groups take four waves: up to those nothing is split.  Beyond,
+// there should be two workgroups a CU, with 16 groups each at least.  Measured (us, one token a row): 16 rows of 512-2048 positions
+// (70B shape, 128 pairs of row and kv head) in shares of 8 groups 24.2, of 16 21.8; 64 rows (512 pairs) split 64.9, whole 56.7; one row of
+// 1000 positions split 10.2, whole 9.0; two rows of 20000 (4 pairs), shares of 8 groups 19.7, of 16 16.6.
+Split split_groups(int64_t blocks, int groups) {
+    if (groups <= WHOLE_GROUPS || blocks >= SPLIT_TARGET) return Split{std::max(groups, 1), 1};
+    const int64_t want = (SPLIT_TARGET + blocks - 1) / blocks;
+    const int most = (int)std::min<int64_t>(want, groups / 16);
+    const int share = (groups + most - 1) / most;
+    return Split{share, (groups + share - 1) / share};
 }
 
 int groups_seen(const StepView& st, int64_t rows, int window) {
@@ -552,11 +571,11 @@ Plan make_plan(int Hkv, int G, const StepView& st, int window) {
         p.tile_cb = most <= 64 ? 1 : 2;
         const int C = 64 * p.tile_cb;
         p.n_slots = (int64_t)st.n_tokens * G / C + st.n_seqs;
-        p.t = split_groups(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window), TILE_TARGET, TILE_LEAST);
+        p.t = split_groups(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window));
     }
     if (p.rows) {
         p.rows_blocks = (int64_t)st.n_seqs * Hkv;
-        p.r = split_groups(p.rows_blocks, groups_seen(st, (p.rows_cols + G - 1) / G, window), ROWS_TARGET, ROWS_LEAST);
+        p.r = split_groups(p.rows_blocks, groups_seen(st, (p.rows_cols + G - 1) / G, window));
     }
     return p;
 }
@@ -565,12 +584,10 @@ Plan make_plan(int Hkv, int G, const StepView& st, int window) {
 // Split workgroups are fewer than target + blocks of fewer than target blocks, whatever the other figures are.
 size_t paged_attention_workspace(int dtype, int hd, int Hkv, int n_q_heads, const StepView& st) {
     const int64_t most = (int64_t)st.max_q_len * (n_q_heads / Hkv);
-    const int groups = (st.max_kv_len + 31) / 32;
-    if (dtype != EE_BF16) return f32_paged_workspace(hd, most, groups);
-    size_t n = 0;
-    if (groups > ROWS_LEAST) n += (size_t)2 * ROWS_TARGET * std::min<int64_t>(ROWS_MOST, most) * share_bytes(hd);
-    if (groups > TILE_LEAST && most > ROWS_MOST) n += (size_t)2 * TILE_TARGET * TILE_MOST * share_bytes(hd);
-    return n;
+    if ((st.max_kv_len + 31) / 32 <= WHOLE_GROUPS) return 0;
+    int64_t columns = f32_paged_columns(hd, most);
+    if (dtype == EE_BF16) columns = std::min<int64_t>(ROWS_MOST, most) + (most > ROWS_MOST ? TILE_MOST : 0);
+    return (size_t)2 * SPLIT_TARGET * columns * share_bytes(hd);
 }
 
 int launch_join(int dtype, const AttnArgs& a, int C, int64_t slots, hipStream_t s) {
@@ -603,7 +620,8 @@ static int run_bf16(const Plan& p, AttnArgs a, char* ws, hipStream_t s) {
         if (p.tile_cb == 1) launch_tile<NK, 1>(p, a, s);
         else launch_tile<NK, 2>(p, a, s);
     } else {
-        hipLaunchKernelGGL(k_bf16_paged_rows<NK>, dim3((unsigned)p.rows_blocks, a.rows.shares), dim3(256), 0, s, a);
+        const dim3 grid((unsigned)p.rows_blocks, a.rows.shares);
+        hipLaunchKernelGGL(k_bf16_paged_rows<NK>, grid, dim3(256), 0, s, a);
     }
     EE_LAUNCH_CHECK();
     return launch_join(EE_BF16, a, C, p.n_slots, s);

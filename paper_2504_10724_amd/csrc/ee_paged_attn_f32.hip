@@ -236,21 +236,14 @@ k_f32_paged(AttnArgs a, int n_slots, int one_tile) {
 }
 
 // ------------------------------------------------------------------ host side
-namespace {
-constexpr int TARGET = 1024, LEAST = 8;                      // workgroups wanted; groups of 32 positions a share has at least
-int column_blocks(int hd, int64_t most_cols) { return hd <= 64 && most_cols > 16 ? 2 : 1; }
-}
-
-size_t f32_paged_workspace(int hd, int64_t most_cols, int groups) {
-    return groups > LEAST ? (size_t)2 * TARGET * 16 * column_blocks(hd, most_cols) * share_bytes(hd) : 0;
-}
+int64_t f32_paged_columns(int hd, int64_t most_cols) { return hd <= 64 && most_cols > 16 ? 32 : 16; }
 
 int f32_paged_attention(AttnArgs a, char* ws, hipStream_t s) {
     const int hd = a.pv.hd, Hkv = a.pv.n_kv_heads;
     const int64_t most = (int64_t)a.st.max_q_len * a.G;
-    const int cb = column_blocks(hd, most), C = 16 * cb, one_tile = most <= C;
+    const int C = (int)f32_paged_columns(hd, most), cb = C / 16, one_tile = most <= C;
     const int64_t slots = one_tile ? a.st.n_seqs : (int64_t)a.st.n_tokens * a.G / C + a.st.n_seqs;
-    const Split sp = split_groups(slots * Hkv, groups_seen(a.st, (C + a.G - 1) / a.G + 1, a.window), TARGET, LEAST);
+    const Split sp = split_groups(slots * Hkv, groups_seen(a.st, (C + a.G - 1) / a.G + 1, a.window));
     a.rows_cols = 0;                                         // all sequences are tiled
     a.tiles.place(sp, ws, slots * Hkv * C, hd);
     auto kern = hd == 64    ? (cb == 1 ? k_f32_paged<64, 1, true> : k_f32_paged<64, 2, true>)
