@@ -75,27 +75,30 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
             P[j] = make_uint4(bf16_pair(e[j][0], e[j][1]), bf16_pair(e[j][2], e[j][3]), bf16_pair(e[j][4], e[j][5]), bf16_pair(e[j][6], e[j][7]));
     }
 
-    // S^T = K Q^T of a group: kf[b NK + k] holds features 32 k .. of the 16 positions of half b
+    // S^T += K Q^T of a group over N of the NK slices of 32 features, from K0 on: kf[b N + k] holds slice K0 + k of the 16 positions of half b
+    template <int K0, int N> __device__ __forceinline__ void add_scores(const uint4 (&kf)[2 * N], floatx4 (&S)[CB][2]) const {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int j = 0; j < CB; ++j) {
+                S[j][0] = mfma(kf[k], q[j][K0 + k], S[j][0]);
+                S[j][1] = mfma(kf[N + k], q[j][K0 + k], S[j][1]);
+            }
+    }
     __device__ __forceinline__ void scores(const uint4 (&kf)[2 * NK], floatx4 (&S)[CB][2]) const {
 #pragma unroll
         for (int j = 0; j < CB; ++j) S[j][0] = S[j][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < NK; ++k)
-#pragma unroll
-            for (int j = 0; j < CB; ++j) {
-                S[j][0] = mfma(kf[k], q[j][k], S[j][0]);
-                S[j][1] = mfma(kf[NK + k], q[j][k], S[j][1]);
-            }
+        add_scores<0, NK>(kf, S);
     }
 
-    // second product of a group at pg with the values vf
-    template <bool EDGE>
-    __device__ __forceinline__ void weigh_group(const uint4 (&vf)[2 * NK], const uint4 (&P)[CB], int pg, int min_lo, int max_hi, int window) {
+    // second product of a group at pg with the values vf of N blocks of 16 features from block H0 on
+    template <bool EDGE, int H0 = 0, int N>
+    __device__ __forceinline__ void weigh_group(const uint4 (&vf)[N], const uint4 (&P)[CB], int pg, int min_lo, int max_hi, int window) {
         if constexpr (EDGE) {
-            weigh_edge(vf, P, pg, min_lo, max_hi, window);
+            weigh_edge<H0, N>(vf, P, pg, min_lo, max_hi, window);
         } else {
 #pragma unroll
-            for (int hb = 0; hb < 2 * NK; ++hb) weigh(hb, vf[hb], P);
+            for (int hb = 0; hb < N; ++hb) weigh(H0 + hb, vf[hb], P);
         }
     }
 
@@ -110,22 +113,23 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
     // infinities of either sign met with a positive probability, NaN and everything non-finite met with a zero one.
     // What lies outside min_lo .. max_hi no column sees; it may be memory nobody has written, and counts as zero.
     // Words hold two bf16; the tests work on both halves without a carry between.
-    __device__ __forceinline__ void weigh_edge(const uint4 (&vf)[2 * NK], const uint4 (&P)[CB], int pg, int min_lo, int max_hi, int window) {
+    template <int H0, int N>
+    __device__ __forceinline__ void weigh_edge(const uint4 (&vf)[N], const uint4 (&P)[CB], int pg, int min_lo, int max_hi, int window) {
         uint32_t in[4], any = 0;
         seen_words(in, min_lo, max_hi, pg);
         auto inside = [&](uint4 v) { return make_uint4(v.x & in[0], v.y & in[1], v.z & in[2], v.w & in[3]); };
 #pragma unroll
-        for (int hb = 0; hb < 2 * NK; ++hb) {
+        for (int hb = 0; hb < N; ++hb) {
             const uint4 v = inside(vf[hb]);
             any |= odd_bits(v.x) | odd_bits(v.y) | odd_bits(v.z) | odd_bits(v.w);
         }
         if (__builtin_expect(!__any(any != 0), 1)) {
 #pragma unroll
-            for (int hb = 0; hb < 2 * NK; ++hb) weigh(hb, inside(vf[hb]), P);
+            for (int hb = 0; hb < N; ++hb) weigh(H0 + hb, inside(vf[hb]), P);
             return;
         }
 #pragma unroll
-        for (int hb = 0; hb < 2 * NK; ++hb) {
+        for (int hb = 0; hb < N; ++hb) {
             __builtin_amdgcn_sched_barrier(0);               // rare: one block at a time, few registers
             const uint4 v = inside(vf[hb]);
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -139,7 +143,7 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
                 neg[i] = odd & ~frac & sign & 0x3f803f80u;
                 pos[i] = odd & ~frac & ~sign & 0x3f803f80u;
             }
-            weigh(hb, make_uint4(fin[0], fin[1], fin[2], fin[3]), P);
+            weigh(H0 + hb, make_uint4(fin[0], fin[1], fin[2], fin[3]), P);
             const uint4 vp = make_uint4(pos[0], pos[1], pos[2], pos[3]), vn = make_uint4(neg[0], neg[1], neg[2], neg[3]),
                         vx = make_uint4(nan[0], nan[1], nan[2], nan[3]),
                         va = make_uint4(pos[0] | neg[0] | nan[0], pos[1] | neg[1] | nan[1], pos[2] | neg[2] | nan[2], pos[3] | neg[3] | nan[3]);
@@ -159,9 +163,9 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
                 const floatx4 up = mfma(vp, ps, zero), down = mfma(vn, ps, zero), bad = mfma(va, pz, mfma(vx, ps, zero));
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    O[j][hb][r] += up[r] > 0.f ? INFINITY : 0.f;
-                    O[j][hb][r] -= down[r] > 0.f ? INFINITY : 0.f;
-                    O[j][hb][r] = bad[r] > 0.f ? NAN : O[j][hb][r];
+                    O[j][H0 + hb][r] += up[r] > 0.f ? INFINITY : 0.f;
+                    O[j][H0 + hb][r] -= down[r] > 0.f ? INFINITY : 0.f;
+                    O[j][H0 + hb][r] = bad[r] > 0.f ? NAN : O[j][H0 + hb][r];
                 }
             }
         }
@@ -307,7 +311,7 @@ __device__ __forceinline__ void load_kib(const char* src, unsigned lane_bytes, u
 // which go through LDS SG groups at a time, the next stage under way while one is worked on.  The workgroups from n_tiles on serve the
 // sequences of few columns (ROWS): in one launch they run beside the tiles and fill its tail.
 template <int NK, int CB, bool ROWS>
-__global__ void __launch_bounds__(256, NK <= 4 ? 2 : 1)
+__global__ void __launch_bounds__(256, 2)
 k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
     constexpr int HD = 32 * NK, C = 64 * CB, SG = NK <= 4 ? 2 : 1, KIB = 4 * NK;   // KiB of a group
     constexpr int STAGES = 2 * SG * KIB * 64, SUMS = ROWS ? (int)sizeof(RowsShared<NK>) / 16 : 0;
@@ -358,12 +362,14 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
     };
     // this wave's part of a stage has landed and it has read the one before; after the barrier so has everybody's and everybody
     auto meet = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-    constexpr bool AHEAD = NK <= 4;                          // wider heads leave no registers for the next group's keys
-    uint4 kf[2 * NK];
+    // Heads of up to 128 features: the next group's keys are read during the second product.  Wider ones do not have the registers: keys
+    // and values are read in two halves each, when they are needed.
+    constexpr bool AHEAD = NK <= 4;
+    uint4 kf[AHEAD ? 2 * NK : 1];
     auto group = [&](int i) { return lds + i % (2 * SG) * KIB * 64 + lane; };
     auto load_keys = [&](int i) {
 #pragma unroll
-        for (int f = 0; f < 2 * NK; ++f) kf[f] = group(i)[f * 64];
+        for (int f = 0; f < (AHEAD ? 2 * NK : 1); ++f) kf[f] = group(i)[f * 64];
     };
     if (n > 0) then = now = look_up(0);
     Columns<NK, CB> col;
@@ -389,32 +395,60 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
             if ((i & 63) == 0 && i > 0) now = then;
             const bool works = pg <= w_last && (!edge.value || pg + 31 >= min_lo) &&
                                (uint32_t)__builtin_amdgcn_readlane((int)now, i & 63) != NO_GROUP;
-            uint4 vf[2 * NK], P[CB];
-            if (works) {
-                floatx4 S[CB][2];
-                if constexpr (!AHEAD) {
-                    load_keys(i);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                col.scores(kf, S);
-                __builtin_amdgcn_sched_barrier(0);           // the values are under way during the softmax
-#pragma unroll
-                for (int f = 0; f < 2 * NK; ++f) vf[f] = group(i)[(2 * NK + f) * 64];
-                __builtin_amdgcn_sched_barrier(0);
-                col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
-            }
-            if (i + 1 < n) {
-                if ((i + 1) % SG == 0) {                     // the stage is in registers: its buffer is free
+            uint4 P[CB];
+            floatx4 S[CB][2];
+            auto next_stage = [&] {                          // after the last read of the stage
+                if (i + 1 < n && (i + 1) % SG == 0) {
                     meet();
                     if ((i + 1) / SG + 1 < n_st) issue((i + 1) / SG + 1);
                 }
-                if constexpr (AHEAD) {
+            };
+            if constexpr (AHEAD) {
+                uint4 vf[2 * NK];
+                if (works) {
+                    col.scores(kf, S);
+                    __builtin_amdgcn_sched_barrier(0);       // the values are under way during the softmax
+#pragma unroll
+                    for (int f = 0; f < 2 * NK; ++f) vf[f] = group(i)[(2 * NK + f) * 64];
                     __builtin_amdgcn_sched_barrier(0);
-                    load_keys(i + 1);                        // the next keys during the second product
+                    col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
+                }
+                next_stage();
+                if (i + 1 < n) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    load_keys(i + 1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                if (works) col.template weigh_group<edge.value>(vf, P, pg, min_lo, w_last, a.window);
+            } else {
+                if (works) {
+                    constexpr int H = NK / 2;
+                    uint4 half[2 * H];
+                    auto keys = [&](int k0) {
+#pragma unroll
+                        for (int f = 0; f < 2 * H; ++f) half[f] = group(i)[(f / H * NK + k0 + f % H) * 64];
+                    };
+                    auto values = [&](int h0) {
+#pragma unroll
+                        for (int f = 0; f < 2 * H; ++f) half[f] = group(i)[(2 * NK + h0 + f) * 64];
+                    };
+#pragma unroll
+                    for (int j = 0; j < CB; ++j) S[j][0] = S[j][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+                    keys(0);
+                    col.template add_scores<0, H>(half, S);
+                    __builtin_amdgcn_sched_barrier(0);
+                    keys(H);
+                    col.template add_scores<H, H>(half, S);
+                    __builtin_amdgcn_sched_barrier(0);
+                    values(0);
+                    col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
+                    col.template weigh_group<edge.value, 0>(half, P, pg, min_lo, w_last, a.window);
+                    __builtin_amdgcn_sched_barrier(0);
+                    values(NK);
+                    col.template weigh_group<edge.value, NK>(half, P, pg, min_lo, w_last, a.window);
+                }
+                next_stage();
             }
-            if (works) col.template weigh_group<edge.value>(vf, P, pg, min_lo, w_last, a.window);
         }
     };
 #pragma unroll 1
@@ -557,7 +591,7 @@ struct Plan {
     int64_t rows_blocks = 0, n_slots = 0;
     Split r, t;
 };
-Plan make_plan(int Hkv, int G, const StepView& st, int window) {
+Plan make_plan(int hd, int Hkv, int G, const StepView& st, int window) {
     Plan p;
     const int64_t most = (int64_t)st.max_q_len * G;
     if (most <= ROWS_MOST) {
@@ -568,7 +602,7 @@ Plan make_plan(int Hkv, int G, const StepView& st, int window) {
         // single tokens beside longer sequences; if every sequence brings max_q_len rows there are none
         p.rows = G <= ROWS_MOST && (int64_t)st.n_seqs * st.max_q_len != st.n_tokens;
         p.rows_cols = p.rows ? ROWS_MOST : 0;
-        p.tile_cb = most <= 64 ? 1 : 2;
+        p.tile_cb = most <= 64 || hd > 128 ? 1 : 2;
         const int C = 64 * p.tile_cb;
         p.n_slots = (int64_t)st.n_tokens * G / C + st.n_seqs;
         p.t = split_groups(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window));
@@ -603,11 +637,17 @@ int launch_join(int dtype, const AttnArgs& a, int C, int64_t slots, hipStream_t 
     return EE_OK;
 }
 
+// Heads of up to 128 features serve single rows in the tiles' launch; the streaming kernel of wider ones needs registers that the tiles
+// do not leave it there.
 template <int NK, int CB>
 static void launch_tile(const Plan& p, const AttnArgs& a, hipStream_t s) {
     const unsigned tiles = (unsigned)(p.n_slots * a.pv.n_kv_heads * a.tiles.shares), rows = p.rows ? (unsigned)(p.rows_blocks * a.rows.shares) : 0;
-    auto kern = p.rows ? k_bf16_paged_tile<NK, CB, true> : k_bf16_paged_tile<NK, CB, false>;
-    hipLaunchKernelGGL(kern, dim3(tiles + rows), dim3(256), 0, s, a, (int)p.n_slots, tiles);
+    if constexpr (NK <= 4) {
+        auto kern = p.rows ? k_bf16_paged_tile<NK, CB, true> : k_bf16_paged_tile<NK, CB, false>;
+        hipLaunchKernelGGL(kern, dim3(tiles + rows), dim3(256), 0, s, a, (int)p.n_slots, tiles);
+    } else {
+        hipLaunchKernelGGL((k_bf16_paged_tile<NK, CB, false>), dim3(tiles), dim3(256), 0, s, a, (int)p.n_slots, tiles);
+    }
 }
 
 template <int NK>
@@ -617,12 +657,12 @@ static int run_bf16(const Plan& p, AttnArgs a, char* ws, hipStream_t s) {
     if (p.tile) ws = a.tiles.place(p.t, ws, p.n_slots * Hkv * C, a.pv.hd);
     if (p.rows) a.rows.place(p.r, ws, p.rows_blocks * a.rows_cols, a.pv.hd);
     if (p.tile) {
-        if (p.tile_cb == 1) launch_tile<NK, 1>(p, a, s);
-        else launch_tile<NK, 2>(p, a, s);
-    } else {
-        const dim3 grid((unsigned)p.rows_blocks, a.rows.shares);
-        hipLaunchKernelGGL(k_bf16_paged_rows<NK>, grid, dim3(256), 0, s, a);
+        if (NK > 4 || p.tile_cb == 1) launch_tile<NK, 1>(p, a, s);
+        else if constexpr (NK <= 4) launch_tile<NK, 2>(p, a, s);
+        EE_LAUNCH_CHECK();
     }
+    if (p.rows && (NK > 4 || !p.tile))
+        hipLaunchKernelGGL(k_bf16_paged_rows<NK>, dim3((unsigned)p.rows_blocks, a.rows.shares), dim3(256), 0, s, a);
     EE_LAUNCH_CHECK();
     return launch_join(EE_BF16, a, C, p.n_slots, s);
 }
@@ -637,7 +677,7 @@ int launch_paged_attention(int dtype, const PagedView& pv, const StepView& st, c
     a.keep = scale == 0.f ? 0u : 0xffffffffu;
     a.window = window;
     if (dtype != EE_BF16) return f32_paged_attention(a, ws, s);
-    const Plan p = make_plan(pv.n_kv_heads, a.G, st, window);
+    const Plan p = make_plan(pv.hd, pv.n_kv_heads, a.G, st, window);
     switch (pv.hd) {
         case 64: return run_bf16<2>(p, a, ws, s);
         case 96: return run_bf16<3>(p, a, ws, s);
