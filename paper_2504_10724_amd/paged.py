@@ -1,5 +1,5 @@
 """Device-memory plumbing around libee's rotary tables and paged cache: PyTorch allocates the buffers and provides the
-stream, libee does all the work.  What a server does with them, per layer and step:
+stream, libee does all the work.  What a server does with them, per layer and step (examples/paged_serving.py runs it):
 
     rope = Rope(head_dim, max_pos)
     kv = PagedCache(n_layers, n_pages, n_kv_heads, head_dim, page_size, dtype="bf16")
@@ -13,7 +13,7 @@ import struct
 import torch
 
 from . import capi as ee
-from .session import _stream
+from .session import _raw_stream
 
 _PAIRINGS = {"half": ee.EE_ROPE_HALF, "interleaved": ee.EE_ROPE_INTERLEAVED}
 _SCALINGS = {"none": ee.EE_ROPE_UNSCALED, "linear": ee.EE_ROPE_LINEAR, "base": ee.EE_ROPE_BASE, "bands": ee.EE_ROPE_BANDS}
@@ -22,6 +22,11 @@ _DTYPES = {torch.float32: ee.EE_F32, torch.bfloat16: ee.EE_BF16}
 
 def _refuse(what):
     raise ee.EEError(ee.EE_ERR_INVALID_ARG, what)
+
+
+def _stream(t):
+    """handle of the current stream of a tensor's device (a fifth of the time the way through the current device takes)"""
+    return torch.cuda.current_stream(t.device).cuda_stream if _raw_stream is None else _raw_stream(t.get_device())
 
 
 _pack_heads = struct.Struct("Pqq").pack      # an ee_heads as bytes, a fifth of the time a ctypes structure takes
@@ -80,7 +85,7 @@ class Rope:
         n, heads, _ = shape
         ee.check(self.lib.ee_rope_apply(self.h, _DTYPES[dtype], _heads(x, "Rope.apply", shape, dtype), _heads(out, "Rope.apply", shape, dtype),
                                         _int32(pos, "Rope.apply: pos", n).data_ptr(), n, heads, inverse,
-                                        None if status is None else _int32(status, "Rope.apply: status", 1).data_ptr(), _stream()))
+                                        None if status is None else _int32(status, "Rope.apply: status", 1).data_ptr(), _stream(x)))
         return out
 
 
@@ -145,7 +150,7 @@ def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
         if q_out is None:
             q_out = torch.empty(shape, dtype=dtype, device=q.device)
         qh, qo = _heads(q, "append", shape, dtype), _heads(q_out, "append", shape, dtype)
-    ee.check(kv.lib.ee_paged_append(kv.h, layer, step.ref, None if rope is None else rope.h, kh, vh, qh, qo, n_q, _stream()))
+    ee.check(kv.lib.ee_paged_append(kv.h, layer, step.ref, None if rope is None else rope.h, kh, vh, qh, qo, n_q, _stream(k)))
     return q_out
 
 
@@ -162,5 +167,5 @@ def attend(kv, layer, step, q, *, out=None, scale=None, window=0, workspace=None
         workspace = kv.workspace(step, heads)
     ee.check(kv.lib.ee_paged_attention(kv.h, layer, step.ref, _heads(q, "attend", shape, dtype), _heads(out, "attend", shape, dtype), heads,
                                        kv.head_dim ** -0.5 if scale is None else scale, window, workspace.data_ptr(), workspace.numel(),
-                                       _stream()))
+                                       _stream(q)))
     return out
