@@ -300,21 +300,26 @@ k_bf16_paged_rows(AttnArgs a) {
 
 // ------------------------------------------------------------------ sequences of many columns
 // 1 KiB (64 lanes x 16 bytes) from memory into LDS, past the registers; waited for with vmcnt by hand
-__device__ __forceinline__ void load_kib(const char* src, unsigned lane_bytes, unsigned lds_byte) {
+template <bool ONCE> __device__ __forceinline__ void load_kib(const char* src, unsigned lane_bytes, unsigned lds_byte) {
     const uint64_t a = reinterpret_cast<uint64_t>(src);
     const uint64_t base = ((uint64_t)(uint32_t)to_scalar((int)(a >> 32)) << 32) | (uint32_t)to_scalar((int)a);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to_scalar(lds_byte)), "v"(lane_bytes), "s"(base)
-                 : "memory");
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to_scalar(lds_byte)), "v"(lane_bytes), "s"(base)
+                     : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to_scalar(lds_byte)), "v"(lane_bytes), "s"(base)
+                     : "memory");
 }
 
 // One workgroup per (tile of 64 CB columns, kv head, share): the four waves take 16 CB columns each and share the keys and values,
-// which go through LDS SG groups at a time, the next stage under way while one is worked on.  The workgroups from n_tiles on serve the
+// which go through LDS, RING - 1 groups under way while one is worked on.  The workgroups from n_tiles on serve the
 // sequences of few columns (ROWS): in one launch they run beside the tiles and fill its tail.
 template <int NK, int CB, bool ROWS>
 __global__ void __launch_bounds__(256, 2)
 k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
-    constexpr int HD = 32 * NK, C = 64 * CB, SG = NK <= 4 ? 2 : 1, KIB = 4 * NK;   // KiB of a group
-    constexpr int STAGES = 2 * SG * KIB * 64, SUMS = ROWS ? (int)sizeof(RowsShared<NK>) / 16 : 0;
+    constexpr bool ONE_TILE = CB == 1 && NK <= 4;            // no sequence of the call has more columns (make_plan)
+    constexpr int HD = 32 * NK, C = 64 * CB, KIB = 4 * NK, RING = ONE_TILE ? 4 : 2;   // KiB of a group; groups in LDS
+    constexpr int STAGES = RING * KIB * 64, SUMS = ROWS ? (int)sizeof(RowsShared<NK>) / 16 : 0;
     __shared__ uint4 lds[STAGES > SUMS ? STAGES : SUMS];
     if constexpr (ROWS) {
         if (blockIdx.x >= n_tiles) {
@@ -344,46 +349,48 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
     const int min_lo = lowest_seen(w_first, a.window);
 
     const unsigned lane_bytes = (unsigned)lane * 16u, lds0 = (unsigned)(size_t)lds;
-    const int n = gb - ga, n_st = (n + SG - 1) / SG;
+    const int n = gb - ga;
     uint32_t now = NO_GROUP, then = NO_GROUP;                // pool groups of the 64 groups around the one at work, around the one asked for
     auto look_up = [&](int i) { return ga + i + lane < gb ? pool_group(a.pv, a.st, s, g, ga + i + lane) : NO_GROUP; };
-    // a wave sends SG NK of the SG 4 NK KiB of stage t; a group that is not there is replaced by the pool's first
-    auto issue = [&](int t) {
-        const int part = w * SG;
-        if (t > 0 && (SG * t & 63) == 0) {
-            then = look_up(SG * t);
-            asm volatile("" : "+v"(then));                   // arrived before the stage is under way
+    // A wave sends NK of the 4 NK KiB of group i into slot i % RING.  A group that is not there is replaced by the pool's first, one past
+    // the end by the last (nobody reads it: the number of loads under way stays the same up to the end).
+    auto issue = [&](int i) {
+        const int u = min(i, n - 1);
+        if (i > 0 && i < n && (i & 63) == 0) {
+            then = look_up(i);
+            asm volatile("" : "+v"(then));                   // arrived before the group is under way
         }
-        const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)then, (SG * t + part / 4) & 63);
-        const char* src = a.pv.pool + (at == NO_GROUP ? 0ull : (uint64_t)at * (HD * 128)) + part % 4 * NK * 1024;
-        const unsigned dst = lds0 + (unsigned)((t & 1) * SG * KIB + part * NK) * 1024u;
+        const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)then, u & 63);
+        const char* src = a.pv.pool + (at == NO_GROUP ? 0ull : (uint64_t)at * (HD * 128)) + w * NK * 1024;
+        const unsigned dst = lds0 + (unsigned)(i % RING * KIB + w * NK) * 1024u;
 #pragma unroll
-        for (int p = 0; p < SG * NK; ++p) load_kib(src + p * 1024, lane_bytes, dst + (unsigned)p * 1024u);
+        for (int p = 0; p < NK; ++p) load_kib<ONE_TILE>(src + p * 1024, lane_bytes, dst + (unsigned)p * 1024u);
     };
-    // this wave's part of a stage has landed and it has read the one before; after the barrier so has everybody's and everybody
-    auto meet = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    // This wave's part of the next group has landed (of RING - 1 groups under way, the RING - 2 later ones may still be) and it has read
+    // the one before; after the barrier so has everybody's and everybody.
+    auto meet = [] { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((RING - 2) * NK) : "memory"); };
     // Heads of up to 128 features: the next group's keys are read during the second product.  Wider ones do not have the registers: keys
     // and values are read in two halves each, when they are needed.
     constexpr bool AHEAD = NK <= 4;
     uint4 kf[AHEAD ? 2 * NK : 1];
-    auto group = [&](int i) { return lds + i % (2 * SG) * KIB * 64 + lane; };
+    auto group = [&](int i) { return lds + i % RING * KIB * 64 + lane; };
     auto load_keys = [&](int i) {
 #pragma unroll
         for (int f = 0; f < (AHEAD ? 2 * NK : 1); ++f) kf[f] = group(i)[f * 64];
     };
     if (n > 0) then = now = look_up(0);
     Columns<NK, CB> col;
-    col.start(a, g, cw, n_cols, first, sr.row0);             // the queries come in beside the page numbers and the first stage
-    if (n > 0) {
-        issue(0);
-        meet();
-    }
+    col.start(a, g, cw, n_cols, first, sr.row0);             // the queries come in beside the page numbers and the first group
+    if (n > 0) issue(0);
 #pragma unroll
-    for (int j = 0; j < CB; ++j)                             // in registers: a wait for them in the loop would wait for its stages
+    for (int j = 0; j < CB; ++j)                             // in registers: a wait for them in the loop would wait for its groups
 #pragma unroll
         for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(col.q[j][k].x), "+v"(col.q[j][k].y), "+v"(col.q[j][k].z), "+v"(col.q[j][k].w));
     if (n > 0) {
-        if (n_st > 1) issue(1);
+#pragma unroll
+        for (int i = 1; i < RING - 1; ++i) issue(i);
+        meet();
+        issue(RING - 1);
         if constexpr (AHEAD) load_keys(0);
     }
     // groups that every column of the tile sees whole: from a0 to a1 (the window starts before, the rows' own positions come after);
@@ -397,10 +404,10 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
                                (uint32_t)__builtin_amdgcn_readlane((int)now, i & 63) != NO_GROUP;
             uint4 P[CB];
             floatx4 S[CB][2];
-            auto next_stage = [&] {                          // after the last read of the stage
-                if (i + 1 < n && (i + 1) % SG == 0) {
+            auto next_group = [&] {                          // after the last read of this one
+                if (i + 1 < n) {
                     meet();
-                    if ((i + 1) / SG + 1 < n_st) issue((i + 1) / SG + 1);
+                    issue(i + RING);
                 }
             };
             if constexpr (AHEAD) {
@@ -413,7 +420,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
                     __builtin_amdgcn_sched_barrier(0);
                     col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
                 }
-                next_stage();
+                next_group();
                 if (i + 1 < n) {
                     __builtin_amdgcn_sched_barrier(0);
                     load_keys(i + 1);
@@ -447,7 +454,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
                     values(NK);
                     col.template weigh_group<edge.value, NK>(half, P, pg, min_lo, w_last, a.window);
                 }
-                next_stage();
+                next_group();
             }
         }
     };
@@ -457,6 +464,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
         if (part == 0) run(std::false_type{}, a0, a1);
     }
 
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // nothing may land in LDS that is no longer this workgroup's
     // A lane holds four neighbouring features of 2 NK blocks; two blocks at a time, lanes 16 apart swap halves, so that a lane has eight of
     // one block and a column's 64 bytes leave in one instruction.
     const bool last = n_shares == 1, wide = last && wide_q(a.out);
