@@ -539,7 +539,7 @@ int ee_rope_apply(const ee_rope* r, int dtype, const ee_heads* x, const ee_heads
  *              K[r][i] at ((((r/16)*(hd/32) + i/32) * 4 + (i%32)/8) * 16 + r%16) * 8 + i%8
  *              V[r][i] at 32*hd + (((i/16)*4 + (r%16)/4) * 16 + i%16) * 8 + (r/16)*4 + r%4
  *   (at head_dim 128 a group is one of ee_kv's, byte for byte).
- * page_size: a multiple of 32, up to 4096.  head_dim: EE_BF16 64, 96, 128, 192 or 256; EE_F32 a multiple of 4 up to 256. */
+ * page_size: a multiple of 32, up to 4096; fewer than 2^32 - 1 groups of 32 positions (of all kv heads) in a layer.  head_dim: EE_BF16 64, 96, 128, 192 or 256; EE_F32 a multiple of 4 up to 256. */
 typedef struct {
     int32_t n_layers;
     int32_t n_pages;     /* pages of every layer                                       */

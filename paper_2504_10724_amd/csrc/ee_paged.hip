@@ -294,6 +294,7 @@ int launch_paged_append(int dtype, const PagedView& pv, const StepView& st, cons
     const int most = (int)(((int64_t)st.max_q_len + 30) / 32 + 1);   // groups of 32 positions that max_q_len rows touch
     const int per_seq = most <= 2 ? most : 3;
     const int64_t units = per_seq <= 2 ? (int64_t)st.n_seqs * per_seq : (int64_t)st.n_tokens / 32 + 2LL * st.n_seqs;
+    if (units >= 1 << 24) return ee_fail(EE_ERR_SHAPE, "ee_paged_append: more workgroups than a launch holds");
     // A kv head a workgroup where sequences bring several rows (2091 rows of 64: 28 us, with two heads 39).  Single rows leave most of such
     // a workgroup idle: as many heads as keep four workgroups a CU (256 rows of 8 kv heads: one 9.6 us, two 7.7, eight 8.7).
     const int heads = st.max_q_len > 1 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(pv.n_kv_heads, units * pv.n_kv_heads / 1024));

@@ -45,6 +45,9 @@ static int check_paged(const ee_paged_config* c) {
     } else {
         return ee_fail(EE_ERR_DTYPE, "paged cache: unknown dtype");
     }
+    // the kernels number a layer's groups of 32 positions with 32 bits (a group takes 8 KiB at least in bf16, 1 KiB in fp32)
+    if ((double)c->n_pages * c->n_kv_heads * (c->page_size / 32) >= 4294967295.0)
+        return ee_fail(EE_ERR_SHAPE, "paged cache: more than 2^32 - 2 groups of 32 positions in a layer");
     size_t blocks, bytes;                              // a pool that no address space holds
     if (__builtin_mul_overflow((size_t)c->n_pages * c->n_kv_heads, (size_t)c->n_layers, &blocks) ||
         __builtin_mul_overflow(blocks, (size_t)8 * c->page_size * c->head_dim, &bytes))
@@ -66,6 +69,7 @@ static int check_step(const char* who, const ee_paged* p, int layer, const ee_pa
     if (st->n_tokens == 0) return EE_OK;
     if (st->n_seqs == 0 || st->max_q_len == 0) return fail(EE_ERR_INVALID_ARG, ": rows without a sequence to belong to");
     if (!st->dev_q_start || !st->dev_kv_len || !st->dev_pages) return fail(EE_ERR_INVALID_ARG, ": null pointer in the step");
+    if (st->max_kv_len > 1 << 30) return fail(EE_ERR_CAPACITY, ": more than 2^30 positions in a sequence");
     if (st->max_kv_len > (int64_t)st->pages_per_seq * p->cfg.page_size)
         return fail(EE_ERR_CAPACITY, ": max_kv_len exceeds what a row of the page table holds");
     return EE_OK;

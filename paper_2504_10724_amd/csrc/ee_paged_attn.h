@@ -37,6 +37,7 @@ struct AttnArgs {
     uint32_t flip, keep;           // what a negative scale puts into q (its signs), and a scale of zero leaves of it
     int   window;                  // 0: none
     int   rows_cols;
+    int   one_tile;                // no sequence has more columns than a tile: slot s of the tiles is sequence s
     Shares tiles, rows;
 };
 
@@ -208,10 +209,16 @@ template <class T> struct ColumnOut {
     }
 };
 
-// Tiles of C columns: sequence s has the slots from floor(q_start[s] G / C) + s on (see seq_of_slot).  By all lanes of a wave; sr is
+// Tiles of C columns: sequence s has the slots from floor(q_start[s] G / C) + s on (see seq_of_slot), or slot s if one tile holds any.  By all lanes of a wave; sr is
 // what seq_rows gives for the sequence, of up to 64 sequences from the loads that found it.
 struct Tile { int s, tile; };
-__device__ __forceinline__ Tile tile_of_slot(const StepView& st, int G, int C, int slot, SeqRows& sr) {
+__device__ __forceinline__ Tile tile_of_slot(const AttnArgs& args, int C, int slot, SeqRows& sr) {
+    const StepView& st = args.st;
+    const int G = args.G;
+    if (args.one_tile) {
+        sr = seq_rows(st, slot);
+        return Tile{slot, 0};
+    }
     const int lane = threadIdx.x & 63;
     auto base = [&](int start, int s) { return (int)((int64_t)min(max(start, 0), st.n_tokens) * G / C) + s; };
     if (st.n_seqs <= 64) {
@@ -234,7 +241,11 @@ __device__ __forceinline__ Tile tile_of_slot(const StepView& st, int G, int C, i
     return Tile{lo, slot - to_scalar(base(st.q_start[lo], lo))};
 }
 
-// Host side.  How to split the positions of `blocks` workgroups, of up to `groups` groups of 32: the workgroups after it are fewer than
+// Host side.  Slots of the tiles of C columns.
+static inline int64_t tile_slots(const AttnArgs& a, int C) {
+    return a.one_tile ? a.st.n_seqs : (int64_t)a.st.n_tokens * a.G / C + a.st.n_seqs;
+}
+// How to split the positions of `blocks` workgroups, of up to `groups` groups of 32: the workgroups after it are fewer than
 // SPLIT_TARGET + blocks, and nothing is split that has SPLIT_TARGET workgroups already or WHOLE_GROUPS groups at most.
 constexpr int SPLIT_TARGET = 512, WHOLE_GROUPS = 48;
 Split split_groups(int64_t blocks, int groups);
@@ -244,4 +255,6 @@ static inline size_t share_bytes(int hd) { return (size_t)hd * sizeof(float) + s
 
 int64_t f32_paged_columns(int hd, int64_t most_cols);       // of a workgroup
 int f32_paged_attention(AttnArgs a, char* ws, hipStream_t s);
+// a launch's workgroups times 256 threads stay below 2^32
+constexpr int64_t MOST_BLOCKS = 1 << 24;
 int launch_join(int dtype, const AttnArgs& a, int C, int64_t slots, hipStream_t s);

@@ -333,7 +333,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
     const int sx = x / a.pv.n_kv_heads, g = x - sx * a.pv.n_kv_heads;
     const int slot = n_slots - 1 - sx;                       // later rows see more positions: they start first
     SeqRows sr;
-    const Tile tl = tile_of_slot(a.st, a.G, C, slot, sr);
+    const Tile tl = tile_of_slot(a, C, slot, sr);
     const int s = tl.s, tile = tl.tile;
     const int n_cols = sr.n * a.G, c0 = tile * C;
     if (sr.n == 0 || n_cols <= a.rows_cols || tile < 0 || c0 >= n_cols) return;
@@ -517,7 +517,7 @@ k_paged_join(AttnArgs a, int C, int n_slots, int n_tiles, int cols) {
     const int slot = tiled ? n_slots - 1 - x : x, width = tiled ? C : a.rows_cols;
     Tile tl{x, 0};
     SeqRows sr;
-    if (tiled) tl = tile_of_slot(a.st, a.G, C, slot, sr);
+    if (tiled) tl = tile_of_slot(a, C, slot, sr);
     else sr = seq_rows(a.st, x);
     const int n_cols = sr.n * a.G, first = sr.len - sr.n, c0 = tl.tile * C, wave = to_scalar(threadIdx.x >> 6);
     if (sr.n == 0 || tl.tile < 0 || tiled != (n_cols > a.rows_cols) || c0 >= n_cols) return;
@@ -603,8 +603,10 @@ struct Plan {
     int64_t rows_blocks = 0, n_slots = 0;
     Split r, t;
 };
-Plan make_plan(int hd, int Hkv, int G, const StepView& st, int window) {
+Plan make_plan(AttnArgs& a) {
     Plan p;
+    const StepView& st = a.st;
+    const int G = a.G, hd = a.pv.hd, Hkv = a.pv.n_kv_heads, window = a.window;
     const int64_t most = (int64_t)st.max_q_len * G;
     if (most <= ROWS_MOST) {
         p.rows = true;
@@ -616,7 +618,8 @@ Plan make_plan(int hd, int Hkv, int G, const StepView& st, int window) {
         p.rows_cols = p.rows ? ROWS_MOST : 0;
         p.tile_cb = most <= 64 || hd > 128 ? 1 : 2;
         const int C = 64 * p.tile_cb;
-        p.n_slots = (int64_t)st.n_tokens * G / C + st.n_seqs;
+        a.one_tile = most <= C;
+        p.n_slots = tile_slots(a, C);
         p.t = split_groups(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window));
     }
     if (p.rows) {
@@ -665,6 +668,8 @@ static void launch_tile(const Plan& p, const AttnArgs& a, hipStream_t s) {
 template <int NK>
 static int run_bf16(const Plan& p, AttnArgs a, char* ws, hipStream_t s) {
     const int Hkv = a.pv.n_kv_heads, C = 64 * p.tile_cb;
+    if (p.n_slots * Hkv * p.t.shares + p.rows_blocks * p.r.shares >= MOST_BLOCKS)
+        return ee_fail(EE_ERR_SHAPE, "ee_paged_attention: more workgroups than a launch holds");
     a.rows_cols = p.rows_cols;
     if (p.tile) ws = a.tiles.place(p.t, ws, p.n_slots * Hkv * C, a.pv.hd);
     if (p.rows) a.rows.place(p.r, ws, p.rows_blocks * a.rows_cols, a.pv.hd);
@@ -689,7 +694,7 @@ int launch_paged_attention(int dtype, const PagedView& pv, const StepView& st, c
     a.keep = scale == 0.f ? 0u : 0xffffffffu;
     a.window = window;
     if (dtype != EE_BF16) return f32_paged_attention(a, ws, s);
-    const Plan p = make_plan(pv.hd, pv.n_kv_heads, a.G, st, window);
+    const Plan p = make_plan(a);
     switch (pv.hd) {
         case 64: return run_bf16<2>(p, a, ws, s);
         case 96: return run_bf16<3>(p, a, ws, s);

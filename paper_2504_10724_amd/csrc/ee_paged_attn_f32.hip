@@ -94,20 +94,18 @@ template <int HD, int CB> struct ColumnsF32 : ColumnState<HD / 16, CB> {
 };
 
 // One workgroup per (16 CB columns of a sequence, kv head, share of the positions); its waves take the share's groups in turn, from
-// memory into registers, and join their sums through LDS.  one_tile: no sequence has more columns, the slots are the sequences.
+// memory into registers, and join their sums through LDS.
 // WHOLE: the heads are HD wide, else less.
 template <int HD, int CB, bool WHOLE>
 __global__ void __launch_bounds__(256, HD <= 128 ? 2 : 1)
-k_f32_paged(AttnArgs a, int n_slots, int one_tile) {
+k_f32_paged(AttnArgs a, int n_slots) {
     constexpr int C = 16 * CB, NC = HD / 64;
     __shared__ float4 so[4][HD / 16][64];
     __shared__ float sm[4][C], sl[4][C];
     const int sx = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - sx * a.pv.n_kv_heads;
     const int slot = n_slots - 1 - sx;                       // later rows see more positions: they start first
-    Tile tl{slot, 0};
     SeqRows sr;
-    if (one_tile) sr = seq_rows(a.st, slot);
-    else tl = tile_of_slot(a.st, a.G, C, slot, sr);
+    const Tile tl = tile_of_slot(a, C, slot, sr);
     const int n_cols = sr.n * a.G, c0 = tl.tile * C, hd = WHOLE ? HD : a.pv.hd;
     if (sr.n == 0 || tl.tile < 0 || c0 >= n_cols) return;
     const int first = sr.len - sr.n, t0 = c0 / a.G, t1 = (min(c0 + C, n_cols) - 1) / a.G;
@@ -241,16 +239,18 @@ int64_t f32_paged_columns(int hd, int64_t most_cols) { return hd <= 64 && most_c
 int f32_paged_attention(AttnArgs a, char* ws, hipStream_t s) {
     const int hd = a.pv.hd, Hkv = a.pv.n_kv_heads;
     const int64_t most = (int64_t)a.st.max_q_len * a.G;
-    const int C = (int)f32_paged_columns(hd, most), cb = C / 16, one_tile = most <= C;
-    const int64_t slots = one_tile ? a.st.n_seqs : (int64_t)a.st.n_tokens * a.G / C + a.st.n_seqs;
+    const int C = (int)f32_paged_columns(hd, most), cb = C / 16;
+    a.one_tile = most <= C;
+    const int64_t slots = tile_slots(a, C);
     const Split sp = split_groups(slots * Hkv, groups_seen(a.st, (C + a.G - 1) / a.G + 1, a.window));
+    if (slots * Hkv * sp.shares >= MOST_BLOCKS) return ee_fail(EE_ERR_SHAPE, "ee_paged_attention: more workgroups than a launch holds");
     a.rows_cols = 0;                                         // all sequences are tiled
     a.tiles.place(sp, ws, slots * Hkv * C, hd);
     auto kern = hd == 64    ? (cb == 1 ? k_f32_paged<64, 1, true> : k_f32_paged<64, 2, true>)
                 : hd < 64   ? (cb == 1 ? k_f32_paged<64, 1, false> : k_f32_paged<64, 2, false>)
                 : hd <= 128 ? (hd == 128 ? k_f32_paged<128, 1, true> : k_f32_paged<128, 1, false>)
                             : (hd == 256 ? k_f32_paged<256, 1, true> : k_f32_paged<256, 1, false>);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(slots * Hkv), a.tiles.shares), dim3(256), 0, s, a, (int)slots, one_tile);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(slots * Hkv), a.tiles.shares), dim3(256), 0, s, a, (int)slots);
     EE_LAUNCH_CHECK();
     return launch_join(EE_F32, a, C, slots, s);
 }

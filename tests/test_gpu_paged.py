@@ -595,3 +595,29 @@ def test_rope_settings_keep_all_their_bits():
         want = R.rotate(x, pos, 64, "half", 1.07, theta=9999.7, scaling=scaling, factor=factor, trained_pos=4096, low=1.1, high=3.7)
         # an angle of up to 1.3e5 in fp64 (2^-36 off at most), a table entry, two products and a sum
         assert ((got - want).abs() <= 4 * U * 1.07 * 2 * x.abs().amax() + 2.0 ** -35 * 8).all(), scaling
+
+
+SPLITS = [
+    # dtype, hq, hkv, hd, page, window, (rows, positions) of each sequence: lengths that are split and ones that are not, more
+    # sequences than a tile has columns, tiles and single rows together
+    ("f32", 4, 1, 64, 64, 0, [(1, 1600 + 7 * s) for s in range(21)]),
+    ("f32", 2, 1, 84, 32, 0, [(3, 1700), (1, 40), (20, 1900), (1, 2200)]),
+    ("bf16", 4, 1, 64, 64, 0, [(1, 1600 + 7 * s) for s in range(21)]),
+    ("bf16", 4, 1, 64, 32, 0, [(9, 1700 + s) for s in range(9)]),              # 36 columns each: one tile a sequence
+    ("bf16", 3, 1, 96, 64, 0, [(50, 1800), (1, 1700), (1, 30), (60, 2100)]),
+    ("bf16", 4, 2, 128, 64, 1600, [(45, 2500), (1, 2400), (1, 1590)]),
+    ("bf16", 8, 1, 192, 64, 0, [(10, 1900), (1, 1700), (3, 100)]),
+]
+
+
+@pytest.mark.parametrize("case", SPLITS, ids=lambda c: "-".join(str(x) for x in c[:6]) + f"-{len(c[6])}seqs")
+def test_long_positions_in_shares(case):
+    """at most 48 groups of 32 positions are never split: these are longer"""
+    dtype, hq, hkv, hd, ps, window, seqs = case
+    print(f"[case] shares {case[:6]} {len(seqs)} sequences", flush=True)
+    b = Batch(seqs, hq, hkv, hd, ps, dtype)
+    x, q = b.fill(), b.queries()
+    assert ee.load().ee_paged_attention_workspace(b.kv.h, hq, C.byref(b.step.c)) > 0
+    got = b.check_attention(x, q, window=window)
+    ws = b.kv.workspace(b.step, hq).fill_(255)                         # whatever the workspace holds
+    assert torch.equal(P.attend(b.kv, 1, b.step, q.cuda(), window=window, workspace=ws), got)

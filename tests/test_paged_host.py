@@ -42,6 +42,7 @@ def _paged(**kw):
     (dict(head_dim=100), ee.EE_ERR_SHAPE), (dict(head_dim=288), ee.EE_ERR_SHAPE), (dict(dtype=5), ee.EE_ERR_DTYPE),
     (dict(dtype=ee.EE_F32, head_dim=6), ee.EE_ERR_SHAPE), (dict(dtype=ee.EE_F32, head_dim=260), ee.EE_ERR_SHAPE),
     (dict(n_layers=2 ** 31 - 1, n_pages=2 ** 31 - 1, n_kv_heads=65535), ee.EE_ERR_SHAPE),
+    (dict(n_layers=1, n_pages=2 ** 31 - 1, n_kv_heads=2, page_size=64), ee.EE_ERR_SHAPE),          # groups beyond 32 bits
 ])
 def test_paged_configurations(kw, code):
     lib, h = ee.load(), C.c_void_p()
@@ -78,7 +79,7 @@ def _step(**kw):
     (dict(n_seqs=-1), ee.EE_ERR_INVALID_ARG), (dict(n_tokens=-1), ee.EE_ERR_INVALID_ARG), (dict(max_kv_len=-1), ee.EE_ERR_INVALID_ARG),
     (dict(n_seqs=0), ee.EE_ERR_INVALID_ARG), (dict(max_q_len=0), ee.EE_ERR_INVALID_ARG), (dict(dev_pages=None), ee.EE_ERR_INVALID_ARG),
     (dict(dev_q_start=None), ee.EE_ERR_INVALID_ARG), (dict(dev_kv_len=None), ee.EE_ERR_INVALID_ARG),
-    (dict(max_kv_len=129), ee.EE_ERR_CAPACITY),
+    (dict(max_kv_len=129), ee.EE_ERR_CAPACITY), (dict(max_kv_len=2 ** 30 + 1, pages_per_seq=2 ** 30), ee.EE_ERR_CAPACITY),
 ])
 def test_steps(kw, code):
     lib, p = _bound()
