@@ -561,7 +561,7 @@ typedef struct {
     int32_t pages_per_seq;       /* width of the page table                                */
     const int32_t* dev_q_start;  /* [n_seqs + 1]                                           */
     const int32_t* dev_kv_len;   /* [n_seqs]                                               */
-    const int32_t* dev_pages;    /* [n_seqs][pages_per_seq]; entries no position needs are not read */
+    const int32_t* dev_pages;    /* [n_seqs][pages_per_seq]; entries no position needs mean nothing */
     int32_t* dev_status;         /* nullable; bits are set, never cleared:                 */
                                  /*   1 = a position without a page or outside the rotary table */
                                  /*   2 = a sequence outside the host's figures: none of its rows is served */

@@ -52,14 +52,20 @@ __device__ __forceinline__ int shares_of(int n_groups, int share) { return max(1
 // The pool's group (32 positions of one kv head) that holds positions 32 grp .. 32 grp + 31 of a sequence, NO_GROUP where the page
 // table names no page.  32 bits: groups are 8 KiB at least.
 constexpr uint32_t NO_GROUP = 0xffffffffu;
-__device__ __forceinline__ uint32_t pool_group(const PagedView& pv, const StepView& st, int s, int g, int grp) {
-    const int per = pv.page_size >> 5, i = grp / per;
-    const int page = st.pages[(int64_t)s * st.pages_per_seq + i];
+__device__ __forceinline__ int page_of_group(const PagedView& pv, const StepView& st, int s, int grp) {
+    const int i = grp / (pv.page_size >> 5);
+    return i < st.pages_per_seq ? st.pages[(int64_t)s * st.pages_per_seq + i] : -1;
+}
+__device__ __forceinline__ uint32_t group_of_page(const PagedView& pv, const StepView& st, int page, int g, int grp) {
+    const int per = pv.page_size >> 5;
     if (page < 0 || page >= pv.n_pages) {
         if (st.status) atomicOr(st.status, 1);
         return NO_GROUP;
     }
-    return ((uint32_t)page * pv.n_kv_heads + g) * per + (grp - i * per);
+    return ((uint32_t)page * pv.n_kv_heads + g) * per + grp % per;
+}
+__device__ __forceinline__ uint32_t pool_group(const PagedView& pv, const StepView& st, int s, int g, int grp) {
+    return group_of_page(pv, st, page_of_group(pv, st, s, grp), g, grp);
 }
 
 __device__ __forceinline__ int to_scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -246,9 +252,11 @@ static inline int64_t tile_slots(const AttnArgs& a, int C) {
     return a.one_tile ? a.st.n_seqs : (int64_t)a.st.n_tokens * a.G / C + a.st.n_seqs;
 }
 // How to split the positions of `blocks` workgroups, of up to `groups` groups of 32: the workgroups after it are fewer than
-// SPLIT_TARGET + blocks, and nothing is split that has SPLIT_TARGET workgroups already or WHOLE_GROUPS groups at most.
-constexpr int SPLIT_TARGET = 512, WHOLE_GROUPS = 48;
-Split split_groups(int64_t blocks, int groups);
+// SPLIT_TARGET + blocks, and nothing is split that has SPLIT_TARGET workgroups already or `whole` groups at most.
+constexpr int SPLIT_TARGET = 512;
+struct SplitRule { int whole, least; };                      // groups that are not worth a split; groups a share has at least
+constexpr SplitRule STREAMED{48, 16}, ONE_TILE_EACH{24, 8};
+Split split_groups(int64_t blocks, int groups, SplitRule rule);
 // groups of 32 positions that `rows` neighbouring rows see together at most
 int groups_seen(const StepView& st, int64_t rows, int window);
 static inline size_t share_bytes(int hd) { return (size_t)hd * sizeof(float) + sizeof(float2); }      // of a column

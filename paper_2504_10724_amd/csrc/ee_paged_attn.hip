@@ -185,6 +185,9 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
     constexpr int HD = 32 * NK, CB = 1, WAVES = 4;
     auto& [so, sm, sl] = sh;
     const int s = pair / a.pv.n_kv_heads, g = pair - s * a.pv.n_kv_heads;
+    const int lane = threadIdx.x & 63, n16 = lane & 15, w = to_scalar(threadIdx.x >> 6);
+    // without a window the share's first page numbers come in beside the sequence's lengths
+    const int early = a.window == 0 ? page_of_group(a.pv, a.st, s, share * a.rows.share + w + WAVES * lane) : 0;
     const SeqRows sr = seq_rows(a.st, s);
     const int n_cols = sr.n * a.G;
     if (sr.n == 0 || n_cols > a.rows_cols) return;
@@ -192,7 +195,6 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
     const GroupRange all = groups_of(min_lo, sr.len - 1);
     const int n_shares = shares_of(all.n, a.rows.share);
     if (share >= n_shares) return;
-    const int lane = threadIdx.x & 63, n16 = lane & 15, w = to_scalar(threadIdx.x >> 6);
     const int ga = all.g0 + share * a.rows.share, gb = min(ga + a.rows.share, all.g0 + all.n);
 
     const char* pool = a.pv.pool;
@@ -202,7 +204,12 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
         const int grp = ga + w + WAVES * (i + lane);
         return grp < gb ? pool_group(a.pv, a.st, s, g, grp) : NO_GROUP;
     };
-    if (n_mine > 0) now = then = look_up(0);
+    if (a.window != 0) {
+        if (n_mine > 0) now = look_up(0);
+    } else if (lane < n_mine) {
+        now = group_of_page(a.pv, a.st, early, g, ga + w + WAVES * lane);
+    }
+    then = now;
     Columns<NK, CB> col;
     col.start(a, g, 0, n_cols, first, sr.row0);
     // keys and values of a group each have registers of their own, which are asked for again as soon as a product has used them;
@@ -299,17 +306,24 @@ k_bf16_paged_rows(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------ sequences of many columns
-// 1 KiB (64 lanes x 16 bytes) from memory into LDS, past the registers; waited for with vmcnt by hand
-template <bool ONCE> __device__ __forceinline__ void load_kib(const char* src, unsigned lane_bytes, unsigned lds_byte) {
+// N x 1 KiB (64 lanes x 16 bytes) from memory into LDS, past the registers; waited for with vmcnt by hand.  An instruction's offset
+// counts in memory and in LDS, so up to four KiB take one address.  ONCE: past L2.
+#define EE_KIB_LOAD(OFFSET, HINT) "\n\tglobal_load_lds_dwordx4 %1, %2 " OFFSET HINT
+#define EE_KIB_LOADS(TEXT) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" TEXT ::"s"(slot), "v"(lane_bytes), "s"(base) : "memory")
+template <int N, bool ONCE> __device__ __forceinline__ void load_kib(const char* src, unsigned lane_bytes, unsigned lds_byte) {
+    static_assert(N >= 2 && N <= 4, "offsets have 12 bits");
     const uint64_t a = reinterpret_cast<uint64_t>(src);
     const uint64_t base = ((uint64_t)(uint32_t)to_scalar((int)(a >> 32)) << 32) | (uint32_t)to_scalar((int)a);
-    if constexpr (ONCE)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to_scalar(lds_byte)), "v"(lane_bytes), "s"(base)
-                     : "memory");
-    else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to_scalar(lds_byte)), "v"(lane_bytes), "s"(base)
-                     : "memory");
+    const int slot = to_scalar((int)lds_byte);
+    if constexpr (ONCE && N == 4) EE_KIB_LOADS(EE_KIB_LOAD("", "nt") EE_KIB_LOAD("offset:1024 ", "nt") EE_KIB_LOAD("offset:2048 ", "nt") EE_KIB_LOAD("offset:3072 ", "nt"));
+    else if constexpr (ONCE && N == 3) EE_KIB_LOADS(EE_KIB_LOAD("", "nt") EE_KIB_LOAD("offset:1024 ", "nt") EE_KIB_LOAD("offset:2048 ", "nt"));
+    else if constexpr (ONCE && N == 2) EE_KIB_LOADS(EE_KIB_LOAD("", "nt") EE_KIB_LOAD("offset:1024 ", "nt"));
+    else if constexpr (N == 4) EE_KIB_LOADS(EE_KIB_LOAD("", "") EE_KIB_LOAD("offset:1024 ", "") EE_KIB_LOAD("offset:2048 ", "") EE_KIB_LOAD("offset:3072 ", ""));
+    else if constexpr (N == 3) EE_KIB_LOADS(EE_KIB_LOAD("", "") EE_KIB_LOAD("offset:1024 ", "") EE_KIB_LOAD("offset:2048 ", ""));
+    else EE_KIB_LOADS(EE_KIB_LOAD("", "") EE_KIB_LOAD("offset:1024 ", ""));
 }
+#undef EE_KIB_LOADS
+#undef EE_KIB_LOAD
 
 // One workgroup per (tile of 64 CB columns, kv head, share): the four waves take 16 CB columns each and share the keys and values,
 // which go through LDS, RING - 1 groups under way while one is worked on.  The workgroups from n_tiles on serve the
@@ -363,8 +377,8 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
         const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)then, u & 63);
         const char* src = a.pv.pool + (at == NO_GROUP ? 0ull : (uint64_t)at * (HD * 128)) + w * NK * 1024;
         const unsigned dst = lds0 + (unsigned)(i % RING * KIB + w * NK) * 1024u;
-#pragma unroll
-        for (int p = 0; p < NK; ++p) load_kib<ONE_TILE>(src + p * 1024, lane_bytes, dst + (unsigned)p * 1024u);
+        load_kib<std::min(NK, 4), ONE_TILE>(src, lane_bytes, dst);
+        if constexpr (NK > 4) load_kib<NK - 4, ONE_TILE>(src + 4096, lane_bytes, dst + 4096u);
     };
     // This wave's part of the next group has landed (of RING - 1 groups under way, the RING - 2 later ones may still be) and it has read
     // the one before; after the barrier so has everybody's and everybody.
@@ -576,14 +590,17 @@ k_paged_join(AttnArgs a, int C, int n_slots, int n_tiles, int cols) {
 
 // ------------------------------------------------------------------ host side
 // Who serves what, and in how many shares.  From the host's figures alone: the device's are not known here.
-// The join of shares is a launch of its own and takes 4 to 5 us, what 48 groups take four waves: up to those nothing is split.  Beyond,
-// there should be two workgroups a CU, with 16 groups each at least.  Measured (us, one token a row): 16 rows of 512-2048 positions
-// (70B shape, 128 pairs of row and kv head) in shares of 8 groups 24.2, of 16 21.8; 64 rows (512 pairs) split 64.9, whole 56.7; one row of
-// 1000 positions split 10.2, whole 9.0; two rows of 20000 (4 pairs), shares of 8 groups 19.7, of 16 16.6.
-Split split_groups(int64_t blocks, int groups) {
-    if (groups <= WHOLE_GROUPS || blocks >= SPLIT_TARGET) return Split{std::max(groups, 1), 1};
+// The join of shares is a launch of its own and takes 4 to 5 us, what 48 groups take four waves that share them: up to those nothing is
+// split.  Beyond, there should be two workgroups a CU.  Measured (us, one token a row): 16 rows of 512-2048 positions (70B shape, 128
+// pairs of row and kv head) in shares of 8 groups 24.2, of 16 21.8; 64 rows (512 pairs) split 64.9, whole 56.7; one row of 1000 positions
+// split 10.2, whole 9.0; two rows of 20000 (4 pairs), shares of 8 groups 19.7, of 16 16.6.  Tiles of 128 columns pay more for the join
+// and gain from having a CU to themselves: two chunks of 600 rows (16 heads of 4 kv heads) split beyond 48 groups 39, beyond 24 47.
+// Where one tile holds any sequence, every wave works on every group and there are few columns to join: 8 rows of 2000 positions with
+// 20 heads of one kv head, shares of 16 groups beyond 48 groups 19.3, of 8 beyond 24 13.2.
+Split split_groups(int64_t blocks, int groups, SplitRule rule) {
+    if (groups <= rule.whole || blocks >= SPLIT_TARGET) return Split{std::max(groups, 1), 1};
     const int64_t want = (SPLIT_TARGET + blocks - 1) / blocks;
-    const int most = (int)std::min<int64_t>(want, groups / 16);
+    const int most = (int)std::min<int64_t>(want, groups / rule.least);
     const int share = (groups + most - 1) / most;
     return Split{share, (groups + share - 1) / share};
 }
@@ -620,11 +637,11 @@ Plan make_plan(AttnArgs& a) {
         const int C = 64 * p.tile_cb;
         a.one_tile = most <= C;
         p.n_slots = tile_slots(a, C);
-        p.t = split_groups(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window));
+        p.t = split_groups(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window), a.one_tile ? ONE_TILE_EACH : STREAMED);
     }
     if (p.rows) {
         p.rows_blocks = (int64_t)st.n_seqs * Hkv;
-        p.r = split_groups(p.rows_blocks, groups_seen(st, (p.rows_cols + G - 1) / G, window));
+        p.r = split_groups(p.rows_blocks, groups_seen(st, (p.rows_cols + G - 1) / G, window), STREAMED);
     }
     return p;
 }
@@ -633,9 +650,9 @@ Plan make_plan(AttnArgs& a) {
 // Split workgroups are fewer than target + blocks of fewer than target blocks, whatever the other figures are.
 size_t paged_attention_workspace(int dtype, int hd, int Hkv, int n_q_heads, const StepView& st) {
     const int64_t most = (int64_t)st.max_q_len * (n_q_heads / Hkv);
-    if ((st.max_kv_len + 31) / 32 <= WHOLE_GROUPS) return 0;
-    int64_t columns = f32_paged_columns(hd, most);
-    if (dtype == EE_BF16) columns = std::min<int64_t>(ROWS_MOST, most) + (most > ROWS_MOST ? TILE_MOST : 0);
+    const int groups = (st.max_kv_len + 31) / 32;
+    int64_t columns = groups > STREAMED.whole ? (dtype == EE_BF16 ? std::min<int64_t>(ROWS_MOST, most) : f32_paged_columns(hd, most)) : 0;
+    if (dtype == EE_BF16 && most > ROWS_MOST && groups > ONE_TILE_EACH.whole) columns += TILE_MOST;
     return (size_t)2 * SPLIT_TARGET * columns * share_bytes(hd);
 }
 

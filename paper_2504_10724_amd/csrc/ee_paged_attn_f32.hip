@@ -104,6 +104,7 @@ k_f32_paged(AttnArgs a, int n_slots) {
     __shared__ float sm[4][C], sl[4][C];
     const int sx = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - sx * a.pv.n_kv_heads;
     const int slot = n_slots - 1 - sx;                       // later rows see more positions: they start first
+    const int lane = threadIdx.x & 63, n16 = lane & 15, gq = lane >> 4, w = to_scalar(threadIdx.x >> 6);
     SeqRows sr;
     const Tile tl = tile_of_slot(a, C, slot, sr);
     const int n_cols = sr.n * a.G, c0 = tl.tile * C, hd = WHOLE ? HD : a.pv.hd;
@@ -113,7 +114,6 @@ k_f32_paged(AttnArgs a, int n_slots) {
     const GroupRange all = groups_of(min_lo, max_hi);
     const int n_shares = shares_of(all.n, a.tiles.share);
     if ((int)blockIdx.y >= n_shares) return;
-    const int lane = threadIdx.x & 63, n16 = lane & 15, gq = lane >> 4, w = to_scalar(threadIdx.x >> 6);
     const int ga = all.g0 + blockIdx.y * a.tiles.share, gb = min(ga + a.tiles.share, all.g0 + all.n);
 
     ColumnsF32<HD, CB> col;
@@ -242,7 +242,7 @@ int f32_paged_attention(AttnArgs a, char* ws, hipStream_t s) {
     const int C = (int)f32_paged_columns(hd, most), cb = C / 16;
     a.one_tile = most <= C;
     const int64_t slots = tile_slots(a, C);
-    const Split sp = split_groups(slots * Hkv, groups_seen(a.st, (C + a.G - 1) / a.G + 1, a.window));
+    const Split sp = split_groups(slots * Hkv, groups_seen(a.st, (C + a.G - 1) / a.G + 1, a.window), STREAMED);
     if (slots * Hkv * sp.shares >= MOST_BLOCKS) return ee_fail(EE_ERR_SHAPE, "ee_paged_attention: more workgroups than a launch holds");
     a.rows_cols = 0;                                         // all sequences are tiled
     a.tiles.place(sp, ws, slots * Hkv * C, hd);
