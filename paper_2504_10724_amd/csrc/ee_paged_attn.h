@@ -100,7 +100,7 @@ __device__ __forceinline__ uint32_t bit_mask(uint32_t bits, int i) { return (uin
 // positions 16 b + 4 gq + r.  NO sums of four features a lane and block, which the kernel's second product adds to.
 template <int NO, int CB> struct ColumnState {
     int   hi[CB];                  // the last position the lane's column sees (-1: none); the first is lowest_seen(hi, window)
-    float neg[CB], lim[CB], l[CB]; // minus the exponents' reference (log2 units); how far above it a score may lie (see softmax); the
+    float neg[CB], lim[CB], l[CB]; // minus the exponents' reference (log2 units); how far above it a score may lie (see exponents); the
                                    // lane's part of the sum
     uint32_t seen;                 // bit j: the column of block j has seen a position
     floatx4 O[CB][NO];
@@ -122,25 +122,18 @@ template <int NO, int CB> struct ColumnState {
 
     __device__ __forceinline__ float maximum(int j) const { return lim[j] == -INFINITY ? -INFINITY : -neg[j]; }
 
-    // Scores S[j][b][r] of positions pg + 16 b + 4 gq + r -> probabilities P[j][4 b + r]; EDGE: some column does not see all.
+    // Scores S[k][j][b][r] of positions 16 b + 4 gq + r of group k -> exponents x[k][j][4 b + r] of their probabilities.  EDGE: some column
+    // does not see all of the group, which starts at pg.
     // A column's reference is its largest score when it was last moved: it moves when a score exceeds it by more than lim = 8, or,
-    // while nothing but -inf has been seen (lim = -inf), when any does.  A lane looks at its own eight scores only; the four lanes
-    // of a column meet when one of the wave's references has to move.
-    template <bool EDGE> __device__ __forceinline__ void softmax(const floatx4 (&S)[CB][2], float (&P)[CB][8], float scale2, int pg, int window) {
-        float x[CB][8], top[CB];
+    // while nothing but -inf has been seen (lim = -inf), when any does.  A lane looks at its own scores only; the four lanes of a column
+    // meet when one of the wave's references has to move.  Then the exponents move by the same step: they cost a second rounding of
+    // relative 2^-24, and the scores need not stay in registers.
+    template <bool EDGE, int NG>
+    __device__ __forceinline__ void exponents(const floatx4 (&S)[NG][CB][2], float (&x)[NG][CB][8], float scale2, int pg, int window) {
+        static_assert(!EDGE || NG == 1, "groups that not all columns see come one by one");
+        float top[CB];
         uint32_t mine[CB];
         bool raise = false;
-        auto exponents = [&](int j) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[j][i] = fmaf(S[j][i >> 2][i & 3], scale2, neg[j]);
-            if constexpr (EDGE) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t keep = bit_mask(mine[j], i);
-                    x[j][i] = __uint_as_float((__float_as_uint(x[j][i]) & keep) | (0xff800000u & ~keep));
-                }
-            }
-        };
         if constexpr (EDGE) {
 #pragma unroll
             for (int j = 0; j < CB; ++j) {
@@ -153,11 +146,26 @@ template <int NO, int CB> struct ColumnState {
         }
 #pragma unroll
         for (int j = 0; j < CB; ++j) {
-            exponents(j);
-            top[j] = fmaxf(fmaxf(fmaxf(x[j][0], x[j][1]), fmaxf(x[j][2], x[j][3])), fmaxf(fmaxf(x[j][4], x[j][5]), fmaxf(x[j][6], x[j][7])));
+#pragma unroll
+            for (int k = 0; k < NG; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[k][j][i] = fmaf(S[k][j][i >> 2][i & 3], scale2, neg[j]);
+            if constexpr (EDGE) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t keep = bit_mask(mine[j], i);
+                    x[0][j][i] = __uint_as_float((__float_as_uint(x[0][j][i]) & keep) | (0xff800000u & ~keep));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < NG; ++k) {
+                const float (&y)[8] = x[k][j];
+                const float m = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
+                top[j] = k == 0 ? m : fmaxf(top[j], m);
+            }
             raise = raise || top[j] > lim[j];
         }
-        if (__any(raise)) {
+        if (__builtin_expect(__any(raise), 0)) {
 #pragma unroll
             for (int j = 0; j < CB; ++j) {
                 const float t = quad_max(top[j]);
@@ -171,9 +179,16 @@ template <int NO, int CB> struct ColumnState {
                 l[j] *= alpha;
 #pragma unroll
                 for (int hb = 0; hb < NO; ++hb) O[j][hb] = O[j][hb] * alpha;
-                exponents(j);
+#pragma unroll
+                for (int k = 0; k < NG; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[k][j][i] -= up ? t : 0.f;
             }
         }
+    }
+
+    // exponents of a group -> probabilities P[j][4 b + r], added to the lane's part of the sum
+    __device__ __forceinline__ void probabilities(const float (&x)[CB][8], float (&P)[CB][8]) {
 #pragma unroll
         for (int j = 0; j < CB; ++j) {
             float (&e)[8] = P[j];

@@ -67,12 +67,17 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
     }
 
     // the probabilities of a group as right operands
-    template <bool EDGE> __device__ __forceinline__ void weights(const floatx4 (&S)[CB][2], uint4 (&P)[CB], float scale2, int pg, int window) {
+    __device__ __forceinline__ void operands(const float (&x)[CB][8], uint4 (&P)[CB]) {
         float e[CB][8];
-        State::template softmax<EDGE>(S, e, scale2, pg, window);
+        State::probabilities(x, e);
 #pragma unroll
         for (int j = 0; j < CB; ++j)
             P[j] = make_uint4(bf16_pair(e[j][0], e[j][1]), bf16_pair(e[j][2], e[j][3]), bf16_pair(e[j][4], e[j][5]), bf16_pair(e[j][6], e[j][7]));
+    }
+    template <bool EDGE> __device__ __forceinline__ void weights(const floatx4 (&S)[1][CB][2], uint4 (&P)[CB], float scale2, int pg, int window) {
+        float x[1][CB][8];
+        State::template exponents<EDGE, 1>(S, x, scale2, pg, window);
+        operands(x[0], P);
     }
 
     // S^T += K Q^T of a group over N of the NK slices of 32 features, from K0 on: kf[b N + k] holds slice K0 + k of the 16 positions of half b
@@ -243,8 +248,8 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
             if (i + 1 < n_mine && ((i + 1) & 63) == 0) then = look_up(i + 1);
             const uint4* next = place(min(i + 1, n_mine - 1));
             uint4 P[CB];
-            floatx4 S[CB][2];
-            if (works) col.scores(kf, S);
+            floatx4 S[1][CB][2];
+            if (works) col.scores(kf, S[0]);
             __builtin_amdgcn_sched_barrier(0);
             if (i + 1 < n_mine) load_keys(next);
             __builtin_amdgcn_sched_barrier(0);
@@ -326,13 +331,20 @@ template <int N, bool ONCE> __device__ __forceinline__ void load_kib(const char*
 #undef EE_KIB_LOAD
 
 // One workgroup per (tile of 64 CB columns, kv head, share): the four waves take 16 CB columns each and share the keys and values,
-// which go through LDS, RING - 1 groups under way while one is worked on.  The workgroups from n_tiles on serve the
-// sequences of few columns (ROWS): in one launch they run beside the tiles and fill its tail.
+// which go through LDS in steps, one under way while one is worked on.  The workgroups from n_tiles on serve the sequences of few
+// columns (ROWS): in one launch they run beside the tiles and fill its tail.
+// Heads of up to 128 features take two groups a step: one test for a larger score and one barrier for 64 positions, and the second
+// group's exponentials lie among the first one's products.  Wider ones do not have the registers: one group a step.
+// Bound by the MFMAs at the clock that they leave the card: a group costs a wave 32 of them (512 cycles), 66 vector instructions (16 of
+// them exponentials, four times as long) and 16 reads of LDS; two waves a SIMD hide one's softmax behind the other's products.  Of a SIMD's
+// two waves the one with MFMAs goes first.  1023 rows after 30000 positions, 32 heads of 128 each with a kv head (0.51 TFLOP): 492 us with
+// the join, 1040 TFLOP/s, where a large matrix product reaches 1198; with one group a step 523, and 545 without the priorities.  Four
+// prompts of 1900-2048 rows, 64 heads of 8 kv heads (0.26 TFLOP): 332, with one group a step 368.
 template <int NK, int CB, bool ROWS>
 __global__ void __launch_bounds__(256, 2)
 k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
     constexpr bool ONE_TILE = CB == 1 && NK <= 4;            // no sequence of the call has more columns (make_plan)
-    constexpr int HD = 32 * NK, C = 64 * CB, KIB = 4 * NK, RING = ONE_TILE ? 4 : 2;   // KiB of a group; groups in LDS
+    constexpr int HD = 32 * NK, C = 64 * CB, KIB = 4 * NK, RING = NK <= 4 ? 4 : 2;    // KiB of a group; groups in LDS
     constexpr int STAGES = RING * KIB * 64, SUMS = ROWS ? (int)sizeof(RowsShared<NK>) / 16 : 0;
     __shared__ uint4 lds[STAGES > SUMS ? STAGES : SUMS];
     if constexpr (ROWS) {
@@ -366,7 +378,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
     const int n = gb - ga;
     uint32_t now = NO_GROUP, then = NO_GROUP;                // pool groups of the 64 groups around the one at work, around the one asked for
     auto look_up = [&](int i) { return ga + i + lane < gb ? pool_group(a.pv, a.st, s, g, ga + i + lane) : NO_GROUP; };
-    // A wave sends NK of the 4 NK KiB of group i into slot i % RING.  A group that is not there is replaced by the pool's first, one past
+    // A wave sends NK of the 4 NK KiB of group i into slot i mod RING.  A group that is not there is replaced by the pool's first, one past
     // the end by the last (nobody reads it: the number of loads under way stays the same up to the end).
     auto issue = [&](int i) {
         const int u = min(i, n - 1);
@@ -376,21 +388,23 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
         }
         const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)then, u & 63);
         const char* src = a.pv.pool + (at == NO_GROUP ? 0ull : (uint64_t)at * (HD * 128)) + w * NK * 1024;
-        const unsigned dst = lds0 + (unsigned)(i % RING * KIB + w * NK) * 1024u;
+        const unsigned dst = lds0 + (unsigned)((i & (RING - 1)) * KIB + w * NK) * 1024u;
         load_kib<std::min(NK, 4), ONE_TILE>(src, lane_bytes, dst);
         if constexpr (NK > 4) load_kib<NK - 4, ONE_TILE>(src + 4096, lane_bytes, dst + 4096u);
     };
-    // This wave's part of the next group has landed (of RING - 1 groups under way, the RING - 2 later ones may still be) and it has read
-    // the one before; after the barrier so has everybody's and everybody.
-    auto meet = [] { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((RING - 2) * NK) : "memory"); };
-    // Heads of up to 128 features: the next group's keys are read during the second product.  Wider ones do not have the registers: keys
-    // and values are read in two halves each, when they are needed.
-    constexpr bool AHEAD = NK <= 4;
-    uint4 kf[AHEAD ? 2 * NK : 1];
-    auto group = [&](int i) { return lds + i % RING * KIB * 64 + lane; };
-    auto load_keys = [&](int i) {
+    // This wave's part of what it has asked for, but `later` groups, has landed, and it has read what is replaced next; after the barrier
+    // so has everybody's and everybody.
+    auto meet = [](auto later) { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(later.value * NK) : "memory"); };
+    using std::integral_constant;
+    constexpr int STEP = NK <= 4 ? 2 : 1;                    // groups at a time
+    const int steps = (n + STEP - 1) / STEP;
+    auto group = [&](int i) { return lds + (i & (RING - 1)) * KIB * 64 + lane; };
+    auto next_step = [&](int u) {                            // after the last read of step u
+        if (u + 1 < steps) {
+            meet(integral_constant<int, 0>{});
 #pragma unroll
-        for (int f = 0; f < (AHEAD ? 2 * NK : 1); ++f) kf[f] = group(i)[f * 64];
+            for (int i = 0; i < STEP; ++i) issue((u + 2) * STEP + i);
+        }
     };
     if (n > 0) then = now = look_up(0);
     Columns<NK, CB> col;
@@ -402,86 +416,121 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
         for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(col.q[j][k].x), "+v"(col.q[j][k].y), "+v"(col.q[j][k].z), "+v"(col.q[j][k].w));
     if (n > 0) {
 #pragma unroll
-        for (int i = 1; i < RING - 1; ++i) issue(i);
-        meet();
-        issue(RING - 1);
-        if constexpr (AHEAD) load_keys(0);
+        for (int i = 1; i < 2 * STEP; ++i) issue(i);
+        meet(integral_constant<int, STEP>{});
     }
-    // groups that every column of the tile sees whole: from a0 to a1 (the window starts before, the rows' own positions come after);
-    // their loop tests nothing
-    const int a0 = min(max((lowest_seen(first + t1, a.window) + 31) / 32 - ga, 0), n), a1 = max(a0, min(((first + t0 + 1) >> 5) - ga, n));
-    auto run = [&](auto edge, int from, int to) {
-        for (int i = from; i < to; ++i) {
-            const int pg = (ga + i) << 5;
-            if ((i & 63) == 0 && i > 0) now = then;
-            const bool works = pg <= w_last && (!edge.value || pg + 31 >= min_lo) &&
-                               (uint32_t)__builtin_amdgcn_readlane((int)now, i & 63) != NO_GROUP;
-            uint4 P[CB];
-            floatx4 S[CB][2];
-            auto next_group = [&] {                          // after the last read of this one
-                if (i + 1 < n) {
-                    meet();
-                    issue(i + RING);
-                }
+    // Groups that every column of the wave sees whole: from a0 to a1 (the window starts before, the rows' own positions come after).  The
+    // loops over steps of such groups test nothing else; all waves make the same steps, whichever loop a wave makes them in.
+    const int a0 = min(max((lowest_seen(w_last, a.window) + 31) / 32 - ga, 0), n), a1 = w_last < 0 ? 0 : max(a0, min(((w_first + 1) >> 5) - ga, n));
+    auto there = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane((int)now, i & 63) != NO_GROUP; };
+    // one group; keys and values are read in two halves each, when they are needed
+    auto one_group = [&](auto edge, int i) {
+        const int pg = (ga + i) << 5;
+        if (edge.value && (i >= n || pg > w_last || pg + 31 < min_lo || !there(i))) return;
+        uint4 P[CB];
+        floatx4 S[1][CB][2];
+        constexpr int H = (NK + 1) / 2;                      // slices of 32 features in the first half
+        auto keys = [&](auto k0, auto& kf) {                 // slices from k0 on
+            constexpr int m = sizeof(kf) / sizeof(kf[0]) / 2;
+#pragma unroll
+            for (int f = 0; f < 2 * m; ++f) kf[f] = group(i)[(f / m * NK + k0.value + f % m) * 64];
+        };
+        uint4 ka[2 * H], kb[2 * (NK - H)];
+#pragma unroll
+        for (int j = 0; j < CB; ++j) S[0][j][0] = S[0][j][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+        keys(integral_constant<int, 0>{}, ka);
+        col.template add_scores<0, H>(ka, S[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        keys(integral_constant<int, H>{}, kb);
+        col.template add_scores<H, NK - H>(kb, S[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        uint4 vf[NK];
+        auto values = [&](int h0) {
+#pragma unroll
+            for (int f = 0; f < NK; ++f) vf[f] = group(i)[(2 * NK + h0 + f) * 64];
+        };
+        values(0);
+        col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
+        col.template weigh_group<edge.value, 0>(vf, P, pg, min_lo, w_last, a.window);
+        __builtin_amdgcn_sched_barrier(0);
+        values(NK);
+        col.template weigh_group<edge.value, NK>(vf, P, pg, min_lo, w_last, a.window);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto whole = [&](int u) {
+        bool all = u * STEP >= a0 && u * STEP + STEP <= a1;
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) all = all && there(u * STEP + i);
+        return all;
+    };
+    auto arrive = [&](int u) {
+        if (u > 0 && (u * STEP & 63) == 0) now = then;
+    };
+    int u = 0;
+    while (u < steps) {
+        if constexpr (STEP == 2) {
+            uint4 ka[2 * NK];
+            auto load_keys = [&](uint4 (&k)[2 * NK], int i, int from, int to) {        // slices from .. to - 1
+#pragma unroll
+                for (int f = 0; f < 2 * NK; ++f)
+                    if (f % NK >= from && f % NK < to) k[f] = group(i)[f * 64];
             };
-            if constexpr (AHEAD) {
-                uint4 vf[2 * NK];
-                if (works) {
-                    __builtin_amdgcn_s_setprio(1);           // of a SIMD's two waves the one with MFMAs goes first: 545 -> 531 us (below)
-                    col.scores(kf, S);
+            constexpr int H = NK / 2;
+            if (whole(u)) {
+                load_keys(ka, 2 * u, 0, H);
+                bool more = true;
+                do {
+                    uint4 kb[2 * NK], va[2 * NK], vb[2 * NK], P[2][CB];
+                    floatx4 S[2][CB][2];
+                    float x[2][CB][8];
+                    load_keys(ka, 2 * u, H, NK);             // the first half came during the second product: there are no registers for more
+                    load_keys(kb, 2 * u + 1, 0, NK);
+                    __builtin_amdgcn_s_setprio(1);
+                    col.scores(ka, S[0]);
+                    col.scores(kb, S[1]);
                     __builtin_amdgcn_s_setprio(0);
-                    __builtin_amdgcn_sched_barrier(0);       // the values are under way during the softmax
+                    __builtin_amdgcn_sched_barrier(0);       // values are under way during the softmax
 #pragma unroll
-                    for (int f = 0; f < 2 * NK; ++f) vf[f] = group(i)[(2 * NK + f) * 64];
+                    for (int f = 0; f < 2 * NK; ++f) va[f] = group(2 * u)[(2 * NK + f) * 64];
                     __builtin_amdgcn_sched_barrier(0);
-                    col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
-                }
-                next_group();
-                if (i + 1 < n) {
+                    col.template exponents<false, 2>(S, x, a.scale2, 0, a.window);
                     __builtin_amdgcn_sched_barrier(0);
-                    load_keys(i + 1);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                __builtin_amdgcn_s_setprio(1);
-                if (works) col.template weigh_group<edge.value>(vf, P, pg, min_lo, w_last, a.window);
-                __builtin_amdgcn_s_setprio(0);
-            } else {
-                if (works) {
-                    constexpr int H = NK / 2;
-                    uint4 half[2 * H];
-                    auto keys = [&](int k0) {
 #pragma unroll
-                        for (int f = 0; f < 2 * H; ++f) half[f] = group(i)[(f / H * NK + k0 + f % H) * 64];
-                    };
-                    auto values = [&](int h0) {
-#pragma unroll
-                        for (int f = 0; f < 2 * H; ++f) half[f] = group(i)[(2 * NK + h0 + f) * 64];
-                    };
-#pragma unroll
-                    for (int j = 0; j < CB; ++j) S[j][0] = S[j][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-                    keys(0);
-                    col.template add_scores<0, H>(half, S);
+                    for (int f = 0; f < 2 * NK; ++f) vb[f] = group(2 * u + 1)[(2 * NK + f) * 64];
                     __builtin_amdgcn_sched_barrier(0);
-                    keys(H);
-                    col.template add_scores<H, H>(half, S);
+                    col.operands(x[0], P[0]);
+                    next_step(u);
+                    ++u;
+                    arrive(u);
+                    more = u < steps && whole(u);
+                    __builtin_amdgcn_s_setprio(1);
                     __builtin_amdgcn_sched_barrier(0);
-                    values(0);
-                    col.template weights<edge.value>(S, P, a.scale2, pg, a.window);
-                    col.template weigh_group<edge.value, 0>(half, P, pg, min_lo, w_last, a.window);
+                    col.template weigh_group<false>(va, P[0], 0, 0, 0, 0);
+                    col.operands(x[1], P[1]);
                     __builtin_amdgcn_sched_barrier(0);
-                    values(NK);
-                    col.template weigh_group<edge.value, NK>(half, P, pg, min_lo, w_last, a.window);
-                }
-                next_group();
+                    if (more) load_keys(ka, 2 * u, 0, H);
+                    __builtin_amdgcn_sched_barrier(0);
+                    col.template weigh_group<false>(vb, P[1], 0, 0, 0, 0);
+                    __builtin_amdgcn_s_setprio(0);
+                } while (more);
+            }
+        } else {
+            while (u < steps && whole(u)) {
+                one_group(std::false_type{}, u);
+                next_step(u);
+                ++u;
+                arrive(u);
             }
         }
-    };
 #pragma unroll 1
-    for (int part = 0; part < 2; ++part) {
-        run(std::true_type{}, part == 0 ? 0 : a1, part == 0 ? a0 : n);
-        if (part == 0) run(std::false_type{}, a0, a1);
+        while (u < steps && !whole(u)) {
+#pragma unroll 1
+            for (int i = 0; i < STEP; ++i) one_group(std::true_type{}, u * STEP + i);
+            next_step(u);
+            ++u;
+            arrive(u);
+        }
     }
-
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // nothing may land in LDS that is no longer this workgroup's
     // A lane holds four neighbouring features of 2 NK blocks; two blocks at a time, lanes 16 apart swap halves, so that a lane has eight of
     // one block and a column's 64 bytes leave in one instruction.

@@ -152,7 +152,8 @@ k_f32_paged(AttnArgs a, int n_slots) {
             const float* kp = (const float*)a.pv.pool + (int64_t)blk * (2 * ps * hd) + (int64_t)(at - blk * per) * (32 * hd);
             const float* vp = kp + (int64_t)ps * hd;
             const int pg = (ga + w + 4 * i) << 5;
-            floatx4 S[CB][2];
+            floatx4 S1[1][CB][2];
+            floatx4 (&S)[CB][2] = S1[0];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 floatx4 kf[HD / 16];
@@ -174,8 +175,9 @@ k_f32_paged(AttnArgs a, int n_slots) {
 #pragma unroll
                 for (int c = 0; c < NC; ++c)
                     v[r][c] = features(vp + (16 * (r >> 2) + 4 * gq + (r & 3)) * hd, 64 * c + 4 * n16, hd);
-            float P[CB][8];
-            col.template softmax<edge.value>(S, P, a.scale2, pg, a.window);
+            float x[1][CB][8], P[CB][8];
+            col.template exponents<edge.value, 1>(S1, x, a.scale2, pg, a.window);
+            col.probabilities(x[0], P);
             if constexpr (edge.value) col.weigh_edge(v, P, hd, pg, min_lo, max_hi, a.window);
             else col.weigh(v, P, hd);
         }
