@@ -5,7 +5,8 @@
 #include <cmath>
 
 // ------------------------------------------------------------------ rotary table
-// frequencies in fp64 per entry: a set-up call, and the angle of a position of a long context keeps its bits
+// cos and sin of position * theta^(-2 i / rot), in fp64 per entry: a set-up call, and the angle of a position of a long context keeps its
+// bits.  Bound by pow, cos and sin: 19 us for 16384 positions of 64 pairs.
 __global__ void __launch_bounds__(256)
 k_rope_pairs(float2* __restrict__ table, int64_t n, int half, double theta, int scaling, double factor, double turns, double low,
              double high, double magnitude) {
@@ -80,15 +81,12 @@ template <int V> __device__ __forceinline__ Item<V> make_item(const RopeView& ro
 }
 
 // Rows past the caches (ONCE: read and written with nontemporal accesses) where a call moves more than they hold: 4097 rows of
-// 72 heads 33.0 -> 29.1 us, 2091 rows of an append 34.5 -> 27.9; of a call that fits (256 rows) 9.7 -> 10.8.
+// 72 heads 33 -> 29 us, 2091 rows of an append 34 -> 28; of a call that fits (256 rows) 9.7 -> 10.8.
 constexpr double CACHED_BYTES = 32e6;                        // eight L2 of 4 MB
-template <int V, bool ONCE, class T> __device__ __forceinline__ void read_row(const T* p, float (&x)[V]) {
-    if constexpr (ONCE && V > 1) {
-        const uint4 w = load_once(reinterpret_cast<const uint4*>(p));
-        load_row<V>(reinterpret_cast<const T*>(&w), x);
-    } else {
-        load_row<V>(p, x);
-    }
+template <int V, class T> struct alignas(V * sizeof(T)) Run { T x[V]; };
+template <int V, bool ONCE, class T> __device__ __forceinline__ Run<V, T> read_run(const T* p) {
+    if constexpr (ONCE && V > 1) return __builtin_bit_cast(Run<V, T>, load_once(reinterpret_cast<const uint4*>(p)));
+    else return *reinterpret_cast<const Run<V, T>*>(p);
 }
 template <int V, bool ONCE, class T> __device__ __forceinline__ void write_row(T* p, const float (&x)[V]) {
     if constexpr (ONCE && V > 1) {
@@ -101,14 +99,20 @@ template <int V, bool ONCE, class T> __device__ __forceinline__ void write_row(T
     }
 }
 
-// x: the head's row; put(first element, values) takes one or two runs of V elements
-template <int V, bool ONCE, class T, class Put>
-__device__ __forceinline__ void turn_item(const Item<V>& it, const T* x, Put put) {
+// An item of a head's row x as it is stored, and its rotation: put(first element, values) takes one or two runs of V elements
+template <int V, class T> struct Taken { Run<V, T> a, b; };
+template <int V, bool ONCE, class T> __device__ __forceinline__ Taken<V, T> take_item(const Item<V>& it, const T* x) {
+    Taken<V, T> v;
+    v.a = read_run<V, ONCE>(x + it.at);
+    if (it.partner >= 0) v.b = read_run<V, ONCE>(x + it.partner);
+    return v;
+}
+template <int V, class T, class Put> __device__ __forceinline__ void turn_item(const Item<V>& it, const Taken<V, T>& x, Put put) {
     float a[V];
-    read_row<V, ONCE>(x + it.at, a);
+    load_row<V>(x.a.x, a);
     if (it.partner >= 0) {
         float b[V];
-        read_row<V, ONCE>(x + it.partner, b);
+        load_row<V>(x.b.x, b);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float u = a[e], w = b[e];
@@ -141,7 +145,12 @@ static bool wide_rows(const HeadsView& h, int V) {
 }
 
 // ------------------------------------------------------------------ rotary positions
-// thread = (token, slice of the heads, item); consecutive threads take consecutive items, then heads n_slices apart
+// (a, b) -> (a cos - b sin, a sin + b cos) of each pair, in fp32, rounded once.  Bound by the bytes read and written, the cos and sin of a
+// position (8 bytes a pair) read once for every four heads.
+// thread = (token, slice of the heads, item); consecutive threads take consecutive items, then heads n_slices apart; four heads a thread, so
+// that their loads are under way together and a token still has threads enough where there are few.
+// 4097 rows of 72 heads of 128, bf16: 27.1 us, 5.6 TB/s (a large copy: 4.9); 1999 rows 14.2, 5.3; eight rows of 8 heads of 64, fp32: 5.8, a launch.
+constexpr int SLICE = 4;                                     // heads a thread serves
 template <class T, int V, bool ONCE>
 __global__ void __launch_bounds__(256)
 k_rope_apply(RopeView rope, int hd, HeadsView x, HeadsView y, const int32_t* __restrict__ pos, int n_tokens, int n_heads, int n_slices,
@@ -158,11 +167,17 @@ k_rope_apply(RopeView rope, int hd, HeadsView x, HeadsView y, const int32_t* __r
     const Item<V> it = make_item<V>(rope, p, u);
     const T* xr = (const T*)x.p + t * x.ts;
     T* yr = (T*)y.p + t * y.ts;
-#pragma unroll 4
-    for (int h = (int)(rest - t * n_slices); h < n_heads; h += n_slices) {
-        T* yh = yr + h * y.hs;
-        turn_item<V, ONCE>(it, xr + h * x.hs, [&](int at, const float (&v)[V]) { write_row<V, ONCE>(yh + at, v); });
-    }
+    const int h0 = (int)(rest - t * n_slices);
+    Taken<V, T> v[SLICE];                                    // x may be y, so that the compiler keeps the order: loads first (16.0 -> 14.2 us)
+#pragma unroll
+    for (int i = 0; i < SLICE; ++i)
+        if (h0 + i * n_slices < n_heads) v[i] = take_item<V, ONCE>(it, xr + (h0 + i * n_slices) * x.hs);
+#pragma unroll
+    for (int i = 0; i < SLICE; ++i)
+        if (h0 + i * n_slices < n_heads) {
+            T* yh = yr + (h0 + i * n_slices) * y.hs;
+            turn_item(it, v[i], [&](int at, const float (&w)[V]) { write_row<V, ONCE>(yh + at, w); });
+        }
 }
 
 int launch_rope_apply(int dtype, const RopeView& rope, int hd, const HeadsView& x, const HeadsView& y, const int32_t* pos, int n_tokens,
@@ -170,7 +185,7 @@ int launch_rope_apply(int dtype, const RopeView& rope, int hd, const HeadsView& 
     const int W = dtype == EE_BF16 ? 8 : 4;
     const bool wide = wide_rope(W, rope, hd) && wide_rows(x, W) && wide_rows(y, W);
     const int items = items_per_head(wide ? W : 1, hd, rope.rot, rope.interleaved);
-    const int n_slices = std::max(1, (n_heads + 3) / 4);
+    const int n_slices = (n_heads + SLICE - 1) / SLICE;
     const bool once = 32.0 / W * n_tokens * n_heads * hd > CACHED_BYTES;
     auto kern = dtype == EE_BF16 ? (!wide ? k_rope_apply<bf16_t, 1, false> : once ? k_rope_apply<bf16_t, 8, true> : k_rope_apply<bf16_t, 8, false>)
                                  : (!wide ? k_rope_apply<float, 1, false> : once ? k_rope_apply<float, 4, true> : k_rope_apply<float, 4, false>);
@@ -195,8 +210,16 @@ int launch_rope_apply(int dtype, const RopeView& rope, int hd, const HeadsView& 
 // Keys and queries: thread = (item of a head, row, first head); it keeps the row's cos and sin over its heads.  A wave's 16-byte
 // items of eight rows fill whole 128-byte lines of the keys' order.  Values (bf16): 16 bytes of a group hold eight positions of
 // one feature, so a thread reads two features of eight rows and writes 32 bytes; positions that are not new keep their bytes.
+//
+// Bound by the bytes of the rows and their places, few rows by the launch; between by a chain of trips to memory (the sequence, its
+// figures and page, the rows, their stores), about 7 us with the launch.  8000 rows in 4 chunks (64 heads, 8 kv heads of 128): 64 us, 5.1
+// TB/s; 2091 rows in 7 chunks and 57 single rows 25.4, 3.4 TB/s; 256 single rows 7.3; one row of 32 heads 6.1.
+// Two heads' loads come before the first one's stores (q may be q_out, so that the compiler keeps the order), and the values' before both:
+// the 8000 rows 74 -> 67.  At most four workgroups a CU: the work of a call of this middle size spreads more evenly (the 2091 rows
+// 28.3 -> 25.4, with three 27.1; 8000 rows 67 -> 64, with three 69; single rows are the same).
+constexpr int AHEAD = 2;
 template <class T, int V, bool ONCE>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4)))
 k_paged_append(PagedView pv, StepView st, RopeView rope, HeadsView k, HeadsView v, HeadsView q, HeadsView qo, int G, int heads, int per_seq) {
     const int s = per_seq <= 2 ? (int)blockIdx.x / per_seq : seq_of_slot(st, blockIdx.x, 32, 2);
     const SeqRows sr = seq_rows(st, s);
@@ -215,6 +238,24 @@ k_paged_append(PagedView pv, StepView st, RopeView rope, HeadsView k, HeadsView 
     const int64_t block = 2LL * ps * hd;
     T* pool = (T*)pv.pool + ((int64_t)page * pv.n_kv_heads + g0) * block;
 
+    // Values, bf16: quads of positions 4 d + i and 16 + 4 d + i (a single row is in one of them) of features 2 f and 2 f + 1.  A single row
+    // leaves threads without keys or queries: they start here.  A thread's first ones are under way beside the keys and queries.
+    const int back = 255 - (int)threadIdx.x, d0 = nr == 1 ? (r0 & 15) >> 2 : 0, nd = nr == 1 ? 1 : 4, pairs = hd / 2, n_v = ng * nd * pairs;
+    auto place_v = [&](int i, int& f, int& d, int& g) { f = i % pairs; const int rest = i / pairs; d = d0 + rest % nd; g = rest / nd; };
+    auto load_v = [&](int i, uint32_t (&w)[8]) {
+        int f, d, g;
+        place_v(i, f, d, g);
+        const bf16_t* src = (const bf16_t*)v.p + (g0 + g) * v.hs + 2 * f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int r = 4 * d + 16 * (e >> 2) + (e & 3);
+            w[e] = r >= r0 && r < r1 ? *reinterpret_cast<const uint32_t*>(src + (row0 + r) * v.ts) : 0u;
+        }
+    };
+    uint32_t w[8];
+    if constexpr (sizeof(T) == 2 && V > 1)
+        if (back < n_v) load_v(back, w);
+
     const bool mapped = page >= 0 && page < pv.n_pages;      // looked at when the rows are there: the page comes in beside them
     const int items = items_per_head(V, hd, rope.rot, rope.interleaved), nh = ng * (G + 1);
     const int slots = 256 / items, slot = (int)threadIdx.x / items, u = (int)threadIdx.x - slot * items;    // items <= hd <= 256
@@ -223,38 +264,41 @@ k_paged_append(PagedView pv, StepView st, RopeView rope, HeadsView k, HeadsView 
         for (int r = r0 + slot % rows; r < r1; r += rows) {
             const Item<V> it = make_item<V>(rope, p0 + r, u);
             const int64_t t = row0 + r;
-#pragma unroll 4
-            for (int h = slot / rows; h < nh; h += steps) {
-                if (h < nh - ng) {
-                    const int hq = g0 * G + h;
-                    T* dst = (T*)qo.p + t * qo.ts + hq * qo.hs;
-                    turn_item<V, ONCE>(it, (const T*)q.p + t * q.ts + hq * q.hs, [&](int at, const float (&x)[V]) { write_row<V, ONCE>(dst + at, x); });
-                } else {
-                    const int g = h - (nh - ng);
-                    T* dst = pool + g * block;
-                    turn_item<V, ONCE>(it, (const T*)k.p + t * k.ts + (g0 + g) * k.hs, [&](int at, const float (&x)[V]) {
-                        if (mapped) store_row<V>(dst + page_k<T>(at0 + r, at, hd, ps), x);
-                    });
+            for (int h0 = slot / rows; h0 < nh; h0 += AHEAD * steps) {
+                Taken<V, T> x[AHEAD];                        // loads, then stores
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int h = h0 + i * steps;
+                    if (h < nh) x[i] = take_item<V, ONCE>(it, h < nh - ng ? (const T*)q.p + t * q.ts + (g0 * G + h) * q.hs
+                                                                          : (const T*)k.p + t * k.ts + (g0 + h - (nh - ng)) * k.hs);
+                }
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int h = h0 + i * steps;
+                    if (h < nh - ng) {
+                        T* dst = (T*)qo.p + t * qo.ts + (g0 * G + h) * qo.hs;
+                        turn_item(it, x[i], [&](int at, const float (&w)[V]) { write_row<V, ONCE>(dst + at, w); });
+                    } else if (h < nh) {
+                        T* dst = pool + (h - (nh - ng)) * block;
+                        turn_item(it, x[i], [&](int at, const float (&w)[V]) {
+                            if (mapped) store_row<V>(dst + page_k<T>(at0 + r, at, hd, ps), w);
+                        });
+                    }
                 }
             }
         }
     }
 
-    const int back = 255 - (int)threadIdx.x;                 // a single row leaves threads without keys or queries: they start here
     if constexpr (sizeof(T) == 2 && V > 1) {
-        // quads of positions 4 d + i and 16 + 4 d + i; a single row is in one of them
-        const int d0 = nr == 1 ? (r0 & 15) >> 2 : 0, nd = nr == 1 ? 1 : 4, pairs = hd / 2;
-        for (int i = back; i < ng * nd * pairs; i += 256) {
-            const int f = i % pairs, rest = i / pairs, d = d0 + rest % nd, g = rest / nd;
-            const bf16_t* src = (const bf16_t*)v.p + (g0 + g) * v.hs + 2 * f;
-            uint32_t w[8];
+        for (int i = back; i < n_v; i += 256) {
+            int f, d, g;
+            place_v(i, f, d, g);
+            if (i != back) load_v(i, w);
             bool all = true;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int r = 4 * d + 16 * (e >> 2) + (e & 3);
-                const bool in = r >= r0 && r < r1;
-                all = all && in;
-                w[e] = in ? *reinterpret_cast<const uint32_t*>(src + (row0 + r) * v.ts) : 0u;
+                all = all && r >= r0 && r < r1;
             }
             bf16_t* dst = (bf16_t*)pool + g * block + page_v<bf16_t>(at0 + 4 * d, 2 * f, hd, ps);
             if (!mapped) continue;

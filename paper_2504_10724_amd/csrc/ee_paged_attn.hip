@@ -180,7 +180,8 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
 // ------------------------------------------------------------------ sequences of few columns
 // One workgroup per (sequence, kv head, share of the positions); its four waves take the share's groups in turn, straight from
 // memory into registers, and join their sums through LDS at the end.  Bound by the cache's bytes.  They are read past L2 (each once;
-// nontemporal): 256 rows over 512-2048 positions (70B shape) 241 -> 214 us (6.2 TB/s), one row over 32768 (7B shape) 102 -> 88 us.
+// nontemporal): 256 rows over 512-2048 positions (64 heads, 8 kv heads) 241 -> 214 us, 6.2 TB/s; one row over 32767 (32 heads, as many kv
+// heads) 102 -> 87 us with the join, 6.2 TB/s.
 template <int NK> struct RowsShared {
     float4 so[4][2 * NK][64];
     float  sm[4][16], sl[4][16];
@@ -568,7 +569,8 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
 // ------------------------------------------------------------------ join of the shares
 // A wave per column and `cols` columns a wave: the shares' maxima and sums, a share a lane, then their weighted sums in share order
 // (the same bits every time), the two halves of the wave a share each where a half holds the features.  The sums of the first shares
-// are asked for beside the statistics.  blockIdx.x < n_tiles: (slot, kv head) of the tiles of C columns; then (sequence, kv head) of the
+// are asked for beside the statistics.  Bound by the launch where there are few columns (32 columns of 16 shares 4.7 us), else by the
+// sums' bytes: 32736 columns of two shares 20 us.  blockIdx.x < n_tiles: (slot, kv head) of the tiles of C columns; then (sequence, kv head) of the
 // sequences of few columns.
 template <class T>
 __global__ void __launch_bounds__(256)
