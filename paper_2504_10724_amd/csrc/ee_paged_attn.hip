@@ -19,19 +19,6 @@ __device__ __forceinline__ floatx4 mfma(uint4 a, uint4 b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
 
-// 8 consecutive features of a row of heads, whatever its alignment
-__device__ __forceinline__ uint4 load_q8(const bf16_t* p, bool wide, uint32_t keep, uint32_t flip) {
-    uint4 v;
-    if (wide) {
-        v = *reinterpret_cast<const uint4*>(p);
-    } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)p[2 * i] | ((uint32_t)p[2 * i + 1] << 16);
-        v = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    return make_uint4((v.x & keep) ^ flip, (v.y & keep) ^ flip, (v.z & keep) ^ flip, (v.w & keep) ^ flip);
-}
 __device__ __forceinline__ bool wide_q(const HeadsView& h) { return (uintptr_t)h.p % 16 == 0 && h.ts % 8 == 0 && h.hs % 8 == 0; }
 
 // the lane's eight positions as masks of the halves of an operand's four words
@@ -54,15 +41,40 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
     // columns c0 .. of the n_cols of a sequence whose first row is row0, at position first
     __device__ __forceinline__ void start(const AttnArgs& a, int g, int c0, int n_cols, int first, int row0) {
         const int lane = threadIdx.x & 63, n16 = lane & 15, gq = lane >> 4;
-        const bool wide = wide_q(a.q);
         State::begin(a, c0, n_cols, first);
+        const bf16_t* p[CB];
 #pragma unroll
         for (int j = 0; j < CB; ++j) {
-            const int c = c0 + 16 * j + n16, t = c / a.G;
-            const bool live = c < n_cols;
-            const bf16_t* p = (const bf16_t*)a.q.p + (int64_t)(row0 + t) * a.q.ts + (int64_t)(g * a.G + c - t * a.G) * a.q.hs + 8 * gq;
+            const int c = min(c0 + 16 * j + n16, n_cols - 1), t = c / a.G;   // past the end: the last column's, until settle
+            p[j] = (const bf16_t*)a.q.p + (int64_t)(row0 + t) * a.q.ts + (int64_t)(g * a.G + c - t * a.G) * a.q.hs + 8 * gq;
+        }
+        if (wide_q(a.q)) {                                   // all loads in one block: they are under way together
 #pragma unroll
-            for (int k = 0; k < NK; ++k) q[j][k] = live ? load_q8(p + 32 * k, wide, a.keep, a.flip) : make_uint4(0, 0, 0, 0);
+            for (int j = 0; j < CB; ++j)
+#pragma unroll
+                for (int k = 0; k < NK; ++k) q[j][k] = *reinterpret_cast<const uint4*>(p[j] + 32 * k);
+        } else {
+#pragma unroll
+            for (int j = 0; j < CB; ++j)
+#pragma unroll
+                for (int k = 0; k < NK; ++k) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)p[j][32 * k + 2 * i] | ((uint32_t)p[j][32 * k + 2 * i + 1] << 16);
+                    q[j][k] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+        }
+    }
+    // the queries have arrived: the sign or zero of the scale goes in, columns past the end come to zero
+    __device__ __forceinline__ void settle(const AttnArgs& a) {
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+            const uint32_t keep = hi[j] >= 0 ? a.keep : 0u, flip = hi[j] >= 0 ? a.flip : 0u;
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                uint4& v = q[j][k];
+                v = make_uint4((v.x & keep) ^ flip, (v.y & keep) ^ flip, (v.z & keep) ^ flip, (v.w & keep) ^ flip);
+            }
         }
     }
 
@@ -237,6 +249,7 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
         load_keys(place(0));
         load_values(place(0));
     }
+    col.settle(a);
     // whether a column does not see all of a group is settled by range, so the loop over the groups that all see has no test:
     // edge before a0 (the window's start) and from a1 on (the rows' own positions)
     auto mine_from = [&](int grp) { return min(max((grp - ga - w + WAVES - 1) / WAVES, 0), n_mine); };
@@ -411,6 +424,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
     Columns<NK, CB> col;
     col.start(a, g, cw, n_cols, first, sr.row0);             // the queries come in beside the page numbers and the first group
     if (n > 0) issue(0);
+    col.settle(a);
 #pragma unroll
     for (int j = 0; j < CB; ++j)                             // in registers: a wait for them in the loop would wait for its groups
 #pragma unroll

@@ -11,10 +11,6 @@
 
 __device__ __forceinline__ floatx4 mfma(float a, float b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-__device__ __forceinline__ float4 load4(const float* p, bool wide) {
-    return wide ? *reinterpret_cast<const float4*>(p) : make_float4(p[0], p[1], p[2], p[3]);
-}
-
 // features f .. f + 3 of a cached row, zeros beyond its hd (a load and selects, no branch)
 __device__ __forceinline__ floatx4 features(const float* row, int f, int hd) {
     const bool in = f < hd;
@@ -122,19 +118,34 @@ k_f32_paged(AttnArgs a, int n_slots) {
     ColumnsF32<HD, CB> col;
     col.begin(a, c0, n_cols, first);
     floatx4 q[CB][HD / 16];                                  // features 16 k + 4 gq + e
-    const bool wide = (uintptr_t)a.q.p % 16 == 0 && a.q.ts % 4 == 0 && a.q.hs % 4 == 0;
+    const float* p[CB];                                      // past the end: the last column's
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
-        const int c = c0 + 16 * j + n16, t = c / a.G;
-        const float* p = (const float*)a.q.p + (int64_t)(sr.row0 + t) * a.q.ts + (int64_t)(g * a.G + c - t * a.G) * a.q.hs + 4 * gq;
+        const int c = min(c0 + 16 * j + n16, n_cols - 1), t = c / a.G;
+        p[j] = (const float*)a.q.p + (int64_t)(sr.row0 + t) * a.q.ts + (int64_t)(g * a.G + c - t * a.G) * a.q.hs;
+    }
+    auto feature = [&](int k) { return WHOLE ? 16 * k + 4 * gq : min(16 * k + 4 * gq, hd - 4); };
+    if ((uintptr_t)a.q.p % 16 == 0 && a.q.ts % 4 == 0 && a.q.hs % 4 == 0) {     // all loads in one block: they are under way together
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int k = 0; k < HD / 16; ++k) q[j][k] = *reinterpret_cast<const floatx4*>(p[j] + feature(k));
+    } else {
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int k = 0; k < HD / 16; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) q[j][k][e] = p[j][feature(k) + e];
+    }
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k) {
-            const float4 x = c < n_cols && 16 * k + 4 * gq < hd ? load4(p + 16 * k, wide) : make_float4(0.f, 0.f, 0.f, 0.f);
-            const float y[4] = {x.x, x.y, x.z, x.w};
+            const uint32_t keep = col.hi[j] >= 0 && (WHOLE || 16 * k + 4 * gq < hd) ? a.keep : 0u, flip = a.flip & 0x80000000u;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) q[j][k][e] = __uint_as_float((__float_as_uint(y[e]) & a.keep) ^ (a.flip & 0x80000000u));
+            for (int e = 0; e < 4; ++e) q[j][k][e] = __uint_as_float((__float_as_uint(q[j][k][e]) & keep) ^ flip);
         }
-    }
 
     const int ps = a.pv.page_size, per = ps >> 5;
     const int n_mine = max(0, (gb - ga - w + 3) >> 2);       // this wave's groups: ga + w, ga + w + 4, ..
