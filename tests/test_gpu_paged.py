@@ -621,3 +621,47 @@ def test_long_positions_in_shares(case):
     got = b.check_attention(x, q, window=window)
     ws = b.kv.workspace(b.step, hq).fill_(255)                         # whatever the workspace holds
     assert torch.equal(P.attend(b.kv, 1, b.step, q.cuda(), window=window, workspace=ws), got)
+
+
+STEPS = [
+    # heads of one and of two groups a step; windows that start in the first and in the second of two groups; lengths of an odd number of groups
+    (128, 8, 2, 0, [(130, 607), (70, 70), (33, 993)]),
+    (128, 4, 4, 301, [(140, 500), (65, 1300)]),
+    (64, 6, 2, 333, [(90, 675), (64, 96)]),
+    (96, 20, 1, 0, [(7, 650), (40, 161)]),
+    (256, 4, 1, 270, [(50, 390), (17, 608)]),
+]
+
+
+@pytest.mark.parametrize("case", STEPS, ids=lambda c: "-".join(str(x) for x in c[:4]))
+def test_tiles_whose_scores_rise_with_the_position(case):
+    """the reference of the exponents moves many times, in groups that all columns see and in others; pages of one group are missing here
+    and there"""
+    hd, hq, hkv, window, seqs = case
+    print(f"[case] rising {case}", flush=True)
+    for drop in ((), [(0, 3, -1), (0, 8, -1), (0, 9, 1 << 20), (1, 1, -1)]):
+        b = Batch(seqs, hq, hkv, hd, 32, "bf16", drop=drop)
+        x, q = b.fill(), b.queries()
+        for (n, length), table in zip(b.seqs, b.pages):
+            for i, page in enumerate(table):
+                if 0 <= page < b.n_pages:
+                    x[0, 0, page] *= 0.5 + 0.75 * i                    # scores of a few at first, of a hundred at the end
+        b.put(x)
+        b.check_attention(x, q, window=window)
+        assert b.status.item() == (1 if drop else 0)
+
+
+@pytest.mark.parametrize("hd", [64, 128, 192])
+def test_tiles_that_begin_with_scores_of_minus_infinity(hd):
+    """positions whose score is -inf weigh nothing, also where nothing else has been seen yet: as if their pages were not there"""
+    print(f"[case] -inf first {hd}", flush=True)
+    seqs, low = [(100, 500)], 5
+    b = Batch(seqs, 4, 2, hd, 32, "bf16")
+    x, q = b.fill(), b.queries().abs()
+    y = x.clone()
+    for page in b.pages[0][:low]:
+        y[0, 0, page] = torch.finfo(b.dt).min
+    b.put(y)
+    got = P.attend(b.kv, 1, b.step, q.cuda())
+    gone = Batch(seqs, 4, 2, hd, 32, "bf16", drop=[(0, i, -1) for i in range(low)])
+    gone.check_attention(x, q, got=got)
