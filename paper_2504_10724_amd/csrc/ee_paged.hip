@@ -339,8 +339,9 @@ int launch_paged_append(int dtype, const PagedView& pv, const StepView& st, cons
     const int per_seq = most <= 2 ? most : 3;
     const int64_t units = per_seq <= 2 ? (int64_t)st.n_seqs * per_seq : (int64_t)st.n_tokens / 32 + 2LL * st.n_seqs;
     if (units >= 1 << 24) return ee_fail(EE_ERR_SHAPE, "ee_paged_append: more workgroups than a launch holds");
-    // A kv head a workgroup where sequences bring several rows (2091 rows of 64: 28 us, with two heads 39).  Single rows leave most of such
-    // a workgroup idle: as many heads as keep four workgroups a CU (256 rows of 8 kv heads: one 9.6 us, two 7.7, eight 8.7).
+    // A kv head a workgroup where sequences bring several rows (2091 rows of 64 heads, 8 kv heads: 25.5 us, with two 31; four times 500 rows of 32
+    // heads, as many kv heads: 23.3, with two 23.0, with four 26.8).  Single rows leave most of such a workgroup idle: as many heads as keep
+    // four workgroups a CU (256 rows of 64 heads, 8 kv heads: one 9.5 us, two 7.5, eight 7.7).
     const int heads = st.max_q_len > 1 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(pv.n_kv_heads, units * pv.n_kv_heads / 1024));
     const dim3 grid((unsigned)units, (unsigned)((pv.n_kv_heads + heads - 1) / heads));
     const bool once = 32.0 / W * st.n_tokens * (n_q_heads + 2.0 * pv.n_kv_heads) * pv.hd > CACHED_BYTES;

@@ -349,11 +349,11 @@ template <int N, bool ONCE> __device__ __forceinline__ void load_kib(const char*
 // columns (ROWS): in one launch they run beside the tiles and fill its tail.
 // Heads of up to 128 features take two groups a step: one test for a larger score and one barrier for 64 positions, and the second
 // group's exponentials lie among the first one's products.  Wider ones do not have the registers: one group a step.
-// Bound by the MFMAs at the clock that they leave the card: a group costs a wave 32 of them (512 cycles), 66 vector instructions (16 of
-// them exponentials, four times as long) and 16 reads of LDS; two waves a SIMD hide one's softmax behind the other's products.  Of a SIMD's
-// two waves the one with MFMAs goes first.  1023 rows after 30000 positions, 32 heads of 128 each with a kv head (0.51 TFLOP): 492 us with
-// the join, 1040 TFLOP/s, where a large matrix product reaches 1198; with one group a step 523, and 545 without the priorities.  Four
-// prompts of 1900-2048 rows, 64 heads of 8 kv heads (0.26 TFLOP): 332, with one group a step 368.
+// Bound by the MFMAs and the softmax that share a SIMD: a group costs a wave 32 MFMAs (512 cycles), 66 vector instructions (16 of them
+// exponentials of 8 cycles, the others of 2 to 5) and 16 reads of LDS, and of two waves one hides a part of what the other does: MFMAs are busy
+// half of the cycles, at 1.95 GHz of 2.4.  1023 rows after 30000 positions, 32 heads of 128 each with a kv head (0.51 TFLOP): 488 us with the
+// join, 1050 TFLOP/s, where a large matrix product reaches 1198; with one group a step 523; where the waves with MFMAs do not go first
+// (s_setprio) 5 % more.  Four prompts of 1900-2048 rows, 64 heads of 8 kv heads (0.26 TFLOP): 318, with one group a step 368.
 template <int NK, int CB, bool ROWS>
 __global__ void __launch_bounds__(256, 2)
 k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
