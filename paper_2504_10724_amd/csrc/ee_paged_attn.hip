@@ -662,6 +662,8 @@ k_paged_join(AttnArgs a, int C, int n_slots, int n_tiles, int cols) {
 // and gain from having a CU to themselves: two chunks of 600 rows (16 heads of 4 kv heads) split beyond 48 groups 39, beyond 24 47.
 // Where one tile holds any sequence, every wave works on every group and there are few columns to join: 8 rows of 2000 positions with
 // 20 heads of one kv head, shares of 16 groups beyond 48 groups 19.3, of 8 beyond 24 13.2.
+// fp32: a group costs four times the MFMA time and twice the bytes: one row of 1975 positions, 6 heads of 84 (2 kv heads), shares of 16 beyond
+// 48 groups 25.1, of 8 beyond 16 18.4, of 4 beyond 16 16.3, beyond 8 the same; one row of 300 positions split 16.5, whole 15.0.
 Split split_groups(int64_t blocks, int groups, SplitRule rule) {
     if (groups <= rule.whole || blocks >= SPLIT_TARGET) return Split{std::max(groups, 1), 1};
     const int64_t want = (SPLIT_TARGET + blocks - 1) / blocks;
@@ -716,7 +718,7 @@ Plan make_plan(AttnArgs& a) {
 size_t paged_attention_workspace(int dtype, int hd, int Hkv, int n_q_heads, const StepView& st) {
     const int64_t most = (int64_t)st.max_q_len * (n_q_heads / Hkv);
     const int groups = (st.max_kv_len + 31) / 32;
-    int64_t columns = groups > STREAMED.whole ? (dtype == EE_BF16 ? std::min<int64_t>(ROWS_MOST, most) : f32_paged_columns(hd, most)) : 0;
+    int64_t columns = groups > (dtype == EE_BF16 ? STREAMED : FP32).whole ? (dtype == EE_BF16 ? std::min<int64_t>(ROWS_MOST, most) : f32_paged_columns(hd, most)) : 0;
     if (dtype == EE_BF16 && most > ROWS_MOST && groups > ONE_TILE_EACH.whole) columns += TILE_MOST;
     return (size_t)2 * SPLIT_TARGET * columns * share_bytes(hd);
 }

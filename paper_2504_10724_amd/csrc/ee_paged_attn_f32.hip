@@ -11,14 +11,8 @@
 
 __device__ __forceinline__ floatx4 mfma(float a, float b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-// features f .. f + 3 of a cached row, zeros beyond its hd (a load and selects, no branch)
-__device__ __forceinline__ floatx4 features(const float* row, int f, int hd) {
-    const bool in = f < hd;
-    floatx4 x = *reinterpret_cast<const floatx4*>(row + (in ? f : 0));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = in ? x[e] : 0.f;
-    return x;
-}
+// features f .. f + 3 of a cached row, or its first ones where these lie beyond its hd
+__device__ __forceinline__ floatx4 features(const float* row, int f, int hd) { return *reinterpret_cast<const floatx4*>(row + (f < hd ? f : 0)); }
 
 // O[j][4 c + e][r]: feature 64 c + 16 gq + 4 r + e
 template <int HD, int CB> struct ColumnsF32 : ColumnState<HD / 16, CB> {
@@ -90,15 +84,18 @@ template <int HD, int CB> struct ColumnsF32 : ColumnState<HD / 16, CB> {
 };
 
 // One workgroup per (16 CB columns of a sequence, kv head, share of the positions); its waves take the share's groups in turn, from
-// memory into registers, and join their sums through LDS.  The rows of more than one wave would need LDS for the keys, too: with 16 or 32
-// columns a workgroup the keys of a sequence come from L2 once for each of them.
-// WHOLE: the heads are HD wide, else less.
-// 64 single rows over 2000 positions, 4 heads of 64 (4 kv heads): 47 us, 5.6 TB/s; four prompts of 1000 rows of the same heads: 48 us, 43
-// TFLOP/s of 154.
+// memory into registers, and join their sums through LDS.  The keys and values of a group are asked for at once: one trip to memory a
+// group and wave instead of three (one row of 1975 positions, 6 heads of 84: 43 -> 25 us before the finer shares; 64 rows of 1000 positions, 4
+// heads of 256 with 2 kv heads: 106 -> 57).  Heads of 132 to 252 features do not have the registers for both halves of the keys (64 rows of
+// 1000 positions, heads of 200: 85 with halves, 125 without).  Asking for the next group as well, while one is worked on, was no faster.
+// WHOLE: the heads are HD wide, else less.  Two waves a SIMD where that does not spill: 4 prompts of 1000 rows, 6 heads of 84: 133 with two
+// waves, 123 with one; 64 rows of 1000 positions, heads of 128: 48.6 with two, 51.7 with one.
+// 64 single rows over 2000 positions, 4 heads of 64 (4 kv heads): 47 us, 5.6 TB/s; four prompts of 1000 rows of the same heads: 46 us, 45
+// TFLOP/s of 154: with 16 or 32 columns a workgroup the keys of a sequence come from L2 once for each of them.
 template <int HD, int CB, bool WHOLE>
-__global__ void __launch_bounds__(256, HD <= 128 ? 2 : 1)
+__global__ void __launch_bounds__(256, HD <= 64 || (HD == 128 && WHOLE) ? 2 : 1)
 k_f32_paged(AttnArgs a, int n_slots) {
-    constexpr int C = 16 * CB, NC = HD / 64;
+    constexpr int C = 16 * CB, NC = HD / 64, HALVES = WHOLE || HD <= 128 ? 2 : 1;    // of a group's keys, asked for at once with its values
     __shared__ float4 so[4][HD / 16][64];
     __shared__ float sm[4][C], sl[4][C];
     const int sx = blockIdx.x / a.pv.n_kv_heads, g = blockIdx.x - sx * a.pv.n_kv_heads;
@@ -117,6 +114,20 @@ k_f32_paged(AttnArgs a, int n_slots) {
 
     ColumnsF32<HD, CB> col;
     col.begin(a, c0, n_cols, first);
+    const int ps = a.pv.page_size, per = ps >> 5;
+    const int n_mine = max(0, (gb - ga - w + 3) >> 2);       // this wave's groups: ga + w, ga + w + 4, ..
+    auto mine_from = [&](int grp) { return min(max((grp - ga - w + 3) >> 2, 0), n_mine); };
+    // groups that every column sees whole: from a0 to a1 of the wave's
+    const int a0 = mine_from((lowest_seen(max_hi, a.window) + 31) >> 5), a1 = max(a0, mine_from((first + t0 + 1) >> 5));
+    // of the 64 groups around the one at work: their blocks in the pool, and which of a block's groups they are
+    uint32_t block = NO_GROUP, part_of = 0;
+    auto look_up = [&](int i) {
+        const int grp = ga + w + 4 * (i + lane);
+        const uint32_t at = grp < gb ? pool_group(a.pv, a.st, tl.s, g, grp) : NO_GROUP;
+        block = at == NO_GROUP ? NO_GROUP : at / (uint32_t)per;
+        part_of = at == NO_GROUP ? 0u : at - block * per;
+    };
+    if (n_mine > 0) look_up(0);
     floatx4 q[CB][HD / 16];                                  // features 16 k + 4 gq + e
     const float* p[CB];                                      // past the end: the last column's
 #pragma unroll
@@ -146,51 +157,48 @@ k_f32_paged(AttnArgs a, int n_slots) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) q[j][k][e] = __uint_as_float((__float_as_uint(q[j][k][e]) & keep) ^ flip);
         }
-
-    const int ps = a.pv.page_size, per = ps >> 5;
-    const int n_mine = max(0, (gb - ga - w + 3) >> 2);       // this wave's groups: ga + w, ga + w + 4, ..
-    auto mine_from = [&](int grp) { return min(max((grp - ga - w + 3) >> 2, 0), n_mine); };
-    // groups that every column sees whole: from a0 to a1 of the wave's
-    const int a0 = mine_from((lowest_seen(max_hi, a.window) + 31) >> 5), a1 = max(a0, mine_from((first + t0 + 1) >> 5));
-    uint32_t where = 0;
     auto run = [&](auto edge, int from, int to) {
         for (int i = from; i < to; ++i) {
-            if ((i & 63) == 0 || i == from) {
-                const int grp = ga + w + 4 * ((i & ~63) + lane);
-                where = grp < gb ? pool_group(a.pv, a.st, tl.s, g, grp) : NO_GROUP;
-            }
-            const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)where, i & 63);
-            if (at == NO_GROUP) continue;
+            if ((i & 63) == 0 && i > 0) look_up(i);
+            const uint32_t blk = (uint32_t)__builtin_amdgcn_readlane((int)block, i & 63), at = (uint32_t)__builtin_amdgcn_readlane((int)part_of, i & 63);
+            if (blk == NO_GROUP) continue;
             // of the block's keys, then its values: the group's offset in both
-            const uint32_t blk = at / (uint32_t)per;
-            const float* kp = (const float*)a.pv.pool + (int64_t)blk * (2 * ps * hd) + (int64_t)(at - blk * per) * (32 * hd);
+            const float* kp = (const float*)a.pv.pool + (int64_t)blk * (2 * ps * hd) + (int64_t)at * (32 * hd);
             const float* vp = kp + (int64_t)ps * hd;
             const int pg = (ga + w + 4 * i) << 5;
-            floatx4 S1[1][CB][2];
-            floatx4 (&S)[CB][2] = S1[0];
+            floatx4 kf[HALVES][HD / 16], v[8][NC], S[1][CB][2];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                floatx4 kf[HD / 16];
+            for (int j = 0; j < CB; ++j) S[0][j][0] = S[0][j][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int k = 0; k < HD / 16; ++k) kf[k] = features(kp + (16 * b + n16) * hd, 16 * k + 4 * gq, hd);
-#pragma unroll
-                for (int j = 0; j < CB; ++j) S[j][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (int b0 = 0; b0 < 2; b0 += HALVES) {
 #pragma unroll
                 for (int k = 0; k < HD / 16; ++k)
-                    if (16 * k < hd)
+#pragma unroll
+                    for (int b = 0; b < HALVES; ++b) kf[b][k] = features(kp + (16 * (b0 + b) + n16) * hd, 16 * k + 4 * gq, hd);
+                __builtin_amdgcn_sched_barrier(0);           // in this order: the first product waits for no value
+                if (b0 + HALVES == 2)
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)              // what lies beyond hd goes to sums that nobody reads
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) v[r][c] = features(vp + (16 * (r >> 2) + 4 * gq + (r & 3)) * hd, 64 * c + 4 * n16, hd);
+#pragma unroll
+                for (int k = 0; k < HD / 16; ++k)
+                    if (WHOLE || 16 * k < hd) {
+                        if (!WHOLE && 16 * k + 16 > hd)      // zeros beyond hd (a query's zero does not keep an infinity out)
+#pragma unroll
+                            for (int b = 0; b < HALVES; ++b)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) kf[b][k][e] = 16 * k + 4 * gq < hd ? kf[b][k][e] : 0.f;
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
 #pragma unroll
-                            for (int j = 0; j < CB; ++j) S[j][b] = mfma(kf[k][e], q[j][k][e], S[j][b]);
+                            for (int j = 0; j < CB; ++j)
+#pragma unroll
+                                for (int b = 0; b < HALVES; ++b) S[0][j][b0 + b] = mfma(kf[b][k][e], q[j][k][e], S[0][j][b0 + b]);
+                    }
             }
-            floatx4 v[8][NC];
-#pragma unroll
-            for (int r = 0; r < 8; ++r)
-#pragma unroll
-                for (int c = 0; c < NC; ++c)
-                    v[r][c] = features(vp + (16 * (r >> 2) + 4 * gq + (r & 3)) * hd, 64 * c + 4 * n16, hd);
             float x[1][CB][8], P[CB][8];
-            col.template exponents<edge.value, 1>(S1, x, a.scale2, pg, a.window);
+            col.template exponents<edge.value, 1>(S, x, a.scale2, pg, a.window);
             col.probabilities(x[0], P);
             if constexpr (edge.value) col.weigh_edge(v, P, hd, pg, min_lo, max_hi, a.window);
             else col.weigh(v, P, hd);
@@ -258,7 +266,7 @@ int f32_paged_attention(AttnArgs a, char* ws, hipStream_t s) {
     const int C = (int)f32_paged_columns(hd, most), cb = C / 16;
     a.one_tile = most <= C;
     const int64_t slots = tile_slots(a, C);
-    const Split sp = split_groups(slots * Hkv, groups_seen(a.st, (C + a.G - 1) / a.G + 1, a.window), STREAMED);
+    const Split sp = split_groups(slots * Hkv, groups_seen(a.st, (C + a.G - 1) / a.G + 1, a.window), FP32);
     if (slots * Hkv * sp.shares >= MOST_BLOCKS) return ee_fail(EE_ERR_SHAPE, "ee_paged_attention: more workgroups than a launch holds");
     a.rows_cols = 0;                                         // all sequences are tiled
     a.tiles.place(sp, ws, slots * Hkv * C, hd);
