@@ -270,7 +270,7 @@ static inline int64_t tile_slots(const AttnArgs& a, int C) {
 // SPLIT_TARGET + blocks, and nothing is split that has SPLIT_TARGET workgroups already or `whole` groups at most.
 constexpr int SPLIT_TARGET = 512;
 struct SplitRule { int whole, least; };                      // groups that are not worth a split; groups a share has at least
-constexpr SplitRule STREAMED{48, 16}, ONE_TILE_EACH{24, 8}, FP32{16, 4};
+constexpr SplitRule STREAMED{48, 16}, FEW_TILES{24, 8}, WIDE{16, 6}, FP32{16, 4};
 Split split_groups(int64_t blocks, int groups, SplitRule rule);
 // groups of 32 positions that `rows` neighbouring rows see together at most
 int groups_seen(const StepView& st, int64_t rows, int window);

@@ -661,7 +661,11 @@ k_paged_join(AttnArgs a, int C, int n_slots, int n_tiles, int cols) {
 // split 10.2, whole 9.0; two rows of 20000 (4 pairs), shares of 8 groups 19.7, of 16 16.6.  Tiles of 128 columns pay more for the join
 // and gain from having a CU to themselves: two chunks of 600 rows (16 heads of 4 kv heads) split beyond 48 groups 39, beyond 24 47.
 // Where one tile holds any sequence, every wave works on every group and there are few columns to join: 8 rows of 2000 positions with
-// 20 heads of one kv head, shares of 16 groups beyond 48 groups 19.3, of 8 beyond 24 13.2.
+// 20 heads of one kv head, shares of 16 groups beyond 48 groups 19.3, of 8 beyond 24 13.2.  So it is where there are few tiles: 100 rows after
+// 2000 positions, 4 heads of 2 kv heads (8 tiles), 23.4 and 18.8; three prompts of 900-1200 rows of the same heads (up to 114 tiles) 28.8 and 32.5.
+// Wide heads (256 features): one row of 1500 positions, 16 heads of 2 kv heads, shares of 16 beyond 48 17.6, of 8 beyond 24 13.4, of 6 beyond 16
+// 13.3; 16 rows of 700-1400 28, 17, 15.5; 4 x 4-10 rows after 400-935 (16 tiles) 25.7, 25.7, 20.0; two chunks of 300 rows after 800 (152 tiles)
+// 37, 45, 45.
 // fp32: a group costs four times the MFMA time and twice the bytes: one row of 1975 positions, 6 heads of 84 (2 kv heads), shares of 16 beyond
 // 48 groups 25.1, of 8 beyond 16 18.4, of 4 beyond 16 16.3, beyond 8 the same; one row of 300 positions split 16.5, whole 15.0.
 Split split_groups(int64_t blocks, int groups, SplitRule rule) {
@@ -704,11 +708,12 @@ Plan make_plan(AttnArgs& a) {
         const int C = 64 * p.tile_cb;
         a.one_tile = most <= C;
         p.n_slots = tile_slots(a, C);
-        p.t = split_groups(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window), a.one_tile ? ONE_TILE_EACH : STREAMED);
+        const bool few = a.one_tile || p.n_slots * Hkv <= (hd > 128 ? 128 : 96);
+        p.t = split_groups(p.n_slots * Hkv, groups_seen(st, (C + G - 1) / G + 1, window), !few ? STREAMED : hd > 128 ? WIDE : FEW_TILES);
     }
     if (p.rows) {
         p.rows_blocks = (int64_t)st.n_seqs * Hkv;
-        p.r = split_groups(p.rows_blocks, groups_seen(st, (p.rows_cols + G - 1) / G, window), STREAMED);
+        p.r = split_groups(p.rows_blocks, groups_seen(st, (p.rows_cols + G - 1) / G, window), hd > 128 ? WIDE : STREAMED);
     }
     return p;
 }
@@ -718,8 +723,9 @@ Plan make_plan(AttnArgs& a) {
 size_t paged_attention_workspace(int dtype, int hd, int Hkv, int n_q_heads, const StepView& st) {
     const int64_t most = (int64_t)st.max_q_len * (n_q_heads / Hkv);
     const int groups = (st.max_kv_len + 31) / 32;
-    int64_t columns = groups > (dtype == EE_BF16 ? STREAMED : FP32).whole ? (dtype == EE_BF16 ? std::min<int64_t>(ROWS_MOST, most) : f32_paged_columns(hd, most)) : 0;
-    if (dtype == EE_BF16 && most > ROWS_MOST && groups > ONE_TILE_EACH.whole) columns += TILE_MOST;
+    if (dtype != EE_BF16) return groups > FP32.whole ? (size_t)2 * SPLIT_TARGET * f32_paged_columns(hd, most) * share_bytes(hd) : 0;
+    int64_t columns = groups > (hd > 128 ? WIDE : STREAMED).whole ? std::min<int64_t>(ROWS_MOST, most) : 0;
+    if (most > ROWS_MOST && groups > (hd > 128 ? WIDE : FEW_TILES).whole) columns += TILE_MOST;
     return (size_t)2 * SPLIT_TARGET * columns * share_bytes(hd);
 }
 
