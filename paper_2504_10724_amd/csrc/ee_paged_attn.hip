@@ -6,8 +6,10 @@
 // leave their registers.  Lane (n16, gq) holds column n16 of a block of 16 and, of a group, the positions 16 b + 4 gq + r.
 //
 // Softmax: one pass, running maximum and sum in fp32 (log2 units).  Sums are rescaled only when a maximum rises by more than
-// 2^8: probabilities up to 256 lose nothing in bf16 or fp32.  Probabilities are rounded to bf16 for the second product (relative 2^-8
-// each, as the values they weigh were), the sum of the row takes them unrounded.
+// 2^8: probabilities up to 256 lose nothing in bf16 or fp32.  The sum of the row takes them unrounded.  Into the second product they
+// go as a pair of bf16 (off by 2^-16) where the cache's bytes bound the call and the MFMAs idle (few columns: 214 us, 6.2 TB/s, with
+// one and with two), as one bf16 (2^-8 each, as the values they weigh were) in the tiles, whose MFMAs and softmax set the time: with
+// pairs 1023 rows after 30000 positions take 740 us instead of 487, four prompts of 1900-2048 rows 425 instead of 312.
 #include "ee_paged_attn.h"
 
 #include <algorithm>
@@ -32,10 +34,12 @@ __device__ __forceinline__ uint32_t odd_bits(uint32_t w) { return ((w & 0x7f807f
 __device__ __forceinline__ uint32_t half_mask(uint32_t bits) { bits >>= 15; return (bits << 16) - bits; }
 
 // ------------------------------------------------------------------ the columns of a wave
-// CB blocks of 16 columns of a (sequence, kv head), and what the softmax and the second product keep for them
-template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[j][hb][r]: feature 16 hb + 4 gq + r
+// CB blocks of 16 columns of a (sequence, kv head), and what the softmax and the second product keep for them; a probability is PARTS bf16
+template <int CB, int PARTS> struct Probabilities { uint4 part[PARTS][CB]; };
+template <int NK, int CB, int PARTS> struct Columns : ColumnState<2 * NK, CB> {       // O[j][hb][r]: feature 16 hb + 4 gq + r
     using State = ColumnState<2 * NK, CB>;
     using State::hi; using State::O;
+    using Probs = Probabilities<CB, PARTS>;
     uint4 q[CB][NK];
 
     // columns c0 .. of the n_cols of a sequence whose first row is row0, at position first
@@ -79,14 +83,26 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
     }
 
     // the probabilities of a group as right operands
-    __device__ __forceinline__ void operands(const float (&x)[CB][8], uint4 (&P)[CB]) {
+    __device__ __forceinline__ void operands(const float (&x)[CB][8], Probs& P) {
         float e[CB][8];
         State::probabilities(x, e);
 #pragma unroll
         for (int j = 0; j < CB; ++j)
-            P[j] = make_uint4(bf16_pair(e[j][0], e[j][1]), bf16_pair(e[j][2], e[j][3]), bf16_pair(e[j][4], e[j][5]), bf16_pair(e[j][6], e[j][7]));
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w[i] = bf16_pair(e[j][2 * i], e[j][2 * i + 1]);
+                    if (part + 1 < PARTS) {                  // what the next part holds of them
+                        e[j][2 * i] -= __uint_as_float(w[i] << 16);
+                        e[j][2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+                    }
+                }
+                P.part[part][j] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
     }
-    template <bool EDGE> __device__ __forceinline__ void weights(const floatx4 (&S)[1][CB][2], uint4 (&P)[CB], float scale2, int pg, int window) {
+    template <bool EDGE> __device__ __forceinline__ void weights(const floatx4 (&S)[1][CB][2], Probs& P, float scale2, int pg, int window) {
         float x[1][CB][8];
         State::template exponents<EDGE, 1>(S, x, scale2, pg, window);
         operands(x[0], P);
@@ -110,7 +126,7 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
 
     // second product of a group at pg with the values vf of N blocks of 16 features from block H0 on
     template <bool EDGE, int H0 = 0, int N>
-    __device__ __forceinline__ void weigh_group(const uint4 (&vf)[N], const uint4 (&P)[CB], int pg, int min_lo, int max_hi, int window) {
+    __device__ __forceinline__ void weigh_group(const uint4 (&vf)[N], const Probs& P, int pg, int min_lo, int max_hi, int window) {
         if constexpr (EDGE) {
             weigh_edge<H0, N>(vf, P, pg, min_lo, max_hi, window);
         } else {
@@ -120,9 +136,11 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
     }
 
     // O += V^T P^T of the 16 features of block hb
-    __device__ __forceinline__ void weigh(int hb, uint4 v, const uint4 (&P)[CB]) {
+    __device__ __forceinline__ void weigh(int hb, uint4 v, const Probs& P) {
 #pragma unroll
-        for (int j = 0; j < CB; ++j) O[j][hb] = mfma(v, P[j], O[j][hb]);
+        for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+            for (int j = 0; j < CB; ++j) O[j][hb] = mfma(v, P.part[part][j], O[j][hb]);
     }
 
     // The same where some column does not see all positions.  A probability of zero does not keep an infinity or NaN among the
@@ -131,7 +149,7 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
     // What lies outside min_lo .. max_hi no column sees; it may be memory nobody has written, and counts as zero.
     // Words hold two bf16; the tests work on both halves without a carry between.
     template <int H0, int N>
-    __device__ __forceinline__ void weigh_edge(const uint4 (&vf)[N], const uint4 (&P)[CB], int pg, int min_lo, int max_hi, int window) {
+    __device__ __forceinline__ void weigh_edge(const uint4 (&vf)[N], const Probs& P, int pg, int min_lo, int max_hi, int window) {
         uint32_t in[4], any = 0;
         seen_words(in, min_lo, max_hi, pg);
         auto inside = [&](uint4 v) { return make_uint4(v.x & in[0], v.y & in[1], v.z & in[2], v.w & in[3]); };
@@ -167,7 +185,8 @@ template <int NK, int CB> struct Columns : ColumnState<2 * NK, CB> {       // O[
             const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < CB; ++j) {
-                const uint32_t pw[4] = {P[j].x, P[j].y, P[j].z, P[j].w};
+                const uint4 first = P.part[0][j];                // zero only where the probability is
+                const uint32_t pw[4] = {first.x, first.y, first.z, first.w};
                 uint32_t sees[4], some[4], none[4];          // 1 where the column sees a position with P > 0, with P = 0
                 seen_words(sees, lowest_seen(hi[j], window), hi[j], pg);
 #pragma unroll
@@ -228,7 +247,8 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
         now = group_of_page(a.pv, a.st, early, g, ga + w + WAVES * lane);
     }
     then = now;
-    Columns<NK, CB> col;
+    using Cols = Columns<NK, CB, 2>;
+    Cols col;
     col.start(a, g, 0, n_cols, first, sr.row0);
     // keys and values of a group each have registers of their own, which are asked for again as soon as a product has used them;
     // a group that is not there is replaced by the pool's first
@@ -261,7 +281,7 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
             const int pg = (ga + w + WAVES * i) << 5;
             if (i + 1 < n_mine && ((i + 1) & 63) == 0) then = look_up(i + 1);
             const uint4* next = place(min(i + 1, n_mine - 1));
-            uint4 P[CB];
+            typename Cols::Probs P;
             floatx4 S[1][CB][2];
             if (works) col.scores(kf, S[0]);
             __builtin_amdgcn_sched_barrier(0);
@@ -421,7 +441,8 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
         }
     };
     if (n > 0) then = now = look_up(0);
-    Columns<NK, CB> col;
+    using Cols = Columns<NK, CB, 1>;
+    Cols col;
     col.start(a, g, cw, n_cols, first, sr.row0);             // the queries come in beside the page numbers and the first group
     if (n > 0) issue(0);
     col.settle(a);
@@ -442,7 +463,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
     auto one_group = [&](auto edge, int i) {
         const int pg = (ga + i) << 5;
         if (edge.value && (i >= n || pg > w_last || pg + 31 < min_lo || !there(i))) return;
-        uint4 P[CB];
+        typename Cols::Probs P;
         floatx4 S[1][CB][2];
         constexpr int H = (NK + 1) / 2;                      // slices of 32 features in the first half
         auto keys = [&](auto k0, auto& kf) {                 // slices from k0 on
@@ -495,7 +516,8 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
                 load_keys(ka, 2 * u, 0, H);
                 bool more = true;
                 do {
-                    uint4 kb[2 * NK], va[2 * NK], vb[2 * NK], P[2][CB];
+                    uint4 kb[2 * NK], va[2 * NK], vb[2 * NK];
+                    typename Cols::Probs P[2];
                     floatx4 S[2][CB][2];
                     float x[2][CB][8];
                     load_keys(ka, 2 * u, H, NK);             // the first half came during the second product: there are no registers for more

@@ -1,0 +1,43 @@
+"""Numerics of the attention over the paged cache that test_gpu_paged.py's tolerances do not tell apart, against 64 bits.
+
+fp32 terms as there: e = U A (2 (hd + 4) D + n + 64), with A = sum_j p_j |v_j| and D = max_j sum_i |q_i k_ji| scale.  A bf16 result
+carries one rounding of 2^-8 of the value."""
+import pytest
+import torch
+
+import paged_ref as R
+from paper_2504_10724_amd import paged as P
+from test_gpu_paged import U, Batch
+
+pytestmark = pytest.mark.gpu
+
+SINGLES = [
+    # hd, query heads, kv heads, window, (rows, positions) of each sequence
+    (64, 6, 2, 0, [(1, 95), (1, 500), (1, 1)]),
+    (96, 8, 1, 0, [(1, 700), (1, 33)]),
+    (128, 8, 2, 0, [(1, 64), (1, 257), (1, 1000)]),
+    (128, 8, 2, 37, [(1, 90), (1, 300)]),
+    (128, 4, 2, 0, [(4, 300), (4, 70)]),                               # four rows of two heads: eight columns
+    (128, 8, 2, 0, [(70, 300), (1, 200), (1, 611)]),                   # beside a chunk, in its launch
+    (192, 4, 2, 0, [(1, 400), (17, 30), (1, 900)]),                    # beside a chunk, in a launch of their own
+    (256, 4, 2, 0, [(1, 130), (1, 800)]),                              # in shares
+]
+
+
+@pytest.mark.parametrize("case", SINGLES, ids=lambda c: "-".join(str(x) for x in c[:4]) + f"-{len(c[4])}seqs")
+def test_few_columns_keep_the_probabilities_bits(case):
+    """sequences of up to 16 columns: a probability enters the second product as a pair of bf16, 2^-8 x 2^-8 of it off at most, so
+    all that a result has lost beside fp32's terms is its own rounding"""
+    hd, hq, hkv, window, seqs = case
+    print(f"[case] precision {case}", flush=True)
+    b = Batch(seqs, hq, hkv, hd, 64, "bf16")
+    x, q = b.fill(), b.queries()
+    got = P.attend(b.kv, 1, b.step, q.cuda(), window=window).cpu().double()
+    want, size, dots = R.attend(q, x[:, 0], b.seqs, b.pages, window, hd ** -0.5)
+    e = size * (2.0 ** -16 + U * (2 * (hd + 4) * dots + max(length for _, length in seqs) + 64))
+    for (n, _), at in zip(seqs, b.start):
+        if n * (hq // hkv) <= 16:
+            rows = slice(at, at + n)
+            err = (got[rows] - want[rows]).abs()
+            tol = 2.0 ** -8 * (want[rows].abs() + e[rows]) + e[rows]
+            assert (err <= tol).all(), (n, float((err / tol).max()))
