@@ -589,7 +589,8 @@ int ee_paged_append(const ee_paged* p, int layer, const ee_paged_step* step, con
  * out and set status bit 1.  A row that sees no position gets zeros.  What lies at positions a row does not see, infinities
  * and NaN included, does not reach it.
  * EE_BF16: scores, softmax statistics and sums in fp32.  For the product with V a probability is rounded to one bf16 (2^-8 of
- * it), to a pair of them (2^-16) for sequences of at most 16 new rows times n_q_heads / n_kv_heads.
+ * it), to a pair of them (2^-16) for sequences of at most 16 new rows times n_q_heads / n_kv_heads.  Weighted sums are divided at the
+ * end: a feature's |v_j| added up over the positions a row sees must stay below fp32's largest value.
  * Workspace: ee_paged_attention_workspace bytes, 256-byte aligned, for calls whose host's figures are at most these; its contents
  * mean nothing between calls.  Calls that overlap in time need one each.
  * n_q_heads: a multiple of n_kv_heads.  out may not overlap q.

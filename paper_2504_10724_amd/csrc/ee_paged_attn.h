@@ -12,7 +12,7 @@ struct Shares {
     int share = 1;                 // groups of 32 positions that a workgroup takes at most ...
     int shares = 1;                // ... and how many of them the longest sequence has
     float*  part = nullptr;        // sums of the shares, unnormalised [workgroup][share][column][hd]
-    float2* stat = nullptr;        // (maximum in log2 units, sum; sum < 0: no position seen) [workgroup][share][column]
+    float2* stat = nullptr;        // (reference of the exponents in log2 units, sum; sum < 0: no position seen) [workgroup][share][column]
     // columns: of all workgroups, before the split; returns what follows in the workspace
     char* place(const Split& sp, char* ws, int64_t columns, int hd) {
         share = sp.share;
@@ -82,7 +82,7 @@ __device__ __forceinline__ float quad_sum(float v) {
     return v + __shfl_xor(v, 32, 64);
 }
 
-// what a maximum of -inf (nothing seen yet, or only scores of -inf) is replaced by in exponents
+// what a largest reference of -inf (nothing seen yet, or only scores of -inf) is replaced by in exponents
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
 
 // Positions lo .. hi of the group at pg as bits (bit r: position pg + r); of these the eight a lane holds (bit e: 16 (e / 4) + 4 gq +
@@ -100,8 +100,7 @@ __device__ __forceinline__ uint32_t bit_mask(uint32_t bits, int i) { return (uin
 // positions 16 b + 4 gq + r.  NO sums of four features a lane and block, which the kernel's second product adds to.
 template <int NO, int CB> struct ColumnState {
     int   hi[CB];                  // the last position the lane's column sees (-1: none); the first is lowest_seen(hi, window)
-    float neg[CB], lim[CB], l[CB]; // minus the exponents' reference (log2 units); how far above it a score may lie (see exponents); the
-                                   // lane's part of the sum
+    float neg[CB], lim[CB], l[CB]; // minus the exponents' reference (log2 units); 0, or -inf while there is none; the lane's part of the sum
     uint32_t seen;                 // bit j: the column of block j has seen a position
     floatx4 O[CB][NO];
 
@@ -120,14 +119,16 @@ template <int NO, int CB> struct ColumnState {
         }
     }
 
-    __device__ __forceinline__ float maximum(int j) const { return lim[j] == -INFINITY ? -INFINITY : -neg[j]; }
+    __device__ __forceinline__ float reference_of(int j) const { return lim[j] == -INFINITY ? -INFINITY : -neg[j]; }
 
     // Scores S[k][j][b][r] of positions 16 b + 4 gq + r of group k -> exponents x[k][j][4 b + r] of their probabilities.  EDGE: some column
     // does not see all of the group, which starts at pg.
-    // A column's reference is its largest score when it was last moved: it moves when a score exceeds it by more than lim = 8, or,
-    // while nothing but -inf has been seen (lim = -inf), when any does.  A lane looks at its own scores only; the four lanes of a column
-    // meet when one of the wave's references has to move.  Then the exponents move by the same step: they cost a second rounding of
-    // relative 2^-24, and the scores need not stay in registers.
+    // A column's reference is HEADROOM above its largest score when it was last moved: it moves when a score exceeds it, or, while
+    // nothing but -inf has been seen (lim = -inf), when any does.  So no probability is above 1, and the sums weighted by them stay in
+    // range as long as the values' own sums do, in whatever order the scores come.  A lane looks at its own scores only; the four lanes of
+    // a column meet when one of the wave's references has to move.  Then the exponents move by the same step: they cost a second rounding
+    // of relative 2^-24, and the scores need not stay in registers.
+    static constexpr float HEADROOM = 8.0f;
     template <bool EDGE, int NG>
     __device__ __forceinline__ void exponents(const floatx4 (&S)[NG][CB][2], float (&x)[NG][CB][8], float scale2, int pg, int window) {
         static_assert(!EDGE || NG == 1, "groups that not all columns see come one by one");
@@ -168,21 +169,21 @@ template <int NO, int CB> struct ColumnState {
         if (__builtin_expect(__any(raise), 0)) {
 #pragma unroll
             for (int j = 0; j < CB; ++j) {
-                const float t = quad_max(top[j]);
+                const float t = quad_max(top[j]), by = t + HEADROOM;
                 const bool up = t > lim[j];
-                const float to = up ? neg[j] - t : neg[j];
+                const float to = up ? neg[j] - by : neg[j];
                 float alpha = __builtin_amdgcn_exp2f(to - neg[j]);
                 if (lim[j] == -INFINITY) alpha = 0.f;        // there is nothing yet
                 if (!up) alpha = 1.f;
                 neg[j] = to;
-                lim[j] = up ? 8.0f : lim[j];
+                lim[j] = up ? 0.0f : lim[j];
                 l[j] *= alpha;
 #pragma unroll
                 for (int hb = 0; hb < NO; ++hb) O[j][hb] = O[j][hb] * alpha;
 #pragma unroll
                 for (int k = 0; k < NG; ++k)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[k][j][i] -= up ? t : 0.f;
+                    for (int i = 0; i < 8; ++i) x[k][j][i] -= up ? by : 0.f;
             }
         }
     }

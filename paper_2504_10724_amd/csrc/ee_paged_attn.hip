@@ -5,11 +5,12 @@
 // a lane's eight scores of a group are its eight elements of the right operand of the second product, so the probabilities never
 // leave their registers.  Lane (n16, gq) holds column n16 of a block of 16 and, of a group, the positions 16 b + 4 gq + r.
 //
-// Softmax: one pass, running maximum and sum in fp32 (log2 units).  Sums are rescaled only when a maximum rises by more than
-// 2^8: probabilities up to 256 lose nothing in bf16 or fp32.  The sum of the row takes them unrounded.  Into the second product they
-// go as a pair of bf16 (off by 2^-16) where the cache's bytes bound the call and the MFMAs idle (few columns: 214 us, 6.2 TB/s, with
-// one and with two), as one bf16 (2^-8 each, as the values they weigh were) in the tiles, whose MFMAs and softmax set the time: with
-// pairs 1023 rows after 30000 positions take 740 us instead of 487, four prompts of 1900-2048 rows 425 instead of 312.
+// Softmax: one pass, running reference and sum in fp32 (log2 units).  The reference lies 8 above the largest score it was set for, and
+// sums are rescaled only when a score exceeds it, which is rare: probabilities stay between 0 and 1 and lose no bit in bf16 or fp32
+// (below 2^-118 of the largest they become 0).  The sum of the row takes them unrounded.  Into the second product they go as a pair of
+// bf16 (off by 2^-16) where the cache's bytes bound the call and the MFMAs idle (few columns: 214 us, 6.2 TB/s, with one and with two),
+// as one bf16 (2^-8 each, as the values they weigh were) in the tiles, whose MFMAs and softmax set the time: with pairs 1023 rows after
+// 30000 positions take 740 us instead of 487, four prompts of 1900-2048 rows 425 instead of 312.
 #include "ee_paged_attn.h"
 
 #include <algorithm>
@@ -304,7 +305,7 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
     // join the waves: maxima and sums, then the weighted sums, the blocks of 16 features in turn
     const float part_l = quad_sum(col.l[0]);
     if (lane < 16) {
-        sm[w][n16] = col.maximum(0);
+        sm[w][n16] = col.reference_of(0);
         sl[w][n16] = col.seen & 1u ? part_l : -1.f;
     }
 #pragma unroll
@@ -580,7 +581,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
         const float l = quad_sum(col.l[j]);
         const bool seen = (col.seen >> j) & 1u;
         const int64_t at = block + c - c0;
-        if (!last && c < n_cols && lane < 16) a.tiles.stat[at] = make_float2(col.maximum(j), seen ? l : -1.f);
+        if (!last && c < n_cols && lane < 16) a.tiles.stat[at] = make_float2(col.reference_of(j), seen ? l : -1.f);
         const float inv = last ? 1.0f / l : 1.f;
 #pragma unroll
         for (int hb = 0; hb < 2 * NK; ++hb) col.O[j][hb] = seen ? col.O[j][hb] * inv : floatx4{0.f, 0.f, 0.f, 0.f};

@@ -214,7 +214,7 @@ k_f32_paged(AttnArgs a, int n_slots) {
     for (int j = 0; j < CB; ++j) {
         const float l = quad_sum(col.l[j]);
         if (lane < 16) {
-            sm[w][16 * j + n16] = col.maximum(j);
+            sm[w][16 * j + n16] = col.reference_of(j);
             sl[w][16 * j + n16] = (col.seen >> j) & 1u ? l : -1.f;
         }
     }

@@ -41,3 +41,21 @@ def test_few_columns_keep_the_probabilities_bits(case):
             err = (got[rows] - want[rows]).abs()
             tol = 2.0 ** -8 * (want[rows].abs() + e[rows]) + e[rows]
             assert (err <= tol).all(), (n, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("at", [50, 178])                              # in the second group, in the second of one of four waves
+@pytest.mark.parametrize("dtype,rows", [("bf16", 1), ("bf16", 8), ("bf16", 100), ("f32", 1), ("f32", 40)])
+def test_large_values_average_whatever_the_order_of_the_scores(dtype, rows, at):
+    """the average of equal finite values is that value, also where a later score is a hundred times as likely as the first ones"""
+    print(f"[case] large values {dtype} {rows} rows, {at}", flush=True)
+    b = Batch([(rows, rows + 200), (rows, rows + 189)], 4, 2, 64, 32, dtype)
+    x, q = torch.zeros(2, 1, b.n_pages, 2, 32, 64, dtype=b.dt), torch.zeros(b.n, 4, 64, dtype=b.dt)
+    x[1] = 4e36
+    q[..., 0] = 1.0
+    for table in b.pages:
+        x[0, 0, table[at // 32], :, at % 32, 0] = 4.84                 # 2^6.98 times the weight of a score of zero
+    b.put(x)
+    got = P.attend(b.kv, 1, b.step, q.cuda(), scale=1.0).cpu().double()
+    value = float(x[1, 0, 0, 0, 0, 0])
+    # weights add up to one within 300 roundings each; the probabilities' and the result's rounding in bf16
+    assert ((got - value).abs() <= value * (600 * U + (2.0 ** -7 if dtype == "bf16" else 0.0))).all(), got.flatten()[:4]
