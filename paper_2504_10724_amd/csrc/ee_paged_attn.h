@@ -33,8 +33,7 @@ struct AttnArgs {
     StepView  st;
     HeadsView q, out;
     int   G;
-    float scale2;                  // |scale| log2 e: exp(x) = 2^(x log2 e)
-    uint32_t flip, keep;           // what a negative scale puts into q (its signs), and a scale of zero leaves of it
+    float scale2;                  // scale log2 e: exp(x) = 2^(x log2 e)
     int   window;                  // 0: none
     int   rows_cols;
     int   one_tile;                // no sequence has more columns than a tile: slot s of the tiles is sequence s

@@ -70,15 +70,15 @@ template <int NK, int CB, int PARTS> struct Columns : ColumnState<2 * NK, CB> { 
                 }
         }
     }
-    // the queries have arrived: the sign or zero of the scale goes in, columns past the end come to zero
-    __device__ __forceinline__ void settle(const AttnArgs& a) {
+    // the queries have arrived: columns past the end come to zero
+    __device__ __forceinline__ void settle() {
 #pragma unroll
         for (int j = 0; j < CB; ++j) {
-            const uint32_t keep = hi[j] >= 0 ? a.keep : 0u, flip = hi[j] >= 0 ? a.flip : 0u;
+            const uint32_t keep = hi[j] >= 0 ? 0xffffffffu : 0u;
 #pragma unroll
             for (int k = 0; k < NK; ++k) {
                 uint4& v = q[j][k];
-                v = make_uint4((v.x & keep) ^ flip, (v.y & keep) ^ flip, (v.z & keep) ^ flip, (v.w & keep) ^ flip);
+                v = make_uint4(v.x & keep, v.y & keep, v.z & keep, v.w & keep);
             }
         }
     }
@@ -270,7 +270,7 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, RowsShared<NK>& sh
         load_keys(place(0));
         load_values(place(0));
     }
-    col.settle(a);
+    col.settle();
     // whether a column does not see all of a group is settled by range, so the loop over the groups that all see has no test:
     // edge before a0 (the window's start) and from a1 on (the rows' own positions)
     auto mine_from = [&](int grp) { return min(max((grp - ga - w + WAVES - 1) / WAVES, 0), n_mine); };
@@ -446,7 +446,7 @@ k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
     Cols col;
     col.start(a, g, cw, n_cols, first, sr.row0);             // the queries come in beside the page numbers and the first group
     if (n > 0) issue(0);
-    col.settle(a);
+    col.settle();
 #pragma unroll
     for (int j = 0; j < CB; ++j)                             // in registers: a wait for them in the loop would wait for its groups
 #pragma unroll
@@ -802,9 +802,7 @@ int launch_paged_attention(int dtype, const PagedView& pv, const StepView& st, c
     AttnArgs a{};
     a.pv = pv; a.st = st; a.q = q; a.out = out;
     a.G = n_q_heads / pv.n_kv_heads;
-    a.scale2 = scale == 0.f ? 1.f : std::fabs(scale) * 1.44269504088896340736f;
-    a.flip = scale < 0.f ? 0x80008000u : 0u;
-    a.keep = scale == 0.f ? 0u : 0xffffffffu;
+    a.scale2 = scale * 1.44269504088896340736f;
     a.window = window;
     if (dtype != EE_BF16) return f32_paged_attention(a, ws, s);
     const Plan p = make_plan(a);

@@ -153,9 +153,9 @@ k_f32_paged(AttnArgs a, int n_slots) {
     for (int j = 0; j < CB; ++j)
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k) {
-            const uint32_t keep = col.hi[j] >= 0 && (WHOLE || 16 * k + 4 * gq < hd) ? a.keep : 0u, flip = a.flip & 0x80000000u;
+            const bool there = col.hi[j] >= 0 && (WHOLE || 16 * k + 4 * gq < hd);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) q[j][k][e] = __uint_as_float((__float_as_uint(q[j][k][e]) & keep) ^ flip);
+            for (int e = 0; e < 4; ++e) q[j][k][e] = there ? q[j][k][e] : 0.f;
         }
     auto run = [&](auto edge, int from, int to) {
         for (int i = from; i < to; ++i) {

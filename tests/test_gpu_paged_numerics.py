@@ -59,3 +59,20 @@ def test_large_values_average_whatever_the_order_of_the_scores(dtype, rows, at):
     value = float(x[1, 0, 0, 0, 0, 0])
     # weights add up to one within 300 roundings each; the probabilities' and the result's rounding in bf16
     assert ((got - value).abs() <= value * (600 * U + (2.0 ** -7 if dtype == "bf16" else 0.0))).all(), got.flatten()[:4]
+
+
+@pytest.mark.parametrize("dtype,rows", [("bf16", 1), ("bf16", 100), ("f32", 1), ("f32", 40)])
+def test_a_scale_of_zero_does_not_hide_what_the_queries_hold(dtype, rows):
+    """0 x NaN and 0 x inf are NaN: so are the row's weights"""
+    print(f"[case] scale zero {dtype} {rows} rows", flush=True)
+    b = Batch([(rows, 150), (rows, rows)], 4, 2, 64, 32, dtype)
+    x, q = b.fill(), b.queries()
+    ref = b.check_attention(x, q, scale=0.0)
+    for value in (float("nan"), float("inf")):
+        y = q.clone()
+        y[0, 1, 3] = value
+        got = P.attend(b.kv, 1, b.step, y.cuda(), scale=0.0)
+        assert got[0, 1].isnan().all()
+        keep = torch.ones(b.n, 4, dtype=torch.bool)
+        keep[0, 1] = False
+        assert torch.equal(got[keep.cuda()], ref[keep.cuda()])
