@@ -232,6 +232,8 @@ k_paged_append(PagedView pv, StepView st, RopeView rope, HeadsView k, HeadsView 
     const int page = st.pages[(int64_t)s * st.pages_per_seq + p0 / pv.page_size];
     const bool beyond = p0 + r1 > rope.max_pos;              // rows that are not in the rotary table
     r1 = min(r1, rope.max_pos - p0);
+    if (beyond && threadIdx.x == 0 && st.status) atomicOr(st.status, 1);
+    if (r0 >= r1) return;                                    // none of the group's rows is left
     const int g0 = blockIdx.y * heads, ng = min(heads, pv.n_kv_heads - g0), hd = pv.hd, ps = pv.page_size, nr = r1 - r0;
     const int at0 = p0 % ps;                                 // of the group in its page
     const int64_t row0 = (int64_t)sr.row0 + p0 - first;      // of position p0 (its own row may not exist)
@@ -328,7 +330,7 @@ k_paged_append(PagedView pv, StepView st, RopeView rope, HeadsView k, HeadsView 
             if (mapped) store_row<V>(pool + g * block + page_v<T>(at0 + r, V * u, hd, ps), x);
         }
     }
-    if (threadIdx.x == 0 && st.status && (!mapped || beyond)) atomicOr(st.status, 1);
+    if (threadIdx.x == 0 && st.status && !mapped) atomicOr(st.status, 1);
 }
 
 int launch_paged_append(int dtype, const PagedView& pv, const StepView& st, const RopeView& rope, const HeadsView& k, const HeadsView& v,
