@@ -102,7 +102,12 @@ int ee_rope_create(const ee_rope_config* cfg, ee_rope** out) {
     if (!r) return ee_fail(EE_ERR_INVALID_ARG, "ee_rope_create: out of host memory");
     r->cfg = *cfg;
     hipError_t e = hipMalloc((void**)&r->d_table, (size_t)cfg->max_pos * cfg->rot_dim * sizeof(float));
-    rc = e == hipSuccess ? launch_rope_pairs(r->d_table, r->cfg, nullptr) : ee_fail(EE_ERR_HIP, std::string("ee_rope_create: ") + hipGetErrorString(e));
+    if (e == hipSuccess) {
+        rc = launch_rope_pairs(r->d_table, r->cfg, nullptr);
+    } else {
+        (void)hipGetLastError();                             // reported here: the next launch's check must not find it
+        rc = ee_fail(EE_ERR_HIP, std::string("ee_rope_create: ") + hipGetErrorString(e));
+    }
     if (rc == EE_OK && hipStreamSynchronize(nullptr) != hipSuccess) rc = ee_fail(EE_ERR_HIP, "ee_rope_create: table kernel failed");
     if (rc != EE_OK) {
         ee_rope_destroy(r);
