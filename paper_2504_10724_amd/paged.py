@@ -32,20 +32,20 @@ def _stream(t):
 _pack_heads = struct.Struct("Pqq").pack      # an ee_heads as bytes, a fifth of the time a ctypes structure takes
 
 
-def _heads(t, what, shape, dtype):
-    """ee_heads of a device tensor [n_tokens][n_heads][hd] whose features are contiguous"""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
-        _refuse(f"{what}: expected a device tensor {shape} of {dtype}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+def _heads(t, what, shape, dtype, device):
+    """ee_heads of a tensor [n_tokens][n_heads][hd] on device number `device` whose features are contiguous"""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        _refuse(f"{what}: expected a tensor {tuple(shape)} of {dtype} on device {device}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
     token, head, feature = t.stride()
     if feature != 1 and shape[2] > 1:
         _refuse(f"{what}: the features of a head must be contiguous")
     return _pack_heads(t.data_ptr(), token, head)
 
 
-def _int32(t, what, n):
-    """a contiguous int32 device tensor of n values"""
-    if t.dtype is not torch.int32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
-        _refuse(f"{what}: expected a contiguous int32 device tensor of {n} values, got {t.numel()} of {t.dtype} on {t.device}")
+def _int32(t, what, n, device):
+    """a contiguous int32 tensor of n values on device number `device`"""
+    if t.dtype is not torch.int32 or t.numel() != n or t.get_device() != device or device < 0 or not t.is_contiguous():
+        _refuse(f"{what}: expected a contiguous int32 tensor of {n} values on a device ({device}), got {t.numel()} of {t.dtype} on {t.device}")
     return t
 
 
@@ -60,6 +60,7 @@ class Rope:
         self.lib = ee.load()
         self.cfg = ee.ee_rope_config(head_dim, head_dim if rot_dim is None else rot_dim, _PAIRINGS[pairing], max_pos, _SCALINGS[scaling],
                                      trained_pos, theta, factor, low, high, magnitude)
+        self.device = torch.cuda.current_device()
         self.h = C.c_void_p()
         ee.check(self.lib.ee_rope_create(C.byref(self.cfg), C.byref(self.h)))
 
@@ -75,7 +76,8 @@ class Rope:
             pass
 
     def apply(self, x, pos, *, out=None, inverse=False, status=None):
-        """x [n][heads][head_dim] (float32 or bfloat16, any token and head stride) rotated at pos (int32 [n]); out may be x.
+        """x [n][heads][head_dim] (float32 or bfloat16, any token and head stride, on the table's device) rotated at pos (int32 [n]);
+        out may be x.  A row whose position is outside the table is not written: without `out` it holds what the new tensor's memory held.
         inverse: by the negative angle, which is the gradient with respect to x of a result's gradient."""
         dtype, shape = x.dtype, x.shape
         if len(shape) != 3 or dtype not in _DTYPES or shape[2] != self.cfg.head_dim:
@@ -83,9 +85,10 @@ class Rope:
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=x.device)
         n, heads, _ = shape
-        ee.check(self.lib.ee_rope_apply(self.h, _DTYPES[dtype], _heads(x, "Rope.apply", shape, dtype), _heads(out, "Rope.apply", shape, dtype),
-                                        _int32(pos, "Rope.apply: pos", n).data_ptr(), n, heads, inverse,
-                                        None if status is None else _int32(status, "Rope.apply: status", 1).data_ptr(), _stream(x)))
+        dev = self.device
+        ee.check(self.lib.ee_rope_apply(self.h, _DTYPES[dtype], _heads(x, "Rope.apply", shape, dtype, dev),
+                                        _heads(out, "Rope.apply", shape, dtype, dev), _int32(pos, "Rope.apply: pos", n, dev).data_ptr(), n, heads,
+                                        inverse, None if status is None else _int32(status, "Rope.apply: status", 1, dev).data_ptr(), _stream(x)))
         return out
 
 
@@ -102,6 +105,7 @@ class PagedCache:
         if nbytes == 0:
             raise ee.EEError(ee.EE_ERR_SHAPE, self.lib.ee_last_error().decode())
         self.pool = torch.empty(nbytes // self.dtype.itemsize, dtype=self.dtype, device="cuda")
+        self.device = self.pool.get_device()
         self.h = C.c_void_p()
         ee.check(self.lib.ee_paged_bind(C.byref(self.cfg), self.pool.data_ptr(), nbytes, C.byref(self.h)))
 
@@ -119,29 +123,34 @@ class PagedCache:
     def workspace(self, step, n_q_heads):
         """what attend needs for this step and every step whose host figures are at most its; keep one per stream"""
         nbytes = self.lib.ee_paged_attention_workspace(self.h, n_q_heads, step.ref)
-        return torch.empty(max(nbytes, 1), dtype=torch.uint8, device="cuda")
+        return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.pool.device)
 
 
 class PagedStep:
     """The new rows of one call (see ee_paged_step).  q_start [n_seqs + 1], kv_len [n_seqs] and pages [n_seqs][width] are int32
-    device tensors that the calls read when they run, so a recorded graph sees what they hold at each replay; status (int32 [1])
-    collects refusals."""
+    tensors on the cache's device that the calls read when they run, so a recorded graph sees what they hold at each replay; status
+    (int32 [1]) collects refusals."""
 
     def __init__(self, q_start, kv_len, pages, *, n_tokens, max_q_len, max_kv_len, status=None):
         n = kv_len.numel()
         if pages.dim() != 2 or pages.shape[0] != n:
             _refuse(f"PagedStep: pages must be [{n}][pages per sequence], got {tuple(pages.shape)}")
-        self.tensors = (_int32(q_start, "PagedStep: q_start", n + 1), _int32(kv_len, "PagedStep: kv_len", n),
-                        _int32(pages, "PagedStep: pages", pages.numel()), None if status is None else _int32(status, "PagedStep: status", 1))
+        self.device = dev = kv_len.get_device()
+        self.tensors = (_int32(q_start, "PagedStep: q_start", n + 1, dev), _int32(kv_len, "PagedStep: kv_len", n, dev),
+                        _int32(pages, "PagedStep: pages", pages.numel(), dev),
+                        None if status is None else _int32(status, "PagedStep: status", 1, dev))
         self.c = ee.ee_paged_step(n, n_tokens, max_q_len, max_kv_len, pages.shape[1], *(None if t is None else t.data_ptr() for t in self.tensors))
         self.n_tokens, self.ref = n_tokens, C.byref(self.c)
 
 
 def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
     """Keys (rotated by rope) and values [n_tokens][n_kv_heads][head_dim] to the rows' positions of `layer`; with q
-    [n_tokens][n_q_heads][head_dim] also the rotated queries to q_out (default: a new tensor, which is returned)."""
-    dtype, shape = kv.dtype, (step.n_tokens, kv.n_kv_heads, kv.head_dim)
-    kh, vh = _heads(k, "append", shape, dtype), _heads(v, "append", shape, dtype)
+    [n_tokens][n_q_heads][head_dim] also the rotated queries to q_out (default: a new tensor, which is returned; rows that are left out
+    hold what its memory held).  Everything is on the cache's device."""
+    dtype, shape, dev = kv.dtype, (step.n_tokens, kv.n_kv_heads, kv.head_dim), kv.device
+    if step.device != dev or (rope is not None and rope.device != dev):
+        _refuse(f"append: the step or the rotary table is not on the cache's device ({dev})")
+    kh, vh = _heads(k, "append", shape, dtype, dev), _heads(v, "append", shape, dtype, dev)
     qh = qo = None
     n_q = 0
     if q is not None:
@@ -149,23 +158,28 @@ def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
         shape = (step.n_tokens, n_q, kv.head_dim)
         if q_out is None:
             q_out = torch.empty(shape, dtype=dtype, device=q.device)
-        qh, qo = _heads(q, "append", shape, dtype), _heads(q_out, "append", shape, dtype)
+        qh, qo = _heads(q, "append", shape, dtype, dev), _heads(q_out, "append", shape, dtype, dev)
     ee.check(kv.lib.ee_paged_append(kv.h, layer, step.ref, None if rope is None else rope.h, kh, vh, qh, qo, n_q, _stream(k)))
     return q_out
 
 
 def attend(kv, layer, step, q, *, out=None, scale=None, window=0, workspace=None):
     """Attention of the step's rows q [n_tokens][n_q_heads][head_dim] over the cached positions of `layer`; scale defaults to
-    1/sqrt(head_dim), window 0 is all earlier positions, workspace is kv.workspace's."""
+    1/sqrt(head_dim), window 0 is all earlier positions, workspace is kv.workspace's.  Everything is on the cache's device.  Rows of
+    a sequence outside the step's figures are not written: without `out` they hold what the new tensor's memory held."""
     if q.dim() != 3:
         _refuse(f"attend: q must be [tokens][heads][features], got {tuple(q.shape)}")
     heads = q.shape[1]
-    shape, dtype = (step.n_tokens, heads, kv.head_dim), kv.dtype
+    shape, dtype, dev = (step.n_tokens, heads, kv.head_dim), kv.dtype, kv.device
+    if step.device != dev:
+        _refuse(f"attend: the step is not on the cache's device ({dev})")
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=q.device)
     if workspace is None:
         workspace = kv.workspace(step, heads)
-    ee.check(kv.lib.ee_paged_attention(kv.h, layer, step.ref, _heads(q, "attend", shape, dtype), _heads(out, "attend", shape, dtype), heads,
-                                       kv.head_dim ** -0.5 if scale is None else scale, window, workspace.data_ptr(), workspace.numel(),
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        _refuse(f"attend: expected a contiguous workspace on device {dev}, got one on {workspace.device}")
+    ee.check(kv.lib.ee_paged_attention(kv.h, layer, step.ref, _heads(q, "attend", shape, dtype, dev), _heads(out, "attend", shape, dtype, dev),
+                                       heads, kv.head_dim ** -0.5 if scale is None else scale, window, workspace.data_ptr(), workspace.nbytes,
                                        _stream(q)))
     return out

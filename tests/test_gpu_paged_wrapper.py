@@ -16,3 +16,61 @@ def test_a_table_that_does_not_fit_leaves_no_error_behind():
         P.Rope(256, 2 ** 31 - 1)
     x = torch.zeros(1, 2, 64, device="cuda")
     assert torch.equal(rope.apply(x, torch.zeros(1, dtype=torch.int32, device="cuda")), x)
+
+
+def _i32(v, device="cuda"):
+    return torch.tensor(v, dtype=torch.int32, device=device)
+
+
+class Call:
+    """two sequences of one new row each, 4 query heads of 2 kv heads of 64, more positions than are left whole"""
+
+    def __init__(self):
+        self.kv = P.PagedCache(2, 130, 2, 64, 32)
+        self.kv.pool.zero_()
+        self.tensors = _i32([0, 1, 2]), _i32([2000, 40]), torch.arange(126, dtype=torch.int32, device="cuda").view(2, 63)
+        self.step = P.PagedStep(*self.tensors, n_tokens=2, max_q_len=1, max_kv_len=2000)
+        self.q = torch.ones(2, 4, 64, dtype=torch.bfloat16, device="cuda")
+        self.k = torch.ones(2, 2, 64, dtype=torch.bfloat16, device="cuda")
+        self.need = ee.load().ee_paged_attention_workspace(self.kv.h, 4, self.step.ref)
+
+
+def test_memory_of_another_device_is_refused():
+    """the host's, before a kernel could be given its address"""
+    print("[case] devices", flush=True)
+    c = Call()
+    assert c.need > 0
+    rope = P.Rope(64, 3000)
+    pos = _i32([1, 2])
+    assert c.kv.device == rope.device == c.step.device == c.q.get_device()
+    host_step = [t.cpu() for t in c.tensors]
+    calls = [lambda: P.attend(c.kv, 1, c.step, c.q, workspace=torch.empty(c.need, dtype=torch.uint8)),
+             lambda: P.attend(c.kv, 1, c.step, c.q, workspace=torch.empty(1, dtype=torch.uint8, device="cuda").expand(c.need)),
+             lambda: P.attend(c.kv, 1, c.step, c.q, out=torch.empty_like(c.q, device="cpu")),
+             lambda: P.attend(c.kv, 1, c.step, c.q.cpu()),
+             lambda: P.append(c.kv, 1, c.step, c.k.cpu(), c.k),
+             lambda: P.append(c.kv, 1, c.step, c.k, c.k.cpu()),
+             lambda: P.append(c.kv, 1, c.step, c.k, c.k, q=c.q, q_out=c.q.cpu()),
+             lambda: P.PagedStep(*host_step, n_tokens=2, max_q_len=1, max_kv_len=2000),
+             lambda: P.PagedStep(*c.tensors, n_tokens=2, max_q_len=1, max_kv_len=2000, status=_i32([0], "cpu")),
+             lambda: P.PagedStep(c.tensors[0], c.tensors[1], host_step[2], n_tokens=2, max_q_len=1, max_kv_len=2000),
+             lambda: rope.apply(c.q.cpu(), pos), lambda: rope.apply(c.q, pos.cpu()), lambda: rope.apply(c.q, pos, out=c.q.cpu()),
+             lambda: rope.apply(c.q, pos, status=_i32([0], "cpu"))]
+    for call in calls:
+        with pytest.raises(ee.EEError):
+            call()
+    # devices are compared by number: another one's handles do not pass either
+    for owner in (rope, c.step):
+        owner.device += 1
+        with pytest.raises(ee.EEError):
+            P.append(c.kv, 1, c.step, c.k, c.k, rope=rope)
+        if owner is c.step:
+            with pytest.raises(ee.EEError):
+                P.attend(c.kv, 1, c.step, c.q)
+        else:
+            with pytest.raises(ee.EEError):
+                rope.apply(c.q, pos)
+        owner.device -= 1
+    P.append(c.kv, 1, c.step, c.k, c.k, rope=rope)
+    out = P.attend(c.kv, 1, c.step, c.q)
+    assert torch.equal(P.attend(c.kv, 1, c.step, c.q, workspace=torch.empty((c.need + 3) // 4, dtype=torch.float32, device="cuda")), out)
