@@ -150,6 +150,8 @@ def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
     dtype, shape, dev = kv.dtype, (step.n_tokens, kv.n_kv_heads, kv.head_dim), kv.device
     if step.device != dev or (rope is not None and rope.device != dev):
         _refuse(f"append: the step or the rotary table is not on the cache's device ({dev})")
+    if rope is not None and not rope.h:                      # the library takes no table for no rotation
+        _refuse("append: the rotary table is closed")
     kh, vh = _heads(k, "append", shape, dtype, dev), _heads(v, "append", shape, dtype, dev)
     qh = qo = None
     n_q = 0

@@ -74,3 +74,21 @@ def test_memory_of_another_device_is_refused():
     P.append(c.kv, 1, c.step, c.k, c.k, rope=rope)
     out = P.attend(c.kv, 1, c.step, c.q)
     assert torch.equal(P.attend(c.kv, 1, c.step, c.q, workspace=torch.empty((c.need + 3) // 4, dtype=torch.float32, device="cuda")), out)
+
+
+def test_closed_handles_are_refused():
+    """a closed rotary table is not "no rotation" """
+    print("[case] closed", flush=True)
+    c = Call()
+    rope = P.Rope(64, 3000)
+    rope.close()
+    with pytest.raises(ee.EEError):
+        P.append(c.kv, 1, c.step, c.k, c.k, rope=rope)
+    with pytest.raises(ee.EEError):
+        rope.apply(c.q, _i32([1, 2]))
+    assert not c.kv.pool.any()
+    c.kv.close()
+    with pytest.raises(ee.EEError):
+        P.append(c.kv, 1, c.step, c.k, c.k)
+    with pytest.raises(ee.EEError):
+        P.attend(c.kv, 1, c.step, c.q)
