@@ -49,6 +49,28 @@ def _int32(t, what, n, device):
     return t
 
 
+def _no_graph(what, *tensors):
+    """the operator has no gradient, and a result that the caller provides takes no part in a graph: nothing that needs one gets lost"""
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            _refuse(f"{what}: a tensor requires a gradient that is not computed; call it under torch.no_grad() or on detached tensors")
+
+
+class _Turn(torch.autograd.Function):
+    """Rope.apply in a graph: its gradient is the inverse rotation of the result's.  Rows that are left out are zeros both ways."""
+
+    @staticmethod
+    def forward(ctx, x, pos, rope, inverse, status):
+        ctx.save_for_backward(pos)
+        ctx.rope, ctx.inverse = rope, inverse
+        return rope.apply(x, pos, out=torch.zeros(x.shape, dtype=x.dtype, device=x.device), inverse=inverse, status=status)
+
+    @staticmethod
+    def backward(ctx, g):
+        g = g if g.stride(2) == 1 else g.contiguous()
+        return _Turn.apply(g, *ctx.saved_tensors, ctx.rope, not ctx.inverse, None), None, None, None, None
+
+
 class Rope:
     """A rotary table (see ee_rope_config): rot_dim features of a head turn (default: all), in "half" or "interleaved" pairs,
     at frequencies scaled by "none", "linear", "base" or "bands"."""
@@ -78,11 +100,16 @@ class Rope:
     def apply(self, x, pos, *, out=None, inverse=False, status=None):
         """x [n][heads][head_dim] (float32 or bfloat16, any token and head stride, on the table's device) rotated at pos (int32 [n]);
         out may be x.  A row whose position is outside the table is not written: without `out` it holds what the new tensor's memory held.
-        inverse: by the negative angle, which is the gradient with respect to x of a result's gradient."""
+        inverse: by the negative angle, which is the gradient with respect to x of a result's gradient.  Where x requires a gradient the
+        result has it, and rows outside the table are zeros; `out` is refused there."""
         dtype, shape = x.dtype, x.shape
         if len(shape) != 3 or dtype not in _DTYPES or shape[2] != self.cfg.head_dim:
             _refuse(f"Rope.apply: x must be [tokens][heads][{self.cfg.head_dim}] of float32 or bfloat16, got {tuple(shape)} of {dtype}")
-        if out is None:
+        if out is not None:
+            _no_graph("Rope.apply with out", x, out)
+        elif x.requires_grad and torch.is_grad_enabled():
+            return _Turn.apply(x, pos, self, inverse, status)
+        else:
             out = torch.empty(shape, dtype=dtype, device=x.device)
         n, heads, _ = shape
         dev = self.device
@@ -152,6 +179,7 @@ def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
         _refuse(f"append: the step or the rotary table is not on the cache's device ({dev})")
     if rope is not None and not rope.h:                      # the library takes no table for no rotation
         _refuse("append: the rotary table is closed")
+    _no_graph("append", k, v, q, q_out)
     kh, vh = _heads(k, "append", shape, dtype, dev), _heads(v, "append", shape, dtype, dev)
     qh = qo = None
     n_q = 0
@@ -175,6 +203,7 @@ def attend(kv, layer, step, q, *, out=None, scale=None, window=0, workspace=None
     shape, dtype, dev = (step.n_tokens, heads, kv.head_dim), kv.dtype, kv.device
     if step.device != dev:
         _refuse(f"attend: the step is not on the cache's device ({dev})")
+    _no_graph("attend", q, out)
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=q.device)
     if workspace is None:

@@ -92,3 +92,63 @@ def test_closed_handles_are_refused():
         P.append(c.kv, 1, c.step, c.k, c.k)
     with pytest.raises(ee.EEError):
         P.attend(c.kv, 1, c.step, c.q)
+
+
+@pytest.mark.parametrize("pairing", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_rotation_has_its_gradient(dtype, pairing):
+    """backward gives the inverse rotation of the result's gradient: of any strides, of heads that share their input, of rows that
+    are left out (none), and of a gradient that is differentiated once more"""
+    print(f"[case] gradient {dtype} {pairing}", flush=True)
+    rope = P.Rope(64, 300, rot_dim=32, pairing=pairing, magnitude=0.75)
+    gen = torch.Generator().manual_seed(5)
+    x, g = (torch.randn(7, 6, 64, generator=gen).to(dtype).cuda() for _ in range(2))
+    pos = _i32([0, 5, 299, 17, 17, 3, 250])
+    for inverse in (False, True):
+        leaf = x.clone().requires_grad_()
+        y = rope.apply(leaf, pos, inverse=inverse)
+        assert torch.equal(y, rope.apply(x, pos, inverse=inverse))
+        want = rope.apply(g, pos, inverse=not inverse)
+        assert torch.equal(torch.autograd.grad(y, leaf, g, retain_graph=True)[0], want)
+        wide = g.transpose(1, 2).contiguous().transpose(1, 2)          # features far apart
+        assert torch.equal(torch.autograd.grad(y, leaf, wide)[0], want)
+        leaf.grad = None
+        rope.apply(leaf, pos, inverse=inverse).sum().backward()        # a gradient of one element, broadcast
+        assert torch.equal(leaf.grad, rope.apply(torch.ones_like(x), pos, inverse=not inverse))
+        shared = x[:, :1].clone().requires_grad_()                     # one head's input for all six
+        rope.apply(shared.expand(7, 6, 64), pos, inverse=inverse).backward(g)
+        near = 6 * 6 * (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24)     # a sum of six values of at most 6, rounded each time
+        assert (shared.grad.double()[:, 0] - want.double().sum(1)).abs().max() <= 6 * near
+        once = leaf.detach().requires_grad_()
+        cot = g.clone().requires_grad_()
+        first, = torch.autograd.grad(rope.apply(once, pos, inverse=inverse), once, cot, create_graph=True)
+        second, = torch.autograd.grad(first, cot, x)
+        assert torch.equal(second, rope.apply(x, pos, inverse=inverse))
+    out = torch.tensor([0, 1, 299, 300, -1, 2, 9], dtype=torch.int32, device="cuda")
+    status = _i32([0])
+    torch.full((1 << 20,), float("nan"), device="cuda")                # memory the next results may be given
+    leaf = x.clone().requires_grad_()
+    y = rope.apply(leaf, out, status=status)
+    y[[0, 1, 2, 5, 6]].float().sum().backward()
+    assert status.item() == 1 and (leaf.grad[[3, 4]] == 0).all() and (y[[3, 4]] == 0).all() and not leaf.grad.isnan().any()
+
+
+def test_gradients_that_nothing_computes_are_refused():
+    """a cache is not trained through; results that the caller provides take no part in a graph"""
+    print("[case] no gradient", flush=True)
+    c = Call()
+    rope, pos = P.Rope(64, 3000), _i32([1, 2])
+    q, k = c.q.clone().requires_grad_(), c.k.clone().requires_grad_()
+    calls = [lambda: rope.apply(q, pos, out=torch.empty_like(c.q)), lambda: rope.apply(q, pos, out=q), lambda: rope.apply(c.q, pos, out=q),
+             lambda: P.append(c.kv, 1, c.step, k, c.k), lambda: P.append(c.kv, 1, c.step, c.k, k),
+             lambda: P.append(c.kv, 1, c.step, c.k, c.k, q=q), lambda: P.append(c.kv, 1, c.step, c.k, c.k, q=c.q, q_out=q),
+             lambda: P.attend(c.kv, 1, c.step, q), lambda: P.attend(c.kv, 1, c.step, c.q, out=q)]
+    for call in calls:
+        with pytest.raises(ee.EEError):
+            call()
+    with torch.no_grad():                                              # no graph is built here: they are only tensors
+        P.append(c.kv, 1, c.step, k, k, rope=rope, q=q)
+        ref = P.attend(c.kv, 1, c.step, q)
+        assert not rope.apply(q, pos).requires_grad
+    P.append(c.kv, 1, c.step, c.k, c.k, rope=rope)
+    assert torch.equal(P.attend(c.kv, 1, c.step, c.q), ref)
