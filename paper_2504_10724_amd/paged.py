@@ -29,6 +29,16 @@ def _stream(t):
     return torch.cuda.current_stream(t.device).cuda_stream if _raw_stream is None else _raw_stream(t.get_device())
 
 
+_MOST = 2 ** 31 - 1
+
+
+def _number(what, *values):
+    """the library's counts have 32 bits, and the binding would pass on the lowest 32 of a larger one"""
+    for v in values:
+        if not -_MOST <= v <= _MOST:
+            _refuse(f"{what}: {v} does not fit 32 bits")
+
+
 _pack_heads = struct.Struct("Pqq").pack      # an ee_heads as bytes, a fifth of the time a ctypes structure takes
 
 
@@ -79,6 +89,7 @@ class Rope:
                  low=1.0, high=4.0, magnitude=0.0):
         if pairing not in _PAIRINGS or scaling not in _SCALINGS:
             _refuse(f"Rope: unknown pairing {pairing!r} or scaling {scaling!r}")
+        _number("Rope", head_dim, max_pos, 0 if rot_dim is None else rot_dim, trained_pos)
         self.lib = ee.load()
         self.cfg = ee.ee_rope_config(head_dim, head_dim if rot_dim is None else rot_dim, _PAIRINGS[pairing], max_pos, _SCALINGS[scaling],
                                      trained_pos, theta, factor, low, high, magnitude)
@@ -125,6 +136,7 @@ class PagedCache:
     def __init__(self, n_layers, n_pages, n_kv_heads, head_dim, page_size, dtype="bf16"):
         if dtype not in ("bf16", "f32"):
             raise ee.EEError(ee.EE_ERR_DTYPE, f"PagedCache: unknown dtype {dtype!r}")
+        _number("PagedCache", n_layers, n_pages, n_kv_heads, head_dim, page_size)
         self.lib = ee.load()
         self.cfg = ee.ee_paged_config(n_layers, n_pages, n_kv_heads, head_dim, page_size, ee.EE_BF16 if dtype == "bf16" else ee.EE_F32)
         self.dtype, self.n_kv_heads, self.head_dim = (torch.bfloat16 if dtype == "bf16" else torch.float32), n_kv_heads, head_dim
@@ -162,6 +174,7 @@ class PagedStep:
         n = kv_len.numel()
         if pages.dim() != 2 or pages.shape[0] != n:
             _refuse(f"PagedStep: pages must be [{n}][pages per sequence], got {tuple(pages.shape)}")
+        _number("PagedStep", n_tokens, max_q_len, max_kv_len)
         self.device = dev = kv_len.get_device()
         self.tensors = (_int32(q_start, "PagedStep: q_start", n + 1, dev), _int32(kv_len, "PagedStep: kv_len", n, dev),
                         _int32(pages, "PagedStep: pages", pages.numel(), dev),
@@ -180,6 +193,7 @@ def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
     if rope is not None and not rope.h:                      # the library takes no table for no rotation
         _refuse("append: the rotary table is closed")
     _no_graph("append", k, v, q, q_out)
+    _number("append", layer)
     kh, vh = _heads(k, "append", shape, dtype, dev), _heads(v, "append", shape, dtype, dev)
     qh = qo = None
     n_q = 0
@@ -204,6 +218,8 @@ def attend(kv, layer, step, q, *, out=None, scale=None, window=0, workspace=None
     if step.device != dev:
         _refuse(f"attend: the step is not on the cache's device ({dev})")
     _no_graph("attend", q, out)
+    window = min(window, _MOST)                              # wider than any sequence
+    _number("attend", layer, window)
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=q.device)
     if workspace is None:

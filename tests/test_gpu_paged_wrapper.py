@@ -152,3 +152,22 @@ def test_gradients_that_nothing_computes_are_refused():
         assert not rope.apply(q, pos).requires_grad
     P.append(c.kv, 1, c.step, c.k, c.k, rope=rope)
     assert torch.equal(P.attend(c.kv, 1, c.step, c.q), ref)
+
+
+def test_numbers_beyond_32_bits():
+    """they used to arrive as their lowest 32 bits"""
+    print("[case] 32 bits", flush=True)
+    c = Call()
+    far, huge = 1 << 32, 1 << 40
+    for call in (lambda: P.attend(c.kv, far + 1, c.step, c.q), lambda: P.append(c.kv, far + 1, c.step, c.k, c.k),
+                 lambda: P.attend(c.kv, 1, c.step, c.q, window=-huge + 1),
+                 lambda: P.PagedStep(*c.tensors, n_tokens=far + 2, max_q_len=1, max_kv_len=2000),
+                 lambda: P.PagedStep(*c.tensors, n_tokens=2, max_q_len=far + 1, max_kv_len=2000),
+                 lambda: P.PagedStep(*c.tensors, n_tokens=2, max_q_len=1, max_kv_len=far + 2000),
+                 lambda: P.PagedCache(1, far + 4, 2, 64, 32), lambda: P.PagedCache(far + 1, 4, 2, 64, 32),
+                 lambda: P.PagedCache(1, 4, far + 2, 64, 32), lambda: P.Rope(64, far + 100), lambda: P.Rope(64, 100, rot_dim=far + 64),
+                 lambda: P.Rope(64, 100, scaling="bands", factor=2.0, trained_pos=far + 9)):
+        with pytest.raises(ee.EEError):
+            call()
+    P.append(c.kv, 1, c.step, c.k, c.k)
+    assert torch.equal(P.attend(c.kv, 1, c.step, c.q, window=huge + 1), P.attend(c.kv, 1, c.step, c.q))      # wider than any sequence
