@@ -52,6 +52,15 @@ def _heads(t, what, shape, dtype, device):
     return _pack_heads(t.data_ptr(), token, head)
 
 
+def _result(t, what, shape, dtype, device):
+    """_heads of a tensor that is written: no two of its rows or heads in one place"""
+    heads = _heads(t, what, shape, dtype, device)
+    token, head, _ = t.stride()
+    if (token == 0 and shape[0] > 1) or (head == 0 and shape[1] > 1):
+        _refuse(f"{what}: rows or heads of the result share their memory")
+    return heads
+
+
 def _int32(t, what, n, device):
     """a contiguous int32 tensor of n values on device number `device`"""
     if t.dtype is not torch.int32 or t.numel() != n or t.get_device() != device or device < 0 or not t.is_contiguous():
@@ -125,7 +134,7 @@ class Rope:
         n, heads, _ = shape
         dev = self.device
         ee.check(self.lib.ee_rope_apply(self.h, _DTYPES[dtype], _heads(x, "Rope.apply", shape, dtype, dev),
-                                        _heads(out, "Rope.apply", shape, dtype, dev), _int32(pos, "Rope.apply: pos", n, dev).data_ptr(), n, heads,
+                                        _result(out, "Rope.apply", shape, dtype, dev), _int32(pos, "Rope.apply: pos", n, dev).data_ptr(), n, heads,
                                         inverse, None if status is None else _int32(status, "Rope.apply: status", 1, dev).data_ptr(), _stream(x)))
         return out
 
@@ -202,7 +211,7 @@ def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
         shape = (step.n_tokens, n_q, kv.head_dim)
         if q_out is None:
             q_out = torch.empty(shape, dtype=dtype, device=q.device)
-        qh, qo = _heads(q, "append", shape, dtype, dev), _heads(q_out, "append", shape, dtype, dev)
+        qh, qo = _heads(q, "append", shape, dtype, dev), _result(q_out, "append", shape, dtype, dev)
     ee.check(kv.lib.ee_paged_append(kv.h, layer, step.ref, None if rope is None else rope.h, kh, vh, qh, qo, n_q, _stream(k)))
     return q_out
 
@@ -226,7 +235,7 @@ def attend(kv, layer, step, q, *, out=None, scale=None, window=0, workspace=None
         workspace = kv.workspace(step, heads)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         _refuse(f"attend: expected a contiguous workspace on device {dev}, got one on {workspace.device}")
-    ee.check(kv.lib.ee_paged_attention(kv.h, layer, step.ref, _heads(q, "attend", shape, dtype, dev), _heads(out, "attend", shape, dtype, dev),
+    ee.check(kv.lib.ee_paged_attention(kv.h, layer, step.ref, _heads(q, "attend", shape, dtype, dev), _result(out, "attend", shape, dtype, dev),
                                        heads, kv.head_dim ** -0.5 if scale is None else scale, window, workspace.data_ptr(), workspace.nbytes,
                                        _stream(q)))
     return out

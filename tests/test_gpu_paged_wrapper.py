@@ -171,3 +171,19 @@ def test_numbers_beyond_32_bits():
             call()
     P.append(c.kv, 1, c.step, c.k, c.k)
     assert torch.equal(P.attend(c.kv, 1, c.step, c.q, window=huge + 1), P.attend(c.kv, 1, c.step, c.q))      # wider than any sequence
+
+
+def test_results_whose_rows_share_memory_are_refused():
+    print("[case] shared results", flush=True)
+    c = Call()
+    rope, pos = P.Rope(64, 3000), _i32([1, 2])
+    row, head = c.q[:1].expand(2, 4, 64), c.q[:, :1].expand(2, 4, 64)
+    for out in (row, head):
+        for call in (lambda: rope.apply(c.q, pos, out=out), lambda: rope.apply(out, pos, out=out), lambda: P.attend(c.kv, 1, c.step, c.q, out=out),
+                     lambda: P.append(c.kv, 1, c.step, c.k, c.k, q=c.q, q_out=out)):
+            with pytest.raises(ee.EEError):
+                call()
+        assert torch.equal(rope.apply(out, pos), rope.apply(out.contiguous(), pos))           # read they may be
+    one = c.q[:1]                                                      # a single row shares with nobody, whatever its stride
+    out = torch.empty(4, 64, dtype=one.dtype, device="cuda").as_strided((1, 4, 64), (0, 64, 1))
+    assert torch.equal(rope.apply(one, pos[:1], out=out), rope.apply(one, pos[:1]))
