@@ -24,9 +24,8 @@ def _refuse(what):
     raise ee.EEError(ee.EE_ERR_INVALID_ARG, what)
 
 
-def _stream(t):
-    """handle of the current stream of a tensor's device (a fifth of the time the way through the current device takes)"""
-    return torch.cuda.current_stream(t.device).cuda_stream if _raw_stream is None else _raw_stream(t.get_device())
+# handle of the current stream of a device, by its number (a fifth of the time the way through the current device takes)
+_stream = _raw_stream or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 _MOST = 2 ** 31 - 1
@@ -42,23 +41,17 @@ def _number(what, *values):
 _pack_heads = struct.Struct("Pqq").pack      # an ee_heads as bytes, a fifth of the time a ctypes structure takes
 
 
-def _heads(t, what, shape, dtype, device):
-    """ee_heads of a tensor [n_tokens][n_heads][hd] on device number `device` whose features are contiguous"""
+def _heads(t, what, shape, dtype, device, written=False):
+    """ee_heads of a tensor [n_tokens][n_heads][hd] on device number `device` whose features are contiguous; of one that is written, no
+    two rows or heads in one place"""
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
         _refuse(f"{what}: expected a tensor {tuple(shape)} of {dtype} on device {device}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
     token, head, feature = t.stride()
     if feature != 1 and shape[2] > 1:
         _refuse(f"{what}: the features of a head must be contiguous")
-    return _pack_heads(t.data_ptr(), token, head)
-
-
-def _result(t, what, shape, dtype, device):
-    """_heads of a tensor that is written: no two of its rows or heads in one place"""
-    heads = _heads(t, what, shape, dtype, device)
-    token, head, _ = t.stride()
-    if (token == 0 and shape[0] > 1) or (head == 0 and shape[1] > 1):
+    if written and not (token and head) and ((token == 0 and shape[0] > 1) or (head == 0 and shape[1] > 1)):
         _refuse(f"{what}: rows or heads of the result share their memory")
-    return heads
+    return _pack_heads(t.data_ptr(), token, head)
 
 
 def _int32(t, what, n, device):
@@ -68,11 +61,9 @@ def _int32(t, what, n, device):
     return t
 
 
-def _no_graph(what, *tensors):
+def _lost(what):
     """the operator has no gradient, and a result that the caller provides takes no part in a graph: nothing that needs one gets lost"""
-    for t in tensors:
-        if t is not None and t.requires_grad and torch.is_grad_enabled():
-            _refuse(f"{what}: a tensor requires a gradient that is not computed; call it under torch.no_grad() or on detached tensors")
+    _refuse(f"{what}: a tensor requires a gradient that is not computed; call it under torch.no_grad() or on detached tensors")
 
 
 class _Turn(torch.autograd.Function):
@@ -126,7 +117,8 @@ class Rope:
         if len(shape) != 3 or dtype not in _DTYPES or shape[2] != self.cfg.head_dim:
             _refuse(f"Rope.apply: x must be [tokens][heads][{self.cfg.head_dim}] of float32 or bfloat16, got {tuple(shape)} of {dtype}")
         if out is not None:
-            _no_graph("Rope.apply with out", x, out)
+            if (x.requires_grad or out.requires_grad) and torch.is_grad_enabled():
+                _lost("Rope.apply with out")
         elif x.requires_grad and torch.is_grad_enabled():
             return _Turn.apply(x, pos, self, inverse, status)
         else:
@@ -134,8 +126,8 @@ class Rope:
         n, heads, _ = shape
         dev = self.device
         ee.check(self.lib.ee_rope_apply(self.h, _DTYPES[dtype], _heads(x, "Rope.apply", shape, dtype, dev),
-                                        _result(out, "Rope.apply", shape, dtype, dev), _int32(pos, "Rope.apply: pos", n, dev).data_ptr(), n, heads,
-                                        inverse, None if status is None else _int32(status, "Rope.apply: status", 1, dev).data_ptr(), _stream(x)))
+                                        _heads(out, "Rope.apply", shape, dtype, dev, True), _int32(pos, "Rope.apply: pos", n, dev).data_ptr(), n, heads,
+                                        inverse, None if status is None else _int32(status, "Rope.apply: status", 1, dev).data_ptr(), _stream(dev)))
         return out
 
 
@@ -149,6 +141,7 @@ class PagedCache:
         self.lib = ee.load()
         self.cfg = ee.ee_paged_config(n_layers, n_pages, n_kv_heads, head_dim, page_size, ee.EE_BF16 if dtype == "bf16" else ee.EE_F32)
         self.dtype, self.n_kv_heads, self.head_dim = (torch.bfloat16 if dtype == "bf16" else torch.float32), n_kv_heads, head_dim
+        self.scale = head_dim ** -0.5
         nbytes = self.lib.ee_paged_pool_bytes(C.byref(self.cfg))
         if nbytes == 0:
             raise ee.EEError(ee.EE_ERR_SHAPE, self.lib.ee_last_error().decode())
@@ -201,8 +194,10 @@ def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
         _refuse(f"append: the step or the rotary table is not on the cache's device ({dev})")
     if rope is not None and not rope.h:                      # the library takes no table for no rotation
         _refuse("append: the rotary table is closed")
-    _no_graph("append", k, v, q, q_out)
-    _number("append", layer)
+    if not -_MOST <= layer <= _MOST:
+        _number("append", layer)
+    if (k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
+        _lost("append")
     kh, vh = _heads(k, "append", shape, dtype, dev), _heads(v, "append", shape, dtype, dev)
     qh = qo = None
     n_q = 0
@@ -211,8 +206,10 @@ def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
         shape = (step.n_tokens, n_q, kv.head_dim)
         if q_out is None:
             q_out = torch.empty(shape, dtype=dtype, device=q.device)
-        qh, qo = _heads(q, "append", shape, dtype, dev), _result(q_out, "append", shape, dtype, dev)
-    ee.check(kv.lib.ee_paged_append(kv.h, layer, step.ref, None if rope is None else rope.h, kh, vh, qh, qo, n_q, _stream(k)))
+        if (q.requires_grad or q_out.requires_grad) and torch.is_grad_enabled():
+            _lost("append")
+        qh, qo = _heads(q, "append", shape, dtype, dev), _heads(q_out, "append", shape, dtype, dev, True)
+    ee.check(kv.lib.ee_paged_append(kv.h, layer, step.ref, None if rope is None else rope.h, kh, vh, qh, qo, n_q, _stream(dev)))
     return q_out
 
 
@@ -226,16 +223,18 @@ def attend(kv, layer, step, q, *, out=None, scale=None, window=0, workspace=None
     shape, dtype, dev = (step.n_tokens, heads, kv.head_dim), kv.dtype, kv.device
     if step.device != dev:
         _refuse(f"attend: the step is not on the cache's device ({dev})")
-    _no_graph("attend", q, out)
-    window = min(window, _MOST)                              # wider than any sequence
-    _number("attend", layer, window)
+    if not (-_MOST <= layer <= _MOST and -_MOST <= window <= _MOST):
+        _number("attend", layer, min(window, _MOST))
+        window = _MOST                                       # wider than any sequence
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=q.device)
+    if (q.requires_grad or out.requires_grad) and torch.is_grad_enabled():
+        _lost("attend")
     if workspace is None:
         workspace = kv.workspace(step, heads)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         _refuse(f"attend: expected a contiguous workspace on device {dev}, got one on {workspace.device}")
-    ee.check(kv.lib.ee_paged_attention(kv.h, layer, step.ref, _heads(q, "attend", shape, dtype, dev), _result(out, "attend", shape, dtype, dev),
-                                       heads, kv.head_dim ** -0.5 if scale is None else scale, window, workspace.data_ptr(), workspace.nbytes,
-                                       _stream(q)))
+    ee.check(kv.lib.ee_paged_attention(kv.h, layer, step.ref, _heads(q, "attend", shape, dtype, dev), _heads(out, "attend", shape, dtype, dev, True),
+                                       heads, kv.scale if scale is None else scale, window, workspace.data_ptr(), workspace.nbytes,
+                                       _stream(dev)))
     return out

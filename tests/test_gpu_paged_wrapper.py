@@ -159,7 +159,8 @@ def test_numbers_beyond_32_bits():
     print("[case] 32 bits", flush=True)
     c = Call()
     far, huge = 1 << 32, 1 << 40
-    for call in (lambda: P.attend(c.kv, far + 1, c.step, c.q), lambda: P.append(c.kv, far + 1, c.step, c.k, c.k),
+    for call in (lambda: P.attend(c.kv, far + 1, c.step, c.q), lambda: P.attend(c.kv, 1 - far, c.step, c.q), lambda: P.append(c.kv, 1 - far, c.step, c.k, c.k),
+                 lambda: P.append(c.kv, far + 1, c.step, c.k, c.k),
                  lambda: P.attend(c.kv, 1, c.step, c.q, window=-huge + 1),
                  lambda: P.PagedStep(*c.tensors, n_tokens=far + 2, max_q_len=1, max_kv_len=2000),
                  lambda: P.PagedStep(*c.tensors, n_tokens=2, max_q_len=far + 1, max_kv_len=2000),
