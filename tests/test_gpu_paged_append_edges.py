@@ -38,3 +38,59 @@ def test_rows_that_all_lie_past_the_rotary_table(dtype, odd):
         assert ((q_out.cpu()[inside].double() - wq).abs() <= near * wq.abs() + 8 * U * 8).all()
         assert (q_out.cpu()[~inside] == 9.0).all()
         assert b.status.item() == 1
+
+
+# ------------------------------------------------------------------ more than 32 MB: rows are read and written past the caches
+@pytest.mark.parametrize("dtype,n,heads,hd,rot", [("bf16", 1003, 67, 128, 128), ("bf16", 1511, 60, 96, 48), ("f32", 1003, 67, 64, 64),
+                                                  ("f32", 1201, 33, 128, 32)])
+@pytest.mark.parametrize("pairing", ["half", "interleaved"])
+def test_rotation_of_more_than_the_caches_hold(dtype, n, heads, hd, rot, pairing):
+    print(f"[case] large rotation {dtype} {n} x {heads} x {hd} {pairing}", flush=True)
+    assert 4 * n * heads * hd * (1 if dtype == "bf16" else 2) > 32e6
+    rope = P.Rope(hd, 5000, rot_dim=rot, pairing=pairing)
+    x = _randn((n, heads, hd), torch.bfloat16 if dtype == "bf16" else torch.float32, 41)
+    pos = torch.randint(0, 5000, (n,), generator=torch.Generator().manual_seed(42), dtype=torch.int32)
+    for inverse in (False, True):
+        want = R.rotate(x, pos, rot, pairing, 1.0, inverse)
+        tol = (2.0 ** -8 * want.abs() if dtype == "bf16" else 0.0) + 8 * U * x.abs().double().amax()
+        for pads in ((0, 0, 0), (16, 8, 8)):
+            xd = _strided(x, *pads)
+            got = rope.apply(xd, pos.cuda(), inverse=inverse)
+            assert ((got.cpu().double() - want).abs() <= tol).all()
+            rope.apply(xd, pos.cuda(), out=xd, inverse=inverse)        # in place: the same bits
+            assert torch.equal(xd, got)
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,hd,rot", [("bf16", 64, 8, 128, 128), ("bf16", 60, 10, 96, 48), ("f32", 32, 16, 64, 64), ("f32", 30, 6, 84, 42)])
+@pytest.mark.parametrize("pairing", ["half", "interleaved"])
+@pytest.mark.parametrize("form", ["chunks", "singles"])
+def test_append_of_more_than_the_caches_hold(dtype, hq, hkv, hd, rot, pairing, form):
+    print(f"[case] large append {dtype} {hq} {hkv} {hd} {pairing} {form}", flush=True)
+    n = -(-33_000_000 // (4 * (hq + 2 * hkv) * hd * (1 if dtype == "bf16" else 2)))
+    if form == "chunks":
+        seqs = [(n // 2, n // 2 + 45), (1, 64), (n // 3, n // 3), (1, 1)]
+        seqs.append((n - sum(r for r, _ in seqs), n))
+    else:
+        seqs = [(1, 1 + 37 * s % 101) for s in range(n)]
+    b = Batch(seqs, hq, hkv, hd, 32, dtype)
+    assert 4 * b.n * (hq + 2 * hkv) * hd * (1 if dtype == "bf16" else 2) > 32e6
+    x = b.fill()
+    rows = _randn((b.n, hq + 2 * hkv, hd), b.dt, 43)
+    q, k, v = rows[:, :hq], rows[:, hq:hq + hkv], rows[:, hq + hkv:]
+    dev = rows.cuda()
+    rope = P.Rope(hd, max(length for _, length in seqs), rot_dim=rot, pairing=pairing)
+    pos = torch.tensor([length - r + j for r, length in seqs for j in range(r)])
+    pages = torch.tensor([b.pages[s][(length - r + j) // 32] for s, (r, length) in enumerate(seqs) for j in range(r)])
+    turned_q, turned_k = R.rotate(q, pos, rot, pairing), R.rotate(k, pos, rot, pairing)
+    near = 2.0 ** -8 if dtype == "bf16" else 0.0
+    wrote = torch.zeros(b.n_pages, 32, dtype=torch.bool)
+    wrote[pages, pos % 32] = True
+    for in_place in (False, True):
+        b.put(x)
+        q_out = P.append(b.kv, 1, b.step, dev[:, hq:hq + hkv], dev[:, hq + hkv:], rope=rope, q=dev[:, :hq], q_out=dev[:, :hq] if in_place else None)
+        got = b.get()[:, 0].transpose(2, 3)                            # [2][page][ps][hkv][hd]
+        assert ((q_out.cpu().double() - turned_q).abs() <= near * turned_q.abs() + 64 * U).all()
+        assert ((got[0, pages, pos % 32].double() - turned_k).abs() <= near * turned_k.abs() + 64 * U).all()
+        assert torch.equal(got[1, pages, pos % 32], v)
+        assert torch.equal(got[:, ~wrote], x[:, 0].transpose(2, 3)[:, ~wrote])
+    assert b.status.item() == 0
