@@ -149,14 +149,14 @@ k_f32_paged(AttnArgs a, int n_slots) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) q[j][k][e] = p[j][feature(k) + e];
     }
+    if constexpr (!WHOLE) {                                  // zeros beyond hd: what was loaded there may be an infinity
 #pragma unroll
-    for (int j = 0; j < CB; ++j)
+        for (int j = 0; j < CB; ++j)
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-            const bool there = col.hi[j] >= 0 && (WHOLE || 16 * k + 4 * gq < hd);
+            for (int k = 0; k < HD / 16; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) q[j][k][e] = there ? q[j][k][e] : 0.f;
-        }
+                for (int e = 0; e < 4; ++e) q[j][k][e] = 16 * k + 4 * gq < hd ? q[j][k][e] : 0.f;
+    }
     auto run = [&](auto edge, int from, int to) {
         for (int i = from; i < to; ++i) {
             if ((i & 63) == 0 && i > 0) look_up(i);
