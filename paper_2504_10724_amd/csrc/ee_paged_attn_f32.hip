@@ -153,9 +153,11 @@ k_f32_paged(AttnArgs a, int n_slots) {
 #pragma unroll
         for (int j = 0; j < CB; ++j)
 #pragma unroll
-            for (int k = 0; k < HD / 16; ++k)
+            for (int k = 0; k < HD / 16; ++k) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) q[j][k][e] = 16 * k + 4 * gq < hd ? q[j][k][e] : 0.f;
+                asm volatile("" : "+v"(q[j][k]));            // settled here: no mask or load is kept for the loop
+            }
     }
     auto run = [&](auto edge, int from, int to) {
         for (int i = from; i < to; ++i) {
