@@ -131,17 +131,18 @@ template <int NK, int CB, int PARTS> struct Columns : ColumnState<2 * NK, CB> { 
         if constexpr (EDGE) {
             weigh_edge<H0, N>(vf, P, pg, min_lo, max_hi, window);
         } else {
-#pragma unroll
-            for (int hb = 0; hb < N; ++hb) weigh(H0 + hb, vf[hb], P);
+            weigh<H0, N>(vf, P);
         }
     }
 
-    // O += V^T P^T of the 16 features of block hb
-    __device__ __forceinline__ void weigh(int hb, uint4 v, const Probs& P) {
+    // O += V^T P^T of the 16 features of each of N blocks from H0 on.  Parts outside: a sum's next product is not its last one's neighbour
+    template <int H0, int N> __device__ __forceinline__ void weigh(const uint4 (&v)[N], const Probs& P) {
 #pragma unroll
         for (int part = 0; part < PARTS; ++part)
 #pragma unroll
-            for (int j = 0; j < CB; ++j) O[j][hb] = mfma(v, P.part[part][j], O[j][hb]);
+            for (int hb = 0; hb < N; ++hb)
+#pragma unroll
+                for (int j = 0; j < CB; ++j) O[j][H0 + hb] = mfma(v[hb], P.part[part][j], O[j][H0 + hb]);
     }
 
     // The same where some column does not see all positions.  A probability of zero does not keep an infinity or NaN among the
@@ -160,8 +161,10 @@ template <int NK, int CB, int PARTS> struct Columns : ColumnState<2 * NK, CB> { 
             any |= odd_bits(v.x) | odd_bits(v.y) | odd_bits(v.z) | odd_bits(v.w);
         }
         if (__builtin_expect(!__any(any != 0), 1)) {
+            uint4 v[N];
 #pragma unroll
-            for (int hb = 0; hb < N; ++hb) weigh(H0 + hb, inside(vf[hb]), P);
+            for (int hb = 0; hb < N; ++hb) v[hb] = inside(vf[hb]);
+            weigh<H0, N>(v, P);
             return;
         }
 #pragma unroll
@@ -179,7 +182,11 @@ template <int NK, int CB, int PARTS> struct Columns : ColumnState<2 * NK, CB> { 
                 neg[i] = odd & ~frac & sign & 0x3f803f80u;
                 pos[i] = odd & ~frac & ~sign & 0x3f803f80u;
             }
-            weigh(H0 + hb, make_uint4(fin[0], fin[1], fin[2], fin[3]), P);
+            const uint4 finite = make_uint4(fin[0], fin[1], fin[2], fin[3]);
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                for (int j = 0; j < CB; ++j) O[j][H0 + hb] = mfma(finite, P.part[part][j], O[j][H0 + hb]);
             const uint4 vp = make_uint4(pos[0], pos[1], pos[2], pos[3]), vn = make_uint4(neg[0], neg[1], neg[2], neg[3]),
                         vx = make_uint4(nan[0], nan[1], nan[2], nan[3]),
                         va = make_uint4(pos[0] | neg[0] | nan[0], pos[1] | neg[1] | nan[1], pos[2] | neg[2] | nan[2], pos[3] | neg[3] | nan[3]);
