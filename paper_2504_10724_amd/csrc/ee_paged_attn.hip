@@ -381,7 +381,9 @@ template <int N, bool ONCE> __device__ __forceinline__ void load_kib(const char*
 // exponentials of 8 cycles, the others of 2 to 5) and 16 reads of LDS, and of two waves one hides a part of what the other does: MFMAs are busy
 // half of the cycles, at 1.95 GHz of 2.4.  1023 rows after 30000 positions, 32 heads of 128 each with a kv head (0.51 TFLOP): 488 us with the
 // join, 1050 TFLOP/s, where a large matrix product reaches 1198; with one group a step 523; where the waves with MFMAs do not go first
-// (s_setprio) 5 % more.  Four prompts of 1900-2048 rows, 64 heads of 8 kv heads (0.26 TFLOP): 318, with one group a step 368.
+// (s_setprio) 5 % more.  Four prompts of 1900-2048 rows, 64 heads of 8 kv heads (0.26 TFLOP): 312, with one group a step 368.  Tiles of 128
+// columns of 128-wide heads have no register left: five 8-byte values a lane are stored before the loop of whole groups and read after it
+// (10 KB a tile, 41 MB of these prompts), a few more in the branch for non-finite values.
 template <int NK, int CB, bool ROWS>
 __global__ void __launch_bounds__(256, 2)
 k_bf16_paged_tile(AttnArgs a, int n_slots, unsigned n_tiles) {
@@ -685,17 +687,21 @@ k_paged_join(AttnArgs a, int C, int n_slots, int n_tiles, int cols) {
 
 // ------------------------------------------------------------------ host side
 // Who serves what, and in how many shares.  From the host's figures alone: the device's are not known here.
-// The join of shares is a launch of its own and takes 4 to 5 us, what 48 groups take four waves that share them: up to those nothing is
-// split.  Beyond, there should be two workgroups a CU.  Measured (us, one token a row): 16 rows of 512-2048 positions (70B shape, 128
+// The join of shares is a launch of its own and takes 4 to 5 us, what 48 groups take four waves that share them: up to those the streaming
+// kernel (STREAMED) and many tiles of 128 columns are not split.  Beyond, there should be two workgroups a CU.  Measured (us, one token a row): 16 rows of 512-2048 positions (70B shape, 128
 // pairs of row and kv head) in shares of 8 groups 24.2, of 16 21.8; 64 rows (512 pairs) split 64.9, whole 56.7; one row of 1000 positions
 // split 10.2, whole 9.0; two rows of 20000 (4 pairs), shares of 8 groups 19.7, of 16 16.6.  Tiles of 128 columns pay more for the join
 // and gain from having a CU to themselves: two chunks of 600 rows (16 heads of 4 kv heads) split beyond 48 groups 39, beyond 24 47.
 // Where one tile holds any sequence, every wave works on every group and there are few columns to join: 8 rows of 2000 positions with
 // 20 heads of one kv head, shares of 16 groups beyond 48 groups 19.3, of 8 beyond 24 13.2.  So it is where there are few tiles: 100 rows after
 // 2000 positions, 4 heads of 2 kv heads (8 tiles), 23.4 and 18.8; three prompts of 900-1200 rows of the same heads (up to 114 tiles) 28.8 and 32.5.
+// Around the 96 tiles that divide the two (16 heads of 4 kv heads, split beyond 48 and beyond 24): one chunk of 600 rows after 600 positions (76
+// tiles) 31.4 and 28.5, of 700 (88) 33.8 and 32.0, of 800 (104) 35.3 and 33.5; two of 200 rows after 700 (56) 25.3 and 22.6, of 300 (80) 28.0
+// and 30.0, of 400 (108) 29.4 and 34.6.
 // Wide heads (256 features): one row of 1500 positions, 16 heads of 2 kv heads, shares of 16 beyond 48 17.6, of 8 beyond 24 13.4, of 6 beyond 16
 // 13.3; 16 rows of 700-1400 28, 17, 15.5; 4 x 4-10 rows after 400-935 (16 tiles) 25.7, 25.7, 20.0; two chunks of 300 rows after 800 (152 tiles)
-// 37, 45, 45.
+// 37, 45, 45.  Around their 128 tiles (beyond 48 and beyond 16): one chunk of 400 rows after 600 positions (102) 33.3 and 29.6, of 480 (122) 35.3
+// and 36.4, of 560 (142) 37.5 and 34.8, of 640 (162) 39.5 and 40.3.
 // fp32: a group costs four times the MFMA time and twice the bytes: one row of 1975 positions, 6 heads of 84 (2 kv heads), shares of 16 beyond
 // 48 groups 25.1, of 8 beyond 16 18.4, of 4 beyond 16 16.3, beyond 8 the same; one row of 300 positions split 16.5, whole 15.0.
 Split split_groups(int64_t blocks, int groups, SplitRule rule) {

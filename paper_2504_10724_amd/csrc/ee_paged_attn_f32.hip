@@ -87,10 +87,13 @@ template <int HD, int CB> struct ColumnsF32 : ColumnState<HD / 16, CB> {
 // memory into registers, and join their sums through LDS.  The keys and values of a group are asked for at once: one trip to memory a
 // group and wave instead of three (one row of 1975 positions, 6 heads of 84: 43 -> 25 us before the finer shares; 64 rows of 1000 positions, 4
 // heads of 256 with 2 kv heads: 106 -> 57).  Heads of 132 to 252 features do not have the registers for both halves of the keys (64 rows of
-// 1000 positions, heads of 200: 85 with halves, 125 without).  Asking for the next group as well, while one is worked on, was no faster.
-// WHOLE: the heads are HD wide, else less.  Two waves a SIMD where that does not spill: 4 prompts of 1000 rows, 6 heads of 84: 133 with two
-// waves, 123 with one; 64 rows of 1000 positions, heads of 128: 48.6 with two, 51.7 with one.
-// 64 single rows over 2000 positions, 4 heads of 64 (4 kv heads): 47 us, 5.6 TB/s; four prompts of 1000 rows of the same heads: 46 us, 45
+// 1000 positions, heads of 200: 76 with halves, 125 without); 38 of their registers are spilled, and some come back between the products of a
+// group.  Asking for the next group as well, while one is worked on, was no faster.
+// WHOLE: the heads are HD wide, else less.  Two waves a SIMD for heads of up to 64 and of 128: 4 prompts of 1000 rows, 6 heads of 84: 133 us
+// with two waves, 123 with one; 64 rows of 1000 positions, heads of 128: 48.6 with two, 51.7 with one; 4 prompts of 1000 rows, 4 heads of
+// 64 (32 columns): 44.8 with two, though 92 registers are spilled in the branch for non-finite values (nowhere else), 47.1 with one; heads
+// of 48, where a dozen of 175 spilled ones lie outside that branch, 46.4 and 45.0.
+// 64 single rows over 2000 positions, 4 heads of 64 (4 kv heads): 47 us, 5.6 TB/s; four prompts of 1000 rows of the same heads: 45 us, 46
 // TFLOP/s of 154: with 16 or 32 columns a workgroup the keys of a sequence come from L2 once for each of them.
 template <int HD, int CB, bool WHOLE>
 __global__ void __launch_bounds__(256, HD <= 64 || (HD == 128 && WHOLE) ? 2 : 1)

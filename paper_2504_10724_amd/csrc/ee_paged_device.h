@@ -18,12 +18,6 @@ template <> __device__ __forceinline__ int page_v<bf16_t>(int p, int i, int hd, 
     return (p >> 5) * 64 * hd + 32 * hd + (((i >> 4) * 4 + ((r & 15) >> 2)) * 16 + (i & 15)) * 8 + ((r >> 4) << 2) + (r & 3);
 }
 
-__device__ __forceinline__ float to_f32(float v) { return v; }
-__device__ __forceinline__ float to_f32(bf16_t v) { return bf16_to_f32(v); }
-template <class T> __device__ __forceinline__ T from_f32(float v);
-template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float v) { return f32_to_bf16(v); }
-
 // V consecutive elements as fp32: one 16-byte access where V elements are 16 bytes, else one by one (V = 1)
 template <int V> __device__ __forceinline__ void load_row(const float* p, float (&x)[V]) {
     if constexpr (V == 4) {
