@@ -96,8 +96,8 @@ __device__ __forceinline__ uint32_t seen_by_lane(uint32_t group) {
 }
 __device__ __forceinline__ uint32_t bit_mask(uint32_t bits, int i) { return (uint32_t)((int)(bits << (31 - i)) >> 31); }
 // The softmax of CB blocks of 16 columns: lane (n16, gq) of a wave holds column n16 of a block and, of a group of 32 positions, the
-// positions 16 b + 4 gq + r.  NO sums of four features a lane and block, which the kernel's second product adds to.
-template <int NO, int CB> struct ColumnState {
+// positions 16 b + 4 gq + r.  NO sums of four features a lane and block, which the kernel's second product adds to.  HEADROOM: see exponents.
+template <int NO, int CB, int HEADROOM> struct ColumnState {
     int   hi[CB];                  // the last position the lane's column sees (-1: none); the first is lowest_seen(hi, window)
     float neg[CB], lim[CB], l[CB]; // minus the exponents' reference (log2 units); 0, or -inf while there is none; the lane's part of the sum
     uint32_t seen;                 // bit j: the column of block j has seen a position
@@ -127,7 +127,9 @@ template <int NO, int CB> struct ColumnState {
     // range as long as the values' own sums do, in whatever order the scores come.  A lane looks at its own scores only; the four lanes of
     // a column meet when one of the wave's references has to move.  Then the exponents move by the same step: they cost a second rounding
     // of relative 2^-24, and the scores need not stay in registers.
-    static constexpr float HEADROOM = 8.0f;
+    // An exponent is rounded as a number of the size of HEADROOM: with 8 a probability is off by up to 2^-21.5 of it, which bf16 does not show;
+    // fp32 takes 1 (2^-24.5).  Four fp32 prompts of 1000 rows, 6 heads of 84: 121.7 us with 1 as with 4, 122 with 8, 126.9 with 0, where the
+    // reference moves for every larger score.
     template <bool EDGE, int NG>
     __device__ __forceinline__ void exponents(const floatx4 (&S)[NG][CB][2], float (&x)[NG][CB][8], float scale2, int pg, int window) {
         static_assert(!EDGE || NG == 1, "groups that not all columns see come one by one");
@@ -168,7 +170,7 @@ template <int NO, int CB> struct ColumnState {
         if (__builtin_expect(__any(raise), 0)) {
 #pragma unroll
             for (int j = 0; j < CB; ++j) {
-                const float t = quad_max(top[j]), by = t + HEADROOM;
+                const float t = quad_max(top[j]), by = t + (float)HEADROOM;
                 const bool up = t > lim[j];
                 const float to = up ? neg[j] - by : neg[j];
                 float alpha = __builtin_amdgcn_exp2f(to - neg[j]);

@@ -6,7 +6,7 @@
 // leave their registers.  Lane (n16, gq) holds column n16 of a block of 16 and, of a group, the positions 16 b + 4 gq + r.
 //
 // Softmax: one pass, running reference and sum in fp32 (log2 units).  The reference lies 8 above the largest score it was set for, and
-// sums are rescaled only when a score exceeds it, which is rare: probabilities stay between 0 and 1 and lose no bit in bf16 or fp32
+// sums are rescaled only when a score exceeds it, which is rare: probabilities stay between 0 and 1 and lose no bit that bf16 shows
 // (below 2^-118 of the largest they become 0).  The sum of the row takes them unrounded.  Into the second product they go as a pair of
 // bf16 (off by 2^-16) where the cache's bytes bound the call and the MFMAs idle (few columns: 214 us, 6.2 TB/s, with one and with two),
 // as one bf16 (2^-8 each, as the values they weigh were) in the tiles, whose MFMAs and softmax set the time: with pairs 1023 rows after
@@ -37,8 +37,8 @@ __device__ __forceinline__ uint32_t half_mask(uint32_t bits) { bits >>= 15; retu
 // ------------------------------------------------------------------ the columns of a wave
 // CB blocks of 16 columns of a (sequence, kv head), and what the softmax and the second product keep for them; a probability is PARTS bf16
 template <int CB, int PARTS> struct Probabilities { uint4 part[PARTS][CB]; };
-template <int NK, int CB, int PARTS> struct Columns : ColumnState<2 * NK, CB> {       // O[j][hb][r]: feature 16 hb + 4 gq + r
-    using State = ColumnState<2 * NK, CB>;
+template <int NK, int CB, int PARTS> struct Columns : ColumnState<2 * NK, CB, 8> {       // O[j][hb][r]: feature 16 hb + 4 gq + r
+    using State = ColumnState<2 * NK, CB, 8>;
     using State::hi; using State::O;
     using Probs = Probabilities<CB, PARTS>;
     uint4 q[CB][NK];

@@ -15,8 +15,8 @@ __device__ __forceinline__ floatx4 mfma(float a, float b, floatx4 c) { return __
 __device__ __forceinline__ floatx4 features(const float* row, int f, int hd) { return *reinterpret_cast<const floatx4*>(row + (f < hd ? f : 0)); }
 
 // O[j][4 c + e][r]: feature 64 c + 16 gq + 4 r + e
-template <int HD, int CB> struct ColumnsF32 : ColumnState<HD / 16, CB> {
-    using State = ColumnState<HD / 16, CB>;
+template <int HD, int CB> struct ColumnsF32 : ColumnState<HD / 16, CB, 1> {
+    using State = ColumnState<HD / 16, CB, 1>;
     using State::hi; using State::O;
 
     // values v[4 b + r][c] (of positions 16 b + 4 gq + r), probabilities P[j][4 b + r]

@@ -76,3 +76,27 @@ def test_a_scale_of_zero_does_not_hide_what_the_queries_hold(dtype, rows):
         keep = torch.ones(b.n, 4, dtype=torch.bool)
         keep[0, 1] = False
         assert torch.equal(got[keep.cuda()], ref[keep.cuda()])
+
+
+@pytest.mark.parametrize("rows,n_seqs", [(1, 64), (40, 3)])
+def test_fp32_weights_of_scores_close_together(rows, n_seqs):
+    """Values are rows of the identity, so that a result is the row's weights.  Scores of one product, at most 0.07 in log2 units: an
+    exponent is off by a few hundredths of a rounding, the hardware's 2^x and 1/x by one unit in the last place each (2 U; as a random
+    rounding 2 U / sqrt 3), the sum of 64 weights by its seven levels of U / sqrt 3 at most, the last product by one: root mean square
+    sqrt(2 * 4/3 + 8/3) U = 2.31 U.  An exponent that was rounded at a size of 8 would add 2^-21 ln 2 / sqrt 3 = 3.2 U."""
+    print(f"[case] close scores {rows} rows", flush=True)
+    b = Batch([(rows, 64)] * n_seqs, 4, 2, 64, 32, "f32")
+    x, q = torch.zeros(2, 1, b.n_pages, 2, 32, 64), torch.zeros(b.n, 4, 64)
+    gen = torch.Generator().manual_seed(7)
+    q[..., 0] = torch.rand(b.n, 4, generator=gen) * 0.2 - 0.1
+    for table in b.pages:
+        for i, page in enumerate(table):
+            x[0, 0, page, :, :, 0] = torch.rand(2, 32, generator=gen) - 0.5
+            x[1, 0, page] = torch.eye(64)[32 * i:32 * i + 32]
+    b.put(x)
+    got = P.attend(b.kv, 1, b.step, q.cuda(), scale=1.0).cpu().double()
+    want, _, _ = R.attend(q, x[:, 0], b.seqs, b.pages, 0, 1.0)
+    seen = want > 0
+    assert (got[~seen] == 0).all()
+    off = (got[seen] / want[seen] - 1).square().mean().sqrt()
+    assert off <= 2.31 * U, float(off / U)
