@@ -552,7 +552,8 @@ typedef struct ee_paged ee_paged;
 
 /* The new tokens of one call.  Sequence s brings the rows q_start[s] .. q_start[s+1]-1 (none is allowed); its row j of q_len
  * stands at position kv_len[s] - q_len + j; position p sits in page pages[s * pages_per_seq + p / page_size].  The host's
- * figures size the launches, the device's say what is there; q_start rises from 0 to n_tokens. */
+ * figures size the launches, the device's say what is there; q_start rises from 0 to n_tokens (where it falls, no memory beside the
+ * call's is touched, but which rows are served, and whether status bit 2 reports it, is not defined). */
 typedef struct {
     int32_t n_seqs;
     int32_t n_tokens;            /* rows of the call                                       */
