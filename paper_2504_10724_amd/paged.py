@@ -93,9 +93,9 @@ class Rope:
         self.lib = ee.load()
         self.cfg = ee.ee_rope_config(head_dim, head_dim if rot_dim is None else rot_dim, _PAIRINGS[pairing], max_pos, _SCALINGS[scaling],
                                      trained_pos, theta, factor, low, high, magnitude)
-        self.device = torch.cuda.current_device()
         self.h = C.c_void_p()
         ee.check(self.lib.ee_rope_create(C.byref(self.cfg), C.byref(self.h)))
+        self.device = torch.cuda.current_device()            # where the table is
 
     def close(self):
         if self.h:
@@ -141,12 +141,11 @@ class PagedCache:
         self.lib = ee.load()
         self.cfg = ee.ee_paged_config(n_layers, n_pages, n_kv_heads, head_dim, page_size, ee.EE_BF16 if dtype == "bf16" else ee.EE_F32)
         self.dtype, self.n_kv_heads, self.head_dim = (torch.bfloat16 if dtype == "bf16" else torch.float32), n_kv_heads, head_dim
-        self.scale = head_dim ** -0.5
         nbytes = self.lib.ee_paged_pool_bytes(C.byref(self.cfg))
         if nbytes == 0:
             raise ee.EEError(ee.EE_ERR_SHAPE, self.lib.ee_last_error().decode())
         self.pool = torch.empty(nbytes // self.dtype.itemsize, dtype=self.dtype, device="cuda")
-        self.device = self.pool.get_device()
+        self.scale, self.device = head_dim ** -0.5, self.pool.get_device()
         self.h = C.c_void_p()
         ee.check(self.lib.ee_paged_bind(C.byref(self.cfg), self.pool.data_ptr(), nbytes, C.byref(self.h)))
 
