@@ -600,6 +600,112 @@ size_t ee_paged_attention_workspace(const ee_paged* p, int n_q_heads, const ee_p
 int ee_paged_attention(const ee_paged* p, int layer, const ee_paged_step* step, const ee_heads* q, const ee_heads* out,
                        int n_q_heads, float scale, int window, void* dev_workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------ pages and who holds them
+ *
+ * Bookkeeping of a paged cache's pages on the device, for callers whose decisions are made there (ee_beam_select's parents, say) and
+ * who record a step into a graph: the calls above read the tables that these ones write, and no call waits for the GPU.
+ *
+ * A table has a row for each sequence: the pages of its positions in order, -1 from ceil(kv_len / page_size) on, and its length.
+ * refs[p] counts the entries that name page p, over all tables that are kept with one state; a page that none names is free.
+ * Rows may share pages (a common prompt, beams of one request).  A new table is all -1 with lengths of 0, and only these calls change
+ * entries, lengths and counts afterwards.  Every result is the same each time, page numbers included.
+ *
+ * Calls on one state, and calls on the caches and tables that go with it, are ordered by the caller: one stream, or events.
+ * Bits set in *dev_status (nullable; never cleared):
+ *   1 = ee_pages_grow: the page that holds a row's last positions is not in 0 .. n_pages-1: the row is left as it was
+ *       ee_pages_copy: a page outside its pool: the pair is left out
+ *   4 = ee_pages_grow: fewer free pages than the call needs: nothing is changed
+ *   8 = a parent that is no row, a negative length or growth, a length beyond the table: the row is left as it was */
+typedef struct {
+    int32_t  n_seqs;
+    int32_t  pages_per_seq;
+    int32_t* dev_pages;    /* [n_seqs][pages_per_seq]: ee_paged_step's                  */
+    int32_t* dev_kv_len;   /* [n_seqs]: ee_paged_step's                                 */
+} ee_page_table;
+
+/* Rows that go with a table's: row i is the `bytes` bytes at dev + i * stride (bytes; rows do not overlap). */
+typedef struct {
+    void*   dev;
+    int64_t stride;
+    int64_t bytes;
+} ee_rows;
+
+#define EE_PAGES_MAX_SEQS 4096    /* rows of a table that ee_pages_grow takes           */
+#define EE_PAGES_MAX_GROUP 16384  /* rows that are forked among each other              */
+#define EE_PAGES_MAX_ROWS 8       /* arrays of ee_rows, tables of ee_pages_compact      */
+typedef struct ee_pages ee_pages;
+
+/* State: the caller's memory, 256-byte aligned; it begins with int32 refs[n_pages], which may be read (the count of zeros is the number
+ * of free pages).  max_seqs: rows of the largest table that ee_pages_grow is called on.  0 on figures that ee_pages_bind refuses. */
+size_t ee_pages_state_bytes(const ee_paged* p, int max_seqs);
+/* p outlives the handle.  No device work: ee_pages_reset makes the state's contents.
+ * Errors: EE_ERR_SHAPE (max_seqs not in 1 .. EE_PAGES_MAX_SEQS), EE_ERR_CAPACITY, EE_ERR_INVALID_ARG. */
+int ee_pages_bind(const ee_paged* p, int max_seqs, void* dev_state, size_t state_bytes, ee_pages** out);
+int ee_pages_destroy(ee_pages* g);
+/* Every page is free.  Enqueue only. */
+int ee_pages_reset(ee_pages* g, void* stream);
+
+/* Row i gains dev_new[i] positions (NULL: one each; 0 is allowed): the table gets the pages that it lacks, the length grows.  A row that will write
+ * into a page that other rows hold gets a page of its own instead, with the groups of 32 positions copied that hold any of the row's, in
+ * every layer; where all rows that hold the page are written by this call, the first of them keeps it.  Pages are handed out by
+ * row, then by place in the row, the lowest free one first.  All or nothing: with too few free pages status bit 4 is set.
+ * What new positions hold is not defined until they are written.
+ * Errors: EE_ERR_CAPACITY if the table has more than max_seqs rows, EE_ERR_INVALID_ARG. */
+int ee_pages_grow(ee_pages* g, const ee_page_table* t, const int32_t* dev_new, int32_t* dev_status, void* stream);
+
+/* Row i of `to` becomes the first min(length, dev_keep[i]) positions (dev_keep NULL: all) of row dev_parent[i] of `from`, whose pages it
+ * shares, and gives back what it held; parent -1: it holds nothing.  `from` NULL or the same table: in place, every row read
+ * before any is written.  So it forks, reorders, cuts and frees.  group > 0: rows group * j .. group * j + group - 1 have their
+ * parents, numbered 0 .. group - 1, among each other; group 0: parents are rows of the whole table.
+ * states: further rows that go along in place (tokens so far, hidden states); those of a parent of -1 stay as they are.
+ * Errors: EE_ERR_SHAPE if to's width is below from's, n_seqs is no multiple of group, with group > 0 the tables' n_seqs
+ * differ, or more than EE_PAGES_MAX_GROUP rows are forked in place among each other; EE_ERR_INVALID_ARG (states without a fork in place; tables that
+ * share only part of their memory). */
+int ee_pages_fork(ee_pages* g, const ee_page_table* to, const ee_page_table* from, const int32_t* dev_parent, const int32_t* dev_keep,
+                  int group, const ee_rows* states, int n_states, int32_t* dev_status, void* stream);
+
+/* Copies page dev_from[i] of one pool to page dev_to[i] of another, i < n, in all layers.  The pools may be one (a page is not
+ * both read and written, then, and none is written twice in any case) and have the same configuration but for n_pages. */
+int ee_pages_copy(const ee_paged* from, const ee_paged* to, const int32_t* dev_from, const int32_t* dev_to, int n, int32_t* dev_status,
+                  void* stream);
+
+/* Moves the pages in use to the numbers 0 .. n_used - 1: those above, in rising order, into the free ones below, in rising order; the
+ * tables, which have to be all that name pages of this state, are changed with them.  What lies above is free then, and the first n_used pages
+ * fit a smaller pool (ee_pages_copy). */
+int ee_pages_compact(ee_pages* g, const ee_page_table* tables, int n_tables, void* stream);
+
+/* ------------------------------------------------------------------ beam search
+ *
+ * The choice of a search's next beams from the logits of its present ones (an exit head's, say).  Request r has the rows r * beams .. of the
+ * logits; beam b's candidate v counts  score[b] + z[b][v] - ln sum_u exp z[b][u].  The `keep` best of a request's beams * vocab
+ * candidates come out in falling order, equal ones in the order of b * vocab + v.  The sums and the candidates' values are held in 64
+ * bits, so that the order is that of the formula.  A beam that has ended (dev_done) has one candidate: end_token, at its score.
+ * A beam whose score or logarithm is not finite (all logits -inf, a NaN or +inf among them) has none, nor has a logit of -inf.
+ * Places that no candidate is left for get score -inf, parent -1, token -1.  A search starts with one live beam: scores 0, -inf, .. */
+typedef struct {
+    int32_t n_groups;    /* requests                                                    */
+    int32_t beams;       /* 1 .. 64                                                     */
+    int32_t keep;        /* 1 .. 128: beams of the next step, or more                   */
+    int32_t vocab;       /* 1 .. 2^30                                                   */
+    int32_t dtype;       /* ee_dtype of the logits                                      */
+    int32_t end_token;   /* -1: no beam ends                                            */
+} ee_beam_config;
+
+/* The chosen: arrays [n_groups][keep].  With keep == beams, score and done may be the arrays that were read. */
+typedef struct {
+    float*   dev_score;
+    int32_t* dev_parent;   /* beam of the request: 0 .. beams-1                           */
+    int32_t* dev_token;
+    uint8_t* dev_done;     /* nullable: 1 = the parent had ended, or the token ends it  */
+} ee_beam_choice;
+
+size_t ee_beam_workspace(const ee_beam_config* c);
+/* Logits: row i at dev_logits + i * row_stride elements.  dev_done [n_groups * beams]: nullable; needs an end_token.
+ * Workspace: ee_beam_workspace bytes, 256-byte aligned; its contents mean nothing between calls, calls that overlap in time need one each.
+ * Errors: EE_ERR_SHAPE, EE_ERR_DTYPE, EE_ERR_CAPACITY (workspace), EE_ERR_INVALID_ARG. */
+int ee_beam_select(const ee_beam_config* c, const void* dev_logits, int64_t row_stride, const float* dev_score, const uint8_t* dev_done,
+                   const ee_beam_choice* out, void* dev_workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------ measurement aid */
 
 /* Kernel classes of the decode step, for ee_timing_read. */

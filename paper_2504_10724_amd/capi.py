@@ -14,6 +14,7 @@ EE_ERR_INVALID_ARG, EE_ERR_SHAPE, EE_ERR_CAPACITY = -1, -2, -3
 EE_ERR_LAYER_NOT_RESIDENT, EE_ERR_EXIT_NOT_RESIDENT, EE_ERR_DTYPE, EE_ERR_HIP = -4, -5, -6, -7
 EE_F32, EE_BF16 = 0, 1
 EE_ROPE_HALF, EE_ROPE_INTERLEAVED = 0, 1
+EE_PAGES_MAX_SEQS, EE_PAGES_MAX_GROUP, EE_PAGES_MAX_ROWS = 4096, 16384, 8
 EE_ROPE_UNSCALED, EE_ROPE_LINEAR, EE_ROPE_BASE, EE_ROPE_BANDS = 0, 1, 2, 3
 
 
@@ -48,7 +49,7 @@ class ee_rope_config(C.Structure):
                 ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double)]
 
 
-class ee_heads(C.Structure):      # arguments of this type are declared as void pointers: ee_heads by reference, or its bytes
+class ee_heads(C.Structure):      # arguments of this type, ee_rows, ee_page_table (several), ee_beam_*: declared as void pointers, by reference or bytes
     _fields_ = [("dev", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
@@ -61,6 +62,23 @@ class ee_paged_step(C.Structure):
     _fields_ = [("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("max_q_len", C.c_int32), ("max_kv_len", C.c_int32),
                 ("pages_per_seq", C.c_int32), ("dev_q_start", C.c_void_p), ("dev_kv_len", C.c_void_p),
                 ("dev_pages", C.c_void_p), ("dev_status", C.c_void_p)]
+
+
+class ee_page_table(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("pages_per_seq", C.c_int32), ("dev_pages", C.c_void_p), ("dev_kv_len", C.c_void_p)]
+
+
+class ee_rows(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("stride", C.c_int64), ("bytes", C.c_int64)]
+
+
+class ee_beam_config(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("beams", C.c_int32), ("keep", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32),
+                ("end_token", C.c_int32)]
+
+
+class ee_beam_choice(C.Structure):
+    _fields_ = [("dev_score", C.c_void_p), ("dev_parent", C.c_void_p), ("dev_token", C.c_void_p), ("dev_done", C.c_void_p)]
 
 
 _vp, _i, _sz, _f = C.c_void_p, C.c_int, C.c_size_t, C.c_float
@@ -119,6 +137,16 @@ _SIGS = {
     "ee_paged_append": (_i, [_vp, _i, C.POINTER(ee_paged_step), _vp, _vp, _vp, _vp, _vp, _i, _vp]),
     "ee_paged_attention_workspace": (_sz, [_vp, _i, C.POINTER(ee_paged_step)]),
     "ee_paged_attention": (_i, [_vp, _i, C.POINTER(ee_paged_step), _vp, _vp, _i, _f, _i, _vp, _sz, _vp]),
+    "ee_pages_state_bytes": (_sz, [_vp, _i]),
+    "ee_pages_bind": (_i, [_vp, _i, _vp, _sz, C.POINTER(_vp)]),
+    "ee_pages_destroy": (_i, [_vp]),
+    "ee_pages_reset": (_i, [_vp, _vp]),
+    "ee_pages_grow": (_i, [_vp, C.POINTER(ee_page_table), _vp, _vp, _vp]),
+    "ee_pages_fork": (_i, [_vp, C.POINTER(ee_page_table), C.POINTER(ee_page_table), _vp, _vp, _i, _vp, _i, _vp, _vp]),
+    "ee_pages_copy": (_i, [_vp, _vp, _vp, _vp, _i, _vp, _vp]),
+    "ee_pages_compact": (_i, [_vp, _vp, _i, _vp]),
+    "ee_beam_workspace": (_sz, [_vp]),
+    "ee_beam_select": (_i, [_vp, _vp, C.c_int64, _vp, _vp, _vp, _vp, _sz, _vp]),
     "ee_timing_enable": (_i, [_i]),
     "ee_timing_reset": (_i, []),
     "ee_timing_read": (_i, [_i, C.POINTER(_i), C.POINTER(_f)]),

@@ -1,0 +1,19 @@
+// ee_beams.h -- the choice of a beam search's next beams: what the kernels get, launchers.
+#pragma once
+
+#include "ee_internal.h"
+
+constexpr int BEAM_MAX_BEAMS = 64, BEAM_MAX_KEEP = 128;
+
+// What a slice of a row's logits leaves: its maximum, sum of exp(z - maximum) in 64 bits, and its `keep` largest logits in falling
+// order with their places in the row (place -1: none).
+struct BeamParts {
+    float*   top;                  // [rows][slices]
+    double*  sum;                  // [rows][slices]
+    float*   value;                // [rows][slices][keep]
+    int32_t* place;                // [rows][slices][keep]
+};
+size_t beam_parts(const ee_beam_config& c, char* ws, BeamParts* parts);    // its bytes
+
+int launch_beam_select(const ee_beam_config& c, const void* logits, int64_t stride, const float* score, const uint8_t* done,
+                       const ee_beam_choice& out, char* ws, hipStream_t s);

@@ -1,11 +1,19 @@
-"""Device-memory plumbing around libee's rotary tables and paged cache: PyTorch allocates the buffers and provides the
-stream, libee does all the work.  What a server does with them, per layer and step (examples/paged_serving.py runs it):
+"""Device-memory plumbing around libee's rotary tables, paged cache and its pages' bookkeeping: PyTorch allocates the buffers and provides
+the stream, libee does all the work.  What a server does with them, per layer and step (examples/paged_serving.py runs it):
 
     rope = Rope(head_dim, max_pos)
     kv = PagedCache(n_layers, n_pages, n_kv_heads, head_dim, page_size, dtype="bf16")
     step = PagedStep(q_start, kv_len, pages, n_tokens=, max_q_len=, max_kv_len=)
     append(kv, layer, step, k, v, rope=rope, q=q, q_out=q)
     out = attend(kv, layer, step, q)
+
+Who owns which page is the server's own business there; where what decides about it is on the device, as in a beam search, the pages
+are kept there too (examples/beam_search.py):
+
+    pages, table = Pages(kv, max_seqs), PageTable(kv, n_seqs, pages_per_seq)
+    pages.fork(table, parent, group=n_beams, rows=[tokens])
+    pages.grow(table)
+    step = PagedStep(q_start, table.kv_len, table.pages, n_tokens=, max_q_len=, max_kv_len=)
 """
 import ctypes as C
 import struct
@@ -237,3 +245,103 @@ def attend(kv, layer, step, q, *, out=None, scale=None, window=0, workspace=None
                                        heads, kv.scale if scale is None else scale, window, workspace.data_ptr(), workspace.nbytes,
                                        _stream(dev)))
     return out
+
+
+class PageTable:
+    """A table of pages (see ee_page_table), empty: pages [n_seqs][pages_per_seq] and kv_len [n_seqs], int32 on the cache's device, which
+    PagedStep takes as they are and Pages alone changes."""
+
+    def __init__(self, kv, n_seqs, pages_per_seq):
+        _number("PageTable", n_seqs, pages_per_seq)
+        if n_seqs < 0 or pages_per_seq < 0:
+            _refuse("PageTable: negative count")
+        self.device = kv.device
+        self.pages = torch.full((n_seqs, pages_per_seq), -1, dtype=torch.int32, device=kv.pool.device)
+        self.kv_len = torch.zeros(n_seqs, dtype=torch.int32, device=kv.pool.device)
+        self.c = ee.ee_page_table(n_seqs, pages_per_seq, self.pages.data_ptr(), self.kv_len.data_ptr())
+        self.n_seqs, self.ref = n_seqs, C.byref(self.c)
+
+
+_pack_rows = struct.Struct("Pqq").pack
+
+
+class Pages:
+    """Who holds which page of a cache (see ee_pages_*), all of them free; tables of up to max_seqs rows grow.  refs (int32 [n_pages])
+    counts the entries that name a page: pages.refs == 0 are the free ones.  Calls change the tables in place and return nothing;
+    status (int32 [1]) collects refusals."""
+
+    def __init__(self, kv, max_seqs):
+        _number("Pages", max_seqs)
+        self.lib, self.kv, self.device = kv.lib, kv, kv.device
+        if not kv.h:
+            _refuse("Pages: the cache is closed")
+        nbytes = self.lib.ee_pages_state_bytes(kv.h, max_seqs)
+        self.state = torch.empty(nbytes, dtype=torch.uint8, device=kv.pool.device)
+        self.refs = self.state[:4 * kv.cfg.n_pages].view(torch.int32)
+        self.h = C.c_void_p()
+        ee.check(self.lib.ee_pages_bind(kv.h, max_seqs, self.state.data_ptr() or 256, nbytes, C.byref(self.h)))
+        self.reset()
+
+    def close(self):
+        if self.h:
+            self.lib.ee_pages_destroy(self.h)
+            self.h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, what, *tables):
+        if not self.kv.h:                                    # the library's handle would look into it
+            _refuse(f"{what}: the cache is closed")
+        for t in tables:
+            if t.device != self.device:
+                _refuse(f"{what}: a table is not on the cache's device ({self.device})")
+
+    def _ints(self, t, what, n):
+        return None if t is None else _int32(t, what, n, self.device).data_ptr()
+
+    def reset(self):
+        """every page is free; tables that name some are the caller's to clear"""
+        self._check("Pages.reset")
+        ee.check(self.lib.ee_pages_reset(self.h, _stream(self.device)))
+
+    def grow(self, table, new=None, *, status=None):
+        """new (int32 [n_seqs], default one each) positions more for the table's rows; pages that others hold too are copied before they
+        are written"""
+        self._check("Pages.grow", table)
+        ee.check(self.lib.ee_pages_grow(self.h, table.ref, self._ints(new, "Pages.grow: new", table.n_seqs),
+                                        self._ints(status, "Pages.grow: status", 1), _stream(self.device)))
+
+    def fork(self, table, parent, *, source=None, keep=None, group=0, rows=(), status=None):
+        """Row i of the table becomes row parent[i] (int32; -1: empty) of source (default: the table itself, in place), cut to keep[i]
+        positions; with `group`, parents are numbered inside groups of that many rows.  rows: tensors [n_seqs][...] whose rows go along."""
+        self._check("Pages.fork", table, *(() if source is None else (source,)))
+        _number("Pages.fork", group)
+        packed = []
+        for x in rows:
+            if x.dim() < 1 or x.shape[0] != table.n_seqs or x.get_device() != self.device or not (x.shape[0] == 0 or x[0].is_contiguous()):
+                _refuse(f"Pages.fork: rows must be [{table.n_seqs}][...] on device {self.device}, each row contiguous, got {tuple(x.shape)} on {x.device}")
+            if x.requires_grad and torch.is_grad_enabled():
+                _lost("Pages.fork")
+            size = x.element_size()
+            packed.append(_pack_rows(x.data_ptr(), x.stride(0) * size, x.numel() // max(x.shape[0], 1) * size))
+        ee.check(self.lib.ee_pages_fork(self.h, table.ref, None if source is None else source.ref, self._ints(parent, "Pages.fork: parent", table.n_seqs),
+                                        self._ints(keep, "Pages.fork: keep", table.n_seqs), group, b"".join(packed) or None, len(packed),
+                                        self._ints(status, "Pages.fork: status", 1), _stream(self.device)))
+
+    def compact(self, *tables):
+        """the pages in use move to the lowest numbers; tables: all that name pages of this cache"""
+        self._check("Pages.compact", *tables)
+        ee.check(self.lib.ee_pages_compact(self.h, b"".join(bytes(t.c) for t in tables) or None, len(tables), _stream(self.device)))
+
+
+def copy_pages(source, to, from_pages, to_pages, *, status=None):
+    """page from_pages[i] of the cache `source` to page to_pages[i] of the cache `to` (int32), in all layers"""
+    if source.device != to.device:
+        _refuse(f"copy_pages: caches on different devices ({source.device}, {to.device})")
+    n, dev = from_pages.numel(), source.device
+    ee.check(source.lib.ee_pages_copy(source.h, to.h, _int32(from_pages, "copy_pages", n, dev).data_ptr(), _int32(to_pages, "copy_pages", n, dev).data_ptr(),
+                                      n, None if status is None else _int32(status, "copy_pages: status", 1, dev).data_ptr(), _stream(dev)))

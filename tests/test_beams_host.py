@@ -1,0 +1,130 @@
+"""The beam search's choice and the pages' bookkeeping: argument checks without a GPU, documented codes before any device work."""
+import ctypes as C
+
+import pytest
+
+from paper_2504_10724_amd import capi as ee
+
+DUMMY = C.c_void_p(4096)
+BAD, SHAPE, CAPACITY = ee.EE_ERR_INVALID_ARG, ee.EE_ERR_SHAPE, ee.EE_ERR_CAPACITY
+
+
+def _beams(**kw):
+    c = dict(n_groups=2, beams=4, keep=4, vocab=1000, dtype=ee.EE_F32, end_token=-1)
+    c.update(kw)
+    return ee.ee_beam_config(**c)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(n_groups=-1), BAD), (dict(beams=0), SHAPE), (dict(beams=65), SHAPE), (dict(keep=0), SHAPE), (dict(keep=129), SHAPE),
+    (dict(vocab=0), SHAPE), (dict(vocab=2 ** 30 + 1), SHAPE), (dict(dtype=2), ee.EE_ERR_DTYPE), (dict(end_token=-2), BAD),
+    (dict(end_token=1000), BAD), (dict(n_groups=2 ** 31 - 1), SHAPE), (dict(n_groups=2 ** 20, vocab=2 ** 30), SHAPE)])
+def test_searches_of_no_such_kind(kw, code):
+    lib, c, out = ee.load(), _beams(**kw), ee.ee_beam_choice(4096, 4096, 4096, None)
+    assert lib.ee_beam_workspace(C.byref(c)) == 0
+    assert lib.ee_beam_select(C.byref(c), DUMMY, 1000, DUMMY, None, C.byref(out), DUMMY, 1 << 60, None) == code
+    assert lib.ee_last_error()
+
+
+def test_choices():
+    lib, c = ee.load(), _beams(end_token=3)
+    need = lib.ee_beam_workspace(C.byref(c))
+    assert need > 0 and lib.ee_beam_workspace(None) == 0
+    args = lambda **kw: ee.ee_beam_choice(*[kw.get(k, 8192) for k in ("score", "parent", "token", "done")])      # noqa: E731
+
+    def call(c=c, logits=DUMMY, score=C.c_void_p(4096), done=None, out=args(), ws=DUMMY, n=need):
+        return lib.ee_beam_select(None if c is None else C.byref(c), logits, 1000, score, done, None if out is None else C.byref(out), ws, n, None)
+    assert call(c=None) == BAD and call(out=None) == BAD and call(logits=None) == BAD and call(score=None) == BAD
+    for k in ("score", "parent", "token"):
+        assert call(out=args(**{k: None})) == BAD
+    assert call(n=need - 1) == CAPACITY and call(ws=None) == BAD and call(ws=C.c_void_p(4097)) == BAD
+    assert call(logits=C.c_void_p(4098)) == BAD
+    assert call(c=_beams(), done=DUMMY) == BAD                                     # ended beams without a token to go on with
+    wide = _beams(keep=8, end_token=3)
+    n = lib.ee_beam_workspace(C.byref(wide))
+    assert call(c=wide, n=n, out=args(score=4096)) == BAD                          # in place of fewer
+    assert call(c=wide, n=n, done=C.c_void_p(12288), out=args(done=12288)) == BAD
+    assert call(c=_beams(n_groups=0), logits=None, score=None, out=args(score=None), ws=None, n=0) == ee.EE_OK
+
+
+def _cache(lib, **kw):
+    c = dict(n_layers=2, n_pages=100, n_kv_heads=2, head_dim=128, page_size=64, dtype=ee.EE_BF16)
+    c.update(kw)
+    cfg, p = ee.ee_paged_config(**c), C.c_void_p()
+    assert lib.ee_paged_bind(C.byref(cfg), DUMMY, 1 << 60, C.byref(p)) == ee.EE_OK
+    return p
+
+
+def test_bookkeeping_handles():
+    lib, h = ee.load(), C.c_void_p()
+    p = _cache(lib)
+    need = lib.ee_pages_state_bytes(p, 8)
+    assert need >= 4 * 100 and lib.ee_pages_state_bytes(None, 8) == 0
+    for n in (0, -1, 4097):
+        assert lib.ee_pages_state_bytes(p, n) == 0 and lib.ee_pages_bind(p, n, DUMMY, 1 << 60, C.byref(h)) == SHAPE
+    assert lib.ee_pages_bind(None, 8, DUMMY, need, C.byref(h)) == BAD and lib.ee_pages_bind(p, 8, None, need, C.byref(h)) == BAD
+    assert lib.ee_pages_bind(p, 8, DUMMY, need - 1, C.byref(h)) == CAPACITY and lib.ee_pages_bind(p, 8, C.c_void_p(4097), need, C.byref(h)) == BAD
+    assert not h.value and lib.ee_pages_reset(None, None) == BAD
+    assert lib.ee_pages_destroy(None) == ee.EE_OK
+    lib.ee_paged_destroy(p)
+
+
+def _table(**kw):
+    c = dict(n_seqs=4, pages_per_seq=3, dev_pages=4096, dev_kv_len=8192)
+    c.update(kw)
+    return ee.ee_page_table(**c)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(n_seqs=-1), BAD), (dict(pages_per_seq=-1), BAD), (dict(pages_per_seq=2 ** 25), CAPACITY), (dict(dev_pages=None), BAD),
+    (dict(dev_kv_len=None), BAD)])
+def test_tables_of_no_such_kind(kw, code):
+    lib, g = ee.load(), C.c_void_p()
+    p = _cache(lib)
+    assert lib.ee_pages_bind(p, 8, DUMMY, 1 << 40, C.byref(g)) == ee.EE_OK
+    t = _table(**kw)
+    assert lib.ee_pages_grow(g, C.byref(t), None, None, None) == code
+    assert lib.ee_pages_fork(g, C.byref(t), None, DUMMY, None, 0, None, 0, None, None) == code
+    assert lib.ee_pages_compact(g, C.byref(t), 1, None) == code
+    lib.ee_pages_destroy(g)
+    lib.ee_paged_destroy(p)
+
+
+def test_bookkeeping_calls():
+    lib, g = ee.load(), C.c_void_p()
+    p = _cache(lib)
+    assert lib.ee_pages_bind(p, 8, DUMMY, 1 << 40, C.byref(g)) == ee.EE_OK
+    t, none, wide = _table(), _table(n_seqs=0), _table(n_seqs=9)
+    T = C.byref
+    assert lib.ee_pages_grow(None, T(t), None, None, None) == BAD and lib.ee_pages_grow(g, None, None, None, None) == BAD
+    assert lib.ee_pages_grow(g, T(wide), None, None, None) == CAPACITY and lib.ee_pages_grow(g, T(none), None, None, None) == ee.EE_OK
+
+    def fork(to=t, source=None, parent=DUMMY, keep=None, group=0, states=(), n=None):
+        a = (ee.ee_rows * 9)(*states)
+        return lib.ee_pages_fork(g, T(to), None if source is None else T(source), parent, keep, group, a if states else None,
+                                 len(states) if n is None else n, None, None)
+    other = dict(dev_pages=16384, dev_kv_len=20480)
+    assert lib.ee_pages_fork(None, T(t), None, DUMMY, None, 0, None, 0, None, None) == BAD
+    assert fork(parent=None) == BAD and fork(group=-1) == BAD and fork(n=-1) == BAD and fork(n=2) == BAD
+    assert fork(to=none, parent=None) == ee.EE_OK
+    assert fork(group=3) == SHAPE                                                  # 4 rows in groups of 3
+    assert fork(source=_table(n_seqs=8, **other), group=4) == SHAPE                # groups of unlike tables
+    assert fork(source=_table(pages_per_seq=4, **other)) == SHAPE                  # rows that do not fit
+    assert fork(source=_table(dev_pages=16384)) == BAD and fork(source=_table(dev_kv_len=16384)) == BAD and fork(source=_table(n_seqs=3)) == BAD
+    assert fork(to=_table(n_seqs=16385)) == SHAPE and fork(to=_table(n_seqs=32770), group=16385) == SHAPE
+    rows = ee.ee_rows(4096, 64, 64)
+    assert fork(states=[rows] * 9) == SHAPE and fork(source=_table(**other), states=[rows]) == BAD
+    assert fork(states=[ee.ee_rows(4096, 63, 64)]) == BAD and fork(states=[ee.ee_rows(4096, 64, -1)]) == BAD
+    assert fork(states=[ee.ee_rows(None, 64, 64)]) == BAD and fork(states=[rows, rows]) == BAD
+    assert lib.ee_pages_compact(None, T(t), 1, None) == BAD and lib.ee_pages_compact(g, None, 1, None) == BAD
+    assert lib.ee_pages_compact(g, T(t), -1, None) == BAD and lib.ee_pages_compact(g, T(t), 9, None) == SHAPE
+    assert lib.ee_pages_compact(g, (ee.ee_page_table * 2)(t, t), 2, None) == BAD
+    for kw, code in ((dict(head_dim=64), SHAPE), (dict(page_size=32), SHAPE), (dict(n_layers=1), SHAPE), (dict(n_kv_heads=1), SHAPE),
+                     (dict(dtype=ee.EE_F32), ee.EE_ERR_DTYPE)):
+        q = _cache(lib, **kw)
+        assert lib.ee_pages_copy(p, q, DUMMY, DUMMY, 1, None, None) == code
+        lib.ee_paged_destroy(q)
+    assert lib.ee_pages_copy(None, p, DUMMY, DUMMY, 1, None, None) == BAD and lib.ee_pages_copy(p, p, DUMMY, DUMMY, -1, None, None) == BAD
+    assert lib.ee_pages_copy(p, p, None, DUMMY, 1, None, None) == BAD and lib.ee_pages_copy(p, p, None, None, 0, None, None) == ee.EE_OK
+    lib.ee_pages_destroy(g)
+    lib.ee_paged_destroy(p)
