@@ -5,13 +5,15 @@
 
 constexpr int BEAM_MAX_BEAMS = 64, BEAM_MAX_KEEP = 128;
 
-// What a slice of a row's logits leaves: its maximum, sum of exp(z - maximum) in 64 bits, and its `keep` largest logits in falling
-// order with their places in the row (place -1: none).
+// What a slice of a row's logits leaves: its maximum, sum of exp(z - maximum) in 64 bits, and a list of logits with their places in the row,
+// in any order, the `keep` largest among them.
 struct BeamParts {
     float*   top;                  // [rows][slices]
     double*  sum;                  // [rows][slices]
-    float*   value;                // [rows][slices][keep]
-    int32_t* place;                // [rows][slices][keep]
+    int32_t* count;                // [rows][slices]: of the list
+    float*   value;                // [rows][slices][room]
+    int32_t* place;                // [rows][slices][room]
+    int32_t  room;
 };
 size_t beam_parts(const ee_beam_config& c, char* ws, BeamParts* parts);    // its bytes
 
