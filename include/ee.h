@@ -639,7 +639,7 @@ typedef struct ee_pages ee_pages;
  * of free pages).  max_seqs: rows of the largest table that ee_pages_grow is called on.  0 on figures that ee_pages_bind refuses. */
 size_t ee_pages_state_bytes(const ee_paged* p, int max_seqs);
 /* p outlives the handle.  No device work: ee_pages_reset makes the state's contents.
- * Errors: EE_ERR_SHAPE (max_seqs not in 1 .. EE_PAGES_MAX_SEQS), EE_ERR_CAPACITY, EE_ERR_INVALID_ARG. */
+ * Errors: EE_ERR_SHAPE (max_seqs not in 1 .. EE_PAGES_MAX_SEQS, more than 2^21 pages), EE_ERR_CAPACITY, EE_ERR_INVALID_ARG. */
 int ee_pages_bind(const ee_paged* p, int max_seqs, void* dev_state, size_t state_bytes, ee_pages** out);
 int ee_pages_destroy(ee_pages* g);
 /* Every page is free.  Enqueue only. */

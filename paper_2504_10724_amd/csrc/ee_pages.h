@@ -9,11 +9,13 @@ struct ee_pages {
     char* state;
 };
 
+constexpr int PAGES_MOST = 1 << 21;  // pages that a state has
+
 // Parts of the state.  What follows the free bits is scratch of the call that runs.
 struct PagesView {
     int32_t*  refs;                // [n_pages]: entries that name the page
     uint32_t* free_bits;           // [ceil(n_pages / 32)]: 1 = refs is 0; bits beyond n_pages are 0
-    int32_t*  mark;                // [n_pages][2]: writers of a shared page and the first of them; a moved page's new number
+    int32_t*  name;                // [n_pages]: a moved page's new number
     int32_t*  src;                 // [max(max_seqs, n_pages / 2 + 1)]: pages to copy, whereto, how many groups of 32 positions
     int32_t*  dst;
     int32_t*  groups;              // [max_seqs]

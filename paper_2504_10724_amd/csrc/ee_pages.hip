@@ -10,7 +10,7 @@ __global__ void __launch_bounds__(256) k_pages_reset(PagesView v) {
     const int words = (v.n_pages + 31) / 32;
     for (int i = blockIdx.x * 256 + threadIdx.x; i < v.n_pages; i += gridDim.x * 256) {
         v.refs[i] = 0;
-        v.mark[2 * (int64_t)i] = v.mark[2 * (int64_t)i + 1] = -1;
+        v.name[i] = -1;
         if (i < words) v.free_bits[i] = i == words - 1 && v.n_pages % 32 ? (1u << v.n_pages % 32) - 1 : ~0u;
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) *v.n_moves = 0;
@@ -23,178 +23,216 @@ int launch_pages_reset(const PagesView& v, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ one workgroup's sums
-// sum of v over the threads before this one, and over all; `waves` holds a value for each wave
-template <int THREADS, class T> __device__ __forceinline__ T sum_before(T v, T* waves, T& total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    T up = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const T u = __shfl_up(up, o, 64);
-        if (lane >= o) up += u;
-    }
-    __syncthreads();                                         // the waves' sums of the last call have been read
-    if (lane == 63) waves[w] = up;
-    __syncthreads();
-    T before = 0;
-    total = 0;
-#pragma unroll
-    for (int i = 0; i < THREADS / 64; ++i) {
-        const T x = waves[i];
-        if (i < w) before += x;
-        total += x;
-    }
-    return before + up - v;
+// sums over the lanes before a lane and itself: of the lanes of a row of 16, then of the rows
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t lane_of(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
 }
-
-// what atomics of other threads of this launch have left: past the caches of the compute unit
-__device__ __forceinline__ int load_now(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t v) {
+    v += lane_of<0x111, 0xf>(v);                             // the lane before, then two, four and eight before
+    v += lane_of<0x112, 0xf>(v);
+    v += lane_of<0x114, 0xf>(v);
+    v += lane_of<0x118, 0xf>(v);
+    v += lane_of<0x142, 0xa>(v);                             // the last lane of the row before, to the second and the fourth row
+    v += lane_of<0x143, 0xc>(v);                             // the last lane of the first half, to the second
+    return v;
+}
+// Of N numbers at once: the sum of each over the threads before this one, and over all.  `waves` holds N numbers for each wave.
+template <int THREADS, int N> __device__ __forceinline__ void sum_before(uint32_t (&v)[N], uint32_t (&total)[N], uint32_t* waves) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    constexpr int WAVES = THREADS / 64;
+    uint32_t up[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) up[k] = sum_up_to(v[k]);
+    __syncthreads();                                         // the waves' sums of the last call have been read
+    if (lane == 63)
+#pragma unroll
+        for (int k = 0; k < N; ++k) waves[k * WAVES + w] = up[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {                            // every wave sums the waves' sums in its own lanes
+        const uint32_t all = sum_up_to(lane < WAVES ? waves[k * WAVES + lane] : 0u);
+        const uint32_t before = w == 0 ? 0u : (uint32_t)__builtin_amdgcn_readlane((int)all, __builtin_amdgcn_readfirstlane(w) - 1);
+        total[k] = (uint32_t)__builtin_amdgcn_readlane((int)all, 63);
+        v[k] = before + up[k] - v[k];
+    }
+}
 
 // ------------------------------------------------------------------ grow
 // Row s needs pages(len + new) - pages(len) pages, and one more where its last page is shared and it does not keep it; a prefix sum
 // over the rows gives each its places among the free pages in rising order, which the free bits give, 32 a word, by another prefix sum.  One
-// workgroup, since every row's pages hang on the rows before it; a thread has PER rows.
-//   shared pages: each writer marks its page, adds itself, and finds how many write it and which is the first
+// workgroup, since every row's pages hang on the rows before it; a thread has PER rows.  It is bound by its trips to memory one behind the other (rows, their last
+// pages, these pages' counts, the results), about 1.2 us each with the kernel's start and end, so nothing else leaves the compute unit:
+//   shared pages: writers meet in a table in LDS, where a page's writers are counted and the first is found
 //   all or nothing: the sums are known before anything is written
-//   the free pages' numbers go to LDS a few words at a time; the threads then take a needed page each
-// Copies are listed for the launch behind this one.
+//   the free pages' numbers go to LDS some words at a time; the threads then take a needed page each
+// Copies are listed for the launch behind this one.  A thread's need is cut above the most pages that a state has, so that sums stay in 32 bits.
 constexpr int GROW = 1024, GROW_WORDS = 256;                 // threads; words of free bits at a time
 template <int PER>
 __global__ void __launch_bounds__(GROW)
 k_pages_grow(PagesView v, TableView t, const int32_t* __restrict__ more, int32_t* status) {
-    __shared__ int32_t first[PER * GROW], place[PER * GROW];  // a row's first needed page; its first new place, sign bit: a copy comes first
-    __shared__ uint16_t page_of[GROW_WORDS * 32];
-    __shared__ long long sums[GROW / 64];
+    constexpr int ROWS = PER * GROW, SLOTS = 2 * ROWS;
+    // the writers' table first, then what the rows take
+    struct Meet { int32_t page[SLOTS], writers[SLOTS], first[SLOTS]; };
+    struct Take { int32_t first[ROWS], place[ROWS]; uint16_t page_of[GROW_WORDS * 32]; };    // a row's first needed page; its first new place, sign bit: a copy comes first
+    __shared__ union { Meet meet; Take take; } lds;
+    __shared__ uint32_t sums[3 * GROW / 64];
     __shared__ int n_copies;
     const int tid = threadIdx.x, ps = v.page_size, words = (v.n_pages + 31) / 32;
-    if (tid == 0) n_copies = 0;
-
-    long long n_free = 0;
-    for (int w = tid; w < words; w += GROW) n_free += __popc(v.free_bits[w]);
-
     int len[PER], add[PER], held[PER], refs[PER];
-    bool shared = false;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int s = tid * PER + i;
         len[i] = s < t.n ? t.len[s] : 0;
         add[i] = s < t.n ? (more ? more[s] : 1) : 0;
+    }
+    uint32_t bits = tid < GROW_WORDS && tid < words ? v.free_bits[tid] : 0u, n_free = 0;
+    for (int w = tid; w < words; w += GROW) n_free += __popc(v.free_bits[w]);
+    if (tid == 0) n_copies = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int s = tid * PER + i;
         held[i] = -1;
         refs[i] = 0;
         if (len[i] < 0 || add[i] < 0 || (int64_t)len[i] + add[i] > (int64_t)t.width * ps) {
             if (status) atomicOr(status, 8);
             add[i] = 0;
         }
+        if (add[i] > 0 && len[i] % ps != 0) held[i] = t.pages[(int64_t)s * t.width + len[i] / ps];
+    }
+    for (int i = tid; i < SLOTS; i += GROW) {
+        lds.meet.page[i] = -1;
+        lds.meet.writers[i] = 0;
+        lds.meet.first[i] = 0x7fffffff;
+    }
+    bool shared = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
         if (add[i] > 0 && len[i] % ps != 0) {
-            held[i] = t.pages[(int64_t)s * t.width + len[i] / ps];
             if (held[i] < 0 || held[i] >= v.n_pages) {
                 if (status) atomicOr(status, 1);
                 held[i] = -1;
                 add[i] = 0;
             } else {
                 refs[i] = v.refs[held[i]];
+                shared = shared || refs[i] > 1;
             }
         }
-        if (refs[i] > 1) {
-            shared = true;
-            v.mark[2 * (int64_t)held[i]] = 0;
-            v.mark[2 * (int64_t)held[i] + 1] = 0x7fffffff;
-        }
-    }
-    __threadfence();
+    bool copy[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) copy[i] = false;
     if (__syncthreads_or(shared)) {
+        int slot[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            if (refs[i] > 1) {
-                atomicAdd(&v.mark[2 * (int64_t)held[i]], 1);
-                atomicMin(&v.mark[2 * (int64_t)held[i] + 1], tid * PER + i);
+            if (refs[i] > 1) {                               // a free slot for it, or the one that another writer has taken; there are two a row
+                int o = (int)((uint32_t)held[i] * 2654435769u >> 16) & (SLOTS - 1);
+                for (;; o = (o + 1) & (SLOTS - 1)) {
+                    const int was = atomicCAS(&lds.meet.page[o], -1, held[i]);
+                    if (was == -1 || was == held[i]) break;
+                }
+                slot[i] = o;
+                atomicAdd(&lds.meet.writers[o], 1);
+                atomicMin(&lds.meet.first[o], tid * PER + i);
             }
-        __threadfence();
         __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (refs[i] > 1) copy[i] = refs[i] > lds.meet.writers[slot[i]] || lds.meet.first[slot[i]] != tid * PER + i;
     }
-    bool copy[PER];
     int need[PER];
-    long long mine = 0, total;
+    uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        copy[i] = refs[i] > 1 && (refs[i] > load_now(&v.mark[2 * (int64_t)held[i]]) || load_now(&v.mark[2 * (int64_t)held[i] + 1]) != tid * PER + i);
         need[i] = add[i] > 0 ? (len[i] + add[i] + ps - 1) / ps - (len[i] + ps - 1) / ps + copy[i] : 0;
-        mine += need[i];
+        mine = min(mine + (uint32_t)need[i], PAGES_MOST + 1u);
     }
-    long long before = sum_before<GROW>(mine, sums, total), free_total;
-    sum_before<GROW>(n_free, sums, free_total);
-    if (total > free_total) {
+    uint32_t before[3] = {mine, n_free, (uint32_t)__popc(bits)}, all[3];
+    sum_before<GROW>(before, all, sums);
+    if (all[0] > all[1]) {
         if (tid == 0) {
             if (status) atomicOr(status, 4);
             *v.n_moves = 0;
         }
         return;
     }
+    const int total = (int)all[0];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {                          // sums fit 32 bits now
-        first[tid * PER + i] = (int)before;
-        place[tid * PER + i] = ((len[i] + ps - 1) / ps) | (copy[i] ? (int)0x80000000 : 0);
-        before += need[i];
+    for (int i = 0; i < PER; ++i) {
+        lds.take.first[tid * PER + i] = (int)before[0];
+        lds.take.place[tid * PER + i] = ((len[i] + ps - 1) / ps) | (copy[i] ? (int)0x80000000 : 0);
+        before[0] += need[i];
     }
     int taken = 0;
-    for (int w0 = 0; w0 < words && taken < (int)total; w0 += GROW_WORDS) {
+    for (int w0 = 0; w0 < words && taken < total; w0 += GROW_WORDS) {
         const int w = w0 + tid;
-        uint32_t bits = tid < GROW_WORDS && w < words ? v.free_bits[w] : 0u;
-        long long here;
-        const int rank = (int)sum_before<GROW>((long long)__popc(bits), sums, here);
-        if (bits && taken + rank < (int)total) {
-            for (int r = rank; bits && taken + r < (int)total; ++r) {
-                page_of[r] = (uint16_t)(tid * 32 + __builtin_ctz(bits));
+        if (w0 > 0) {                                        // the first words are in the sums above
+            bits = tid < GROW_WORDS && w < words ? v.free_bits[w] : 0u;
+            uint32_t one[1] = {(uint32_t)__popc(bits)}, here[1];
+            sum_before<GROW>(one, here, sums);
+            before[2] = one[0];
+            all[2] = here[0];
+        }
+        const int rank = (int)before[2];
+        if (bits && taken + rank < total) {
+            for (int r = rank; bits && taken + r < total; ++r) {
+                lds.take.page_of[r] = (uint16_t)(tid * 32 + __builtin_ctz(bits));
                 bits &= bits - 1;
             }
             v.free_bits[w] = bits;
         }
         __syncthreads();
-        const int n = min((int)here, (int)total - taken);
+        const int n = min((int)all[2], total - taken);
+        // a row's copy: by its own thread, which knows the page
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int r = lds.take.first[tid * PER + i] - taken;
+            if (copy[i] && r >= 0 && r < n) {
+                const int c = atomicAdd(&n_copies, 1), page = w0 * 32 + lds.take.page_of[r];
+                v.src[c] = held[i];
+                v.dst[c] = page;
+                v.groups[c] = (len[i] % ps + 31) / 32;
+                atomicSub(&v.refs[held[i]], 1);
+                t.pages[(int64_t)(tid * PER + i) * t.width + len[i] / ps] = page;
+                v.refs[page] = 1;
+            }
+        }
         for (int r = tid; r < n; r += GROW) {
-            const int page = w0 * 32 + page_of[r], k = taken + r;
+            const int page = w0 * 32 + lds.take.page_of[r], k = taken + r;
             int s = 0;                                       // the last row whose first page is not behind this one
 #pragma unroll
-            for (int o = PER * GROW / 2; o > 0; o >>= 1)
-                if (first[s + o] <= k) s += o;
-            const int at = place[s] & 0x7fffffff, nth = k - first[s];
-            int32_t* row = t.pages + (int64_t)s * t.width;
-            if (place[s] < 0 && nth == 0) {
-                const int old = row[at - 1], c = atomicAdd(&n_copies, 1);
-                v.src[c] = old;
-                v.dst[c] = page;
-                v.groups[c] = (t.len[s] % ps + 31) / 32;
-                atomicSub(&v.refs[old], 1);
-                row[at - 1] = page;
-            } else {
-                row[at + nth - (place[s] < 0)] = page;
-            }
+            for (int o = ROWS / 2; o > 0; o >>= 1)
+                if (lds.take.first[s + o] <= k) s += o;
+            const int at = lds.take.place[s], nth = k - lds.take.first[s] - (at < 0);
+            if (nth < 0) continue;                           // the copy
+            t.pages[(int64_t)s * t.width + (at & 0x7fffffff) + nth] = page;
             v.refs[page] = 1;
         }
         taken += n;
         __syncthreads();
     }
-    __syncthreads();
 #pragma unroll
     for (int i = 0; i < PER; ++i)
         if (add[i] > 0) t.len[tid * PER + i] = len[i] + add[i];
+    __syncthreads();
     if (tid == 0) *v.n_moves = n_copies;
 }
 
 // ------------------------------------------------------------------ copies
 // 16 bytes a lane, four at a time.  Bound by the bytes read and written.
+typedef uint32_t words __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void copy_run(const char* __restrict__ src, char* __restrict__ dst, int bytes) {
-    const uint4* a = reinterpret_cast<const uint4*>(src);
-    uint4* b = reinterpret_cast<uint4*>(dst);
+    const words* a = reinterpret_cast<const words*>(src);
+    words* b = reinterpret_cast<words*>(dst);
     const int n = bytes / 16;
-    for (int o = threadIdx.x; o < n; o += 1024) {
-        uint4 x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (o + 256 * i < n) x[i] = a[o + 256 * i];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (o + 256 * i < n) b[o + 256 * i] = x[i];
+    int o = threadIdx.x;
+    for (; o + 768 < n; o += 1024) {
+        const words w = a[o], x = a[o + 256], y = a[o + 512], z = a[o + 768];
+        b[o] = w;
+        b[o + 256] = x;
+        b[o + 512] = y;
+        b[o + 768] = z;
     }
+    for (; o < n; o += 256) b[o] = a[o];
 }
 
 // the listed pages' first groups of 32 positions, in all layers: an item is one group of one block
@@ -222,7 +260,7 @@ k_pages_copy(PoolView from, PoolView to, const int32_t* __restrict__ src, const 
             int32_t* p = tables.t[k].pages;
             for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)n_rename * 256) {
                 const int e = p[i];
-                if (e >= 0 && e < from.n_pages && name[2 * (int64_t)e] >= 0) p[i] = name[2 * (int64_t)e];
+                if (e >= 0 && e < from.n_pages && name[e] >= 0) p[i] = name[e];
             }
         }
         return;
@@ -270,49 +308,70 @@ int launch_pages_copy(const PoolView& from, const PoolView& to, const int32_t* s
 //
 // Counts: what a row takes is counted before what it gives up is counted down, each by atomics; and a page that a row takes is named by that row's
 // parent until the tile that takes it has counted it.  So a count falls to 0 once, in the thread that frees the page, whatever the order.
+constexpr int FORK = 256, LDS = 65536, IN_LDS = 2048;        // threads; bytes a workgroup may have; rows whose parents it keeps there
 struct ForkLaunch {
     ForkView f;
     int32_t* refs;
     uint32_t* free_bits;
     int32_t n_pages, page_size;
-    int32_t rows, tiles, cols, table_tiles;
-    int32_t first[EE_PAGES_MAX_ROWS], unit[EE_PAGES_MAX_ROWS], n_units[EE_PAGES_MAX_ROWS];     // of a state: its first tile, bytes of a unit, units of a tile
+    int32_t rows, tiles, shift, table_tiles;                 // 1 << shift: columns of a tile
+    struct { int32_t first, unit, shift; } state[EE_PAGES_MAX_ROWS];     // its first tile, bytes of a unit, units of a tile as a shift
 };
 
 struct ForkRows {
     const ForkView& f;
+    const int32_t* kept;                                     // in LDS, or null
     int base, limit;
     // the row of `from` that row i of the group takes; -1: none, -2: it stays as it is
-    __device__ __forceinline__ int source(int i) const {
+    __device__ __forceinline__ int look(int i) const {
         const int row = base + i, p = f.parent[row];
         if (p < -1 || p >= limit || (f.keep && f.keep[row] < 0)) return -2;
         return p < 0 ? -1 : (f.group ? row / f.group * f.group : 0) + p;
     }
+    __device__ __forceinline__ int source(int i) const { return kept ? kept[i] : look(i); }
 };
 
-template <class U> __device__ __forceinline__ void fork_states(const ForkRows& r, const StateRows& st, int64_t c0, int cols, int n, U* lds) {
-    const int nc = (int)min((int64_t)cols, st.bytes / (int64_t)sizeof(U) - c0);
-    for (int e = threadIdx.x; e < n * nc; e += 256) lds[e] = reinterpret_cast<const U*>(st.p + (int64_t)(r.base + e / nc) * st.stride)[c0 + e % nc];
+template <class U> __device__ __forceinline__ void fork_states(const ForkRows& r, const StateRows& st, int64_t c0, int shift, int n, U* lds) {
+    const int64_t units = st.bytes / (int64_t)sizeof(U), c = c0 + (threadIdx.x & ((1 << shift) - 1));
+    const int first = threadIdx.x >> shift, step = FORK >> shift, at = threadIdx.x & ((1 << shift) - 1);
+    if (c < units)
+#pragma unroll 4
+        for (int i = first; i < n; i += step) lds[(i << shift) + at] = reinterpret_cast<const U*>(st.p + (int64_t)(r.base + i) * st.stride)[c];
     __syncthreads();
-    for (int e = threadIdx.x; e < n * nc; e += 256) {
-        const int i = e / nc, src = r.source(i) - r.base;
-        if (src >= 0 && src != i) reinterpret_cast<U*>(st.p + (int64_t)(r.base + i) * st.stride)[c0 + e % nc] = lds[src * nc + e % nc];
-    }
+    if (c < units)
+        for (int i = first; i < n; i += step) {
+            const int src = r.source(i) - r.base;
+            if (src >= 0 && src != i) reinterpret_cast<U*>(st.p + (int64_t)(r.base + i) * st.stride)[c] = lds[(src << shift) + at];
+        }
 }
 
-__global__ void __launch_bounds__(256) k_pages_fork(ForkLaunch a) {
-    extern __shared__ int4 shared[];
-    int32_t* lds = reinterpret_cast<int32_t*>(shared);
+__global__ void __launch_bounds__(FORK) k_pages_fork(ForkLaunch a) {
+    extern __shared__ words shared[];
     const ForkView& f = a.f;
     const int g = blockIdx.x / a.tiles, tile = blockIdx.x - g * a.tiles;
-    const ForkRows r{f, g * a.rows, f.group ? f.group : f.from.n};
+    ForkRows r{f, nullptr, g * a.rows, f.group ? f.group : f.from.n};
     const int n = min(a.rows, f.to.n - r.base);
+    char* free_lds = reinterpret_cast<char*>(shared);
+    if (n <= IN_LDS) {
+        int32_t* kept = reinterpret_cast<int32_t*>(shared);
+        bool any = false;
+        for (int i = threadIdx.x; i < n; i += FORK) {
+            const int src = r.look(i);
+            kept[i] = src;
+            any = any || src == -2 || src != r.base + i;
+        }
+        any = __syncthreads_or(any);
+        if (f.in_place && !any && !f.keep) return;           // every row is its own child
+        r.kept = kept;
+        free_lds += (n + 3) / 4 * 16;
+    }
+    int32_t* lds = reinterpret_cast<int32_t*>(free_lds);
     if (tile == 0) {                                         // lengths
         if (f.in_place) {
-            for (int i = threadIdx.x; i < n; i += 256) lds[i] = f.to.len[r.base + i];
+            for (int i = threadIdx.x; i < n; i += FORK) lds[i] = f.to.len[r.base + i];
             __syncthreads();
         }
-        for (int i = threadIdx.x; i < n; i += 256) {
+        for (int i = threadIdx.x; i < n; i += FORK) {
             const int src = r.source(i);
             if (src == -2) {
                 if (f.status) atomicOr(f.status, 8);
@@ -326,47 +385,59 @@ __global__ void __launch_bounds__(256) k_pages_fork(ForkLaunch a) {
     }
     if (tile > a.table_tiles) {
         int k = f.n_states - 1;
-        while (tile < a.first[k]) --k;
-        const int64_t c0 = (int64_t)(tile - a.first[k]) * a.n_units[k];
-        if (a.unit[k] == 16) fork_states<uint4>(r, f.states[k], c0, a.n_units[k], n, reinterpret_cast<uint4*>(shared));
-        else if (a.unit[k] == 4) fork_states<uint32_t>(r, f.states[k], c0, a.n_units[k], n, reinterpret_cast<uint32_t*>(shared));
-        else fork_states<uint8_t>(r, f.states[k], c0, a.n_units[k], n, reinterpret_cast<uint8_t*>(shared));
+        while (tile < a.state[k].first) --k;
+        const int shift = a.state[k].shift;
+        const int64_t c0 = (int64_t)(tile - a.state[k].first) << shift;
+        if (a.state[k].unit == 16) fork_states<words>(r, f.states[k], c0, shift, n, reinterpret_cast<words*>(free_lds));
+        else if (a.state[k].unit == 4) fork_states<uint32_t>(r, f.states[k], c0, shift, n, reinterpret_cast<uint32_t*>(free_lds));
+        else fork_states<uint8_t>(r, f.states[k], c0, shift, n, reinterpret_cast<uint8_t*>(free_lds));
         return;
     }
-    const int c0 = (tile - 1) * a.cols, nc = min(a.cols, f.to.width - c0);
-    auto entry = [&](int e) -> int32_t* { return f.to.pages + (int64_t)(r.base + e / nc) * f.to.width + c0 + e % nc; };
+    const int shift = a.shift, at = threadIdx.x & ((1 << shift) - 1), j = ((tile - 1) << shift) + at;
+    const int first = threadIdx.x >> shift, step = FORK >> shift;
+    const bool inside = j < f.to.width;
+    int32_t* column = f.to.pages + (int64_t)r.base * f.to.width + j;
     if (f.in_place) {
-        for (int e = threadIdx.x; e < n * nc; e += 256) lds[e] = *entry(e);
+        if (inside)
+#pragma unroll 4
+            for (int i = first; i < n; i += step) lds[(i << shift) + at] = column[(int64_t)i * f.to.width];
         __syncthreads();
     }
     auto each = [&](auto&& change) {                         // change(place, old page, new page) of every entry that changes
-        for (int e = threadIdx.x; e < n * nc; e += 256) {
-            const int i = e / nc, j = c0 + e % nc, src = r.source(i);
+        if (!inside) return;
+        for (int i = first; i < n; i += step) {
+            const int src = r.source(i);
             if (src == -2) continue;
             int fresh = -1;
             if (src >= 0 && j < f.from.width && (!f.keep || (int64_t)j * a.page_size < f.keep[r.base + i]))
-                fresh = f.in_place ? lds[(src - r.base) * nc + e % nc] : f.from.pages[(int64_t)src * f.from.width + j];
-            int32_t* at = entry(e);
-            const int old = f.in_place ? lds[e] : *at;
-            if (fresh != old) change(at, old, fresh);
+                fresh = f.in_place ? lds[((src - r.base) << shift) + at] : f.from.pages[(int64_t)src * f.from.width + j];
+            int32_t* place = column + (int64_t)i * f.to.width;
+            const int old = f.in_place ? lds[(i << shift) + at] : *place;
+            if (fresh != old) change(place, old, fresh);
         }
     };
-    auto take = [&](int page) { if (page >= 0 && page < a.n_pages) atomicAdd(a.refs + page, 1); };
+    auto take = [&](int page) { return page >= 0 && page < a.n_pages ? atomicAdd(a.refs + page, 1) : 0; };
     auto give = [&](int page) {
         if (page >= 0 && page < a.n_pages && atomicSub(a.refs + page, 1) == 1) atomicOr(a.free_bits + (page >> 5), 1u << (page & 31));
     };
     if (f.in_place) {
-        each([&](int32_t*, int, int fresh) { take(fresh); });
-        __threadfence();
+        int counted = 0;
+        each([&](int32_t*, int, int fresh) { counted += take(fresh); });
+        asm volatile("" ::"v"(counted));                     // all of them are done when their results are there
         __syncthreads();
-        each([&](int32_t* at, int old, int fresh) { *at = fresh; give(old); });
+        each([&](int32_t* place, int old, int fresh) { *place = fresh; give(old); });
     } else {
-        each([&](int32_t* at, int old, int fresh) { take(fresh); *at = fresh; give(old); });
+        each([&](int32_t* place, int old, int fresh) { take(fresh); *place = fresh; give(old); });
     }
 }
 
+static int below_shift(int64_t n) {                          // the largest shift of a tile's columns, 1 << shift <= n and FORK
+    int s = 0;
+    while (s < 8 && (2ll << s) <= n) ++s;
+    return s;
+}
+
 int launch_pages_fork(const PagesView& v, const ForkView& f, hipStream_t s) {
-    constexpr int LDS = 65536, TILE = 2048, STATE = 32768;   // bytes a tile may have, entries of a table's, bytes of a state's
     ForkLaunch a;
     a.f = f;
     a.refs = v.refs;
@@ -374,25 +445,28 @@ int launch_pages_fork(const PagesView& v, const ForkView& f, hipStream_t s) {
     a.n_pages = v.n_pages;
     a.page_size = v.page_size;
     a.rows = f.in_place ? (f.group ? f.group : f.to.n) : std::min(16, f.to.n);
-    a.cols = std::max(1, std::min(f.to.width, std::max(TILE / a.rows, std::min(16, LDS / 4 / a.rows))));
-    a.table_tiles = (f.to.width + a.cols - 1) / a.cols;
+    const size_t kept = a.rows <= IN_LDS ? (a.rows + 3) / 4 * 16 : 0, room = LDS - kept;
+    // two entries a thread, but at least 16 columns while LDS has room
+    const int64_t fit = f.in_place ? room / 4 / a.rows : FORK;
+    a.shift = below_shift(std::max<int64_t>(1, std::min<int64_t>(fit, std::max(512 / a.rows, 16))));
+    a.table_tiles = (int)(((int64_t)f.to.width + (1 << a.shift) - 1) >> a.shift);
     int64_t tiles = 1 + a.table_tiles;
-    size_t lds = f.in_place ? (size_t)4 * a.rows * a.cols : 0;
+    size_t lds = f.in_place ? (size_t)4 * a.rows << a.shift : 0;
     for (int k = 0; k < f.n_states; ++k) {
         const StateRows& st = f.states[k];
         const uintptr_t all = (uintptr_t)st.p | (uintptr_t)st.stride | (uintptr_t)st.bytes;
-        const int unit = all % 16 == 0 && 16 * a.rows <= LDS ? 16 : all % 4 == 0 ? 4 : 1;
+        const int unit = all % 16 == 0 && 16 * (size_t)a.rows <= room ? 16 : all % 4 == 0 ? 4 : 1;
         const int64_t units = st.bytes / unit;
-        a.unit[k] = unit;
-        a.n_units[k] = (int)std::max<int64_t>(1, std::min<int64_t>(units, STATE / (a.rows * unit)));
-        a.first[k] = (int)std::min<int64_t>(tiles, 0x7fffffff);
-        tiles += (units + a.n_units[k] - 1) / a.n_units[k];
-        lds = std::max(lds, (size_t)a.rows * a.n_units[k] * unit);
+        a.state[k].unit = unit;
+        a.state[k].shift = below_shift(std::max<int64_t>(1, std::min<int64_t>(room / unit / a.rows, std::max(512 / a.rows, 16))));
+        a.state[k].first = (int)std::min<int64_t>(tiles, 0x7fffffff);
+        tiles += (units + (1 << a.state[k].shift) - 1) >> a.state[k].shift;
+        lds = std::max(lds, (size_t)a.rows * unit << a.state[k].shift);
     }
     const int64_t blocks = (f.to.n + a.rows - 1) / a.rows * tiles;
     if (tiles > 0x7fffffff || blocks > 0x7fffffff) return ee_fail(EE_ERR_SHAPE, "ee_pages_fork: more workgroups than a launch holds");
     a.tiles = (int)tiles;
-    hipLaunchKernelGGL(k_pages_fork, dim3((unsigned)blocks), dim3(256), lds, s, a);
+    hipLaunchKernelGGL(k_pages_fork, dim3((unsigned)blocks), dim3(FORK), kept + lds, s, a);
     EE_LAUNCH_CHECK();
     return EE_OK;
 }
@@ -402,13 +476,13 @@ int launch_pages_fork(const PagesView& v, const ForkView& f, hipStream_t s) {
 // workgroup.  Pages read and pages written are apart, so the copies behind need no order.
 constexpr int PLAN = 1024;
 __global__ void __launch_bounds__(PLAN) k_pages_plan(PagesView v) {
-    __shared__ long long sums[PLAN / 64];
+    __shared__ uint32_t sums[2 * PLAN / 64];
     const int tid = threadIdx.x, words = (v.n_pages + 31) / 32;
-    long long n_free = 0, all;
-    for (int w = tid; w < words; w += PLAN) n_free += __popc(v.free_bits[w]);
-    sum_before<PLAN>(n_free, sums, all);
-    const int used = v.n_pages - (int)all;
-    for (int i = tid; i < v.n_pages; i += PLAN) v.mark[2 * (int64_t)i] = -1;
+    uint32_t n_free[1] = {0}, all[1];
+    for (int w = tid; w < words; w += PLAN) n_free[0] += __popc(v.free_bits[w]);
+    sum_before<PLAN>(n_free, all, sums);
+    const int used = v.n_pages - (int)all[0];
+    for (int i = tid; i < v.n_pages; i += PLAN) v.name[i] = -1;
     int n_holes = 0, n_moved = 0;
     for (int w0 = 0; w0 < words; w0 += PLAN) {
         const int w = w0 + tid;
@@ -421,18 +495,18 @@ __global__ void __launch_bounds__(PLAN) k_pages_plan(PagesView v) {
             moved = ~bits & there & ~below;
             if (holes || moved) v.free_bits[w] = there & ~below;
         }
-        long long both;
-        const long long before = sum_before<PLAN>((long long)__popc(holes) << 32 | (long long)__popc(moved), sums, both);
-        for (int r = n_holes + (int)(before >> 32); holes; ++r, holes &= holes - 1) v.dst[r] = w * 32 + __builtin_ctz(holes);
-        for (int r = n_moved + (int)(before & 0xffffffff); moved; ++r, moved &= moved - 1) v.src[r] = w * 32 + __builtin_ctz(moved);
-        n_holes += (int)(both >> 32);
-        n_moved += (int)(both & 0xffffffff);
+        uint32_t before[2] = {(uint32_t)__popc(holes), (uint32_t)__popc(moved)}, both[2];
+        sum_before<PLAN>(before, both, sums);
+        for (int r = n_holes + (int)before[0]; holes; ++r, holes &= holes - 1) v.dst[r] = w * 32 + __builtin_ctz(holes);
+        for (int r = n_moved + (int)before[1]; moved; ++r, moved &= moved - 1) v.src[r] = w * 32 + __builtin_ctz(moved);
+        n_holes += (int)both[0];
+        n_moved += (int)both[1];
     }
     __threadfence();
     __syncthreads();
     for (int r = tid; r < n_moved; r += PLAN) {
         const int old = v.src[r], page = v.dst[r];
-        v.mark[2 * (int64_t)old] = page;
+        v.name[old] = page;
         v.refs[page] = v.refs[old];
         v.refs[old] = 0;
     }
@@ -452,7 +526,7 @@ int launch_pages_compact(const PagesView& v, const PoolView& pool, const TableVi
     const int n_rename = (int)std::min(256.0, (entries + 1023) / 1024);
     const double items = (double)(v.n_pages / 2 + 1) * pool.n_layers * ((pool.page + PIECE - 1) / PIECE);
     hipLaunchKernelGGL(k_pages_copy, dim3(copy_grid(items) + n_rename), dim3(256), 0, s, pool, pool, v.src, v.dst, v.n_moves, 0, (int32_t*)nullptr, t,
-                       v.mark, n_rename);
+                       v.name, n_rename);
     EE_LAUNCH_CHECK();
     return EE_OK;
 }

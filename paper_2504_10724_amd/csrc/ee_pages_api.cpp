@@ -13,7 +13,7 @@ size_t pages_state(const ee_pages& g, PagesView* v) {
     PagesView w;
     w.refs = (int32_t*)take(4 * n);
     w.free_bits = (uint32_t*)take(4 * ((n + 31) / 32));
-    w.mark = (int32_t*)take(8 * n);
+    w.name = (int32_t*)take(4 * n);
     w.src = (int32_t*)take(4 * moves);
     w.dst = (int32_t*)take(4 * moves);
     w.groups = (int32_t*)take(4 * (size_t)g.max_seqs);
@@ -59,13 +59,14 @@ static int check_table(const std::string& who, const ee_pages* g, const ee_page_
 extern "C" {
 
 size_t ee_pages_state_bytes(const ee_paged* p, int max_seqs) {
-    if (!p || max_seqs < 1 || max_seqs > EE_PAGES_MAX_SEQS) return 0;
+    if (!p || max_seqs < 1 || max_seqs > EE_PAGES_MAX_SEQS || p->cfg.n_pages > PAGES_MOST) return 0;
     return pages_state(ee_pages{p, max_seqs, nullptr}, nullptr);
 }
 
 int ee_pages_bind(const ee_paged* p, int max_seqs, void* dev_state, size_t state_bytes, ee_pages** out) {
     if (!p || !dev_state || !out) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_bind: null pointer");
     if (max_seqs < 1 || max_seqs > EE_PAGES_MAX_SEQS) return ee_fail(EE_ERR_SHAPE, "ee_pages_bind: max_seqs must be 1 to EE_PAGES_MAX_SEQS");
+    if (p->cfg.n_pages > PAGES_MOST) return ee_fail(EE_ERR_SHAPE, "ee_pages_bind: more than 2^21 pages");
     if (state_bytes < ee_pages_state_bytes(p, max_seqs)) return ee_fail(EE_ERR_CAPACITY, "ee_pages_bind: state smaller than ee_pages_state_bytes");
     if ((uintptr_t)dev_state % 256 != 0) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_bind: state must be 256-byte aligned");
     ee_pages* g = new (std::nothrow) ee_pages{p, max_seqs, (char*)dev_state};

@@ -64,6 +64,9 @@ def test_bookkeeping_handles():
         assert lib.ee_pages_state_bytes(p, n) == 0 and lib.ee_pages_bind(p, n, DUMMY, 1 << 60, C.byref(h)) == SHAPE
     assert lib.ee_pages_bind(None, 8, DUMMY, need, C.byref(h)) == BAD and lib.ee_pages_bind(p, 8, None, need, C.byref(h)) == BAD
     assert lib.ee_pages_bind(p, 8, DUMMY, need - 1, C.byref(h)) == CAPACITY and lib.ee_pages_bind(p, 8, C.c_void_p(4097), need, C.byref(h)) == BAD
+    many = _cache(lib, n_layers=1, n_pages=2 ** 21 + 1, n_kv_heads=1, head_dim=64, page_size=32)
+    assert lib.ee_pages_state_bytes(many, 8) == 0 and lib.ee_pages_bind(many, 8, DUMMY, 1 << 60, C.byref(h)) == SHAPE
+    lib.ee_paged_destroy(many)
     assert not h.value and lib.ee_pages_reset(None, None) == BAD
     assert lib.ee_pages_destroy(None) == ee.EE_OK
     lib.ee_paged_destroy(p)
