@@ -631,7 +631,7 @@ typedef struct {
 } ee_rows;
 
 #define EE_PAGES_MAX_SEQS 4096    /* rows of a table that ee_pages_grow takes           */
-#define EE_PAGES_MAX_GROUP 16384  /* rows that are forked among each other              */
+#define EE_PAGES_MAX_GROUP 4096   /* rows that are forked in place among each other     */
 #define EE_PAGES_MAX_ROWS 8       /* arrays of ee_rows, tables of ee_pages_compact      */
 typedef struct ee_pages ee_pages;
 

@@ -14,7 +14,7 @@ EE_ERR_INVALID_ARG, EE_ERR_SHAPE, EE_ERR_CAPACITY = -1, -2, -3
 EE_ERR_LAYER_NOT_RESIDENT, EE_ERR_EXIT_NOT_RESIDENT, EE_ERR_DTYPE, EE_ERR_HIP = -4, -5, -6, -7
 EE_F32, EE_BF16 = 0, 1
 EE_ROPE_HALF, EE_ROPE_INTERLEAVED = 0, 1
-EE_PAGES_MAX_SEQS, EE_PAGES_MAX_GROUP, EE_PAGES_MAX_ROWS = 4096, 16384, 8
+EE_PAGES_MAX_SEQS, EE_PAGES_MAX_GROUP, EE_PAGES_MAX_ROWS = 4096, 4096, 8
 EE_ROPE_UNSCALED, EE_ROPE_LINEAR, EE_ROPE_BASE, EE_ROPE_BANDS = 0, 1, 2, 3
 
 

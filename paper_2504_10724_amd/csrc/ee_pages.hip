@@ -304,11 +304,13 @@ int launch_pages_copy(const PoolView& from, const PoolView& to, const int32_t* s
 // ------------------------------------------------------------------ fork
 // A workgroup takes a tile: some columns of the rows that are forked among each other (in place: all of them, through LDS, so that every
 // entry is read before one is written) or of 16 rows (from another table).  Tile 0 has the lengths, then come the table's columns, then those
-// of the states.  Entries that stay cost nothing but their reads: beams of one request share most of theirs.
+// of the states.  Entries that stay cost nothing but their reads: beams of one request share most of theirs.  Bound by trips to memory one behind the
+// other: parents and entries are asked for together, then counts go up and down, then pages that are free are marked.
 //
 // Counts: what a row takes is counted before what it gives up is counted down, each by atomics; and a page that a row takes is named by that row's
 // parent until the tile that takes it has counted it.  So a count falls to 0 once, in the thread that frees the page, whatever the order.
-constexpr int FORK = 256, LDS = 65536, IN_LDS = 2048;        // threads; bytes a workgroup may have; rows whose parents it keeps there
+constexpr int FORK = 256, LDS = 65536;                       // threads; bytes a workgroup may have
+constexpr int FEW_ROWS = 8, AT_ONCE = 4;                     // rows of a column that one thread takes; entries that it has under way
 struct ForkLaunch {
     ForkView f;
     int32_t* refs;
@@ -320,66 +322,75 @@ struct ForkLaunch {
 
 struct ForkRows {
     const ForkView& f;
-    const int32_t* kept;                                     // in LDS, or null
-    int base, limit;
-    // the row of `from` that row i of the group takes; -1: none, -2: it stays as it is
-    __device__ __forceinline__ int look(int i) const {
-        const int row = base + i, p = f.parent[row];
-        if (p < -1 || p >= limit || (f.keep && f.keep[row] < 0)) return -2;
-        return p < 0 ? -1 : (f.group ? row / f.group * f.group : 0) + p;
+    int32_t* kept;                                           // in LDS, of each row its source and the columns that it keeps
+    int base, n, limit, page_size;
+    struct Row { int src, cols; };
+    // the row of `from` that row i of the group takes (-1: none, -2: it stays as it is), and how many of its columns
+    __device__ __forceinline__ Row make(int i, int parent, int keep) const {
+        const int row = base + i;
+        if (parent < -1 || parent >= limit || keep < 0) return Row{-2, 0};
+        return Row{parent < 0 ? -1 : (f.group ? row / f.group * f.group : 0) + parent, f.keep ? (int)(((int64_t)keep + page_size - 1) / page_size) : 0x7fffffff};
     }
-    __device__ __forceinline__ int source(int i) const { return kept ? kept[i] : look(i); }
+    __device__ __forceinline__ int parent_of(int i) const { return i < n ? f.parent[base + i] : 0; }
+    __device__ __forceinline__ int keep_of(int i) const { return i < n && f.keep ? f.keep[base + i] : 0; }
+    __device__ __forceinline__ Row row(int i) const { return Row{kept[2 * i], kept[2 * i + 1]}; }
+    // a thread's first row comes in registers, asked for before this
+    __device__ __forceinline__ void keep_rows(int parent, int keep) const {
+#pragma unroll 1
+        for (int i = threadIdx.x; i < n; i += FORK) {
+            const Row r = i == (int)threadIdx.x ? make(i, parent, keep) : make(i, parent_of(i), keep_of(i));
+            kept[2 * i] = r.src;
+            kept[2 * i + 1] = r.cols;
+        }
+    }
 };
 
-template <class U> __device__ __forceinline__ void fork_states(const ForkRows& r, const StateRows& st, int64_t c0, int shift, int n, U* lds) {
-    const int64_t units = st.bytes / (int64_t)sizeof(U), c = c0 + (threadIdx.x & ((1 << shift) - 1));
-    const int first = threadIdx.x >> shift, step = FORK >> shift, at = threadIdx.x & ((1 << shift) - 1);
+template <class U> __device__ __forceinline__ void fork_states(const ForkRows& r, const StateRows& st, int64_t c0, int shift, int parent, int keep, U* lds) {
+    const int at = threadIdx.x & ((1 << shift) - 1), first = threadIdx.x >> shift, step = FORK >> shift;
+    const int64_t units = st.bytes / (int64_t)sizeof(U), c = c0 + at;
+    auto place = [&](int i) { return reinterpret_cast<U*>(st.p + (int64_t)(r.base + i) * st.stride) + c; };
     if (c < units)
-#pragma unroll 4
-        for (int i = first; i < n; i += step) lds[(i << shift) + at] = reinterpret_cast<const U*>(st.p + (int64_t)(r.base + i) * st.stride)[c];
+#pragma unroll 1
+        for (int i0 = first; i0 < r.n; i0 += AT_ONCE * step) {
+            U x[AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) x[k] = *place(min(i0 + k * step, r.n - 1));
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k)
+                if (i0 + k * step < r.n) lds[((i0 + k * step) << shift) + at] = x[k];
+        }
+    r.keep_rows(parent, keep);
     __syncthreads();
     if (c < units)
-        for (int i = first; i < n; i += step) {
-            const int src = r.source(i) - r.base;
-            if (src >= 0 && src != i) reinterpret_cast<U*>(st.p + (int64_t)(r.base + i) * st.stride)[c] = lds[(src << shift) + at];
+#pragma unroll 1
+        for (int i = first; i < r.n; i += step) {
+            const int src = r.row(i).src - r.base;
+            if (src >= 0 && src != i) *place(i) = lds[(src << shift) + at];
         }
 }
 
 __global__ void __launch_bounds__(FORK) k_pages_fork(ForkLaunch a) {
     extern __shared__ words shared[];
     const ForkView& f = a.f;
-    const int g = blockIdx.x / a.tiles, tile = blockIdx.x - g * a.tiles;
-    ForkRows r{f, nullptr, g * a.rows, f.group ? f.group : f.from.n};
-    const int n = min(a.rows, f.to.n - r.base);
-    char* free_lds = reinterpret_cast<char*>(shared);
-    if (n <= IN_LDS) {
-        int32_t* kept = reinterpret_cast<int32_t*>(shared);
-        bool any = false;
-        for (int i = threadIdx.x; i < n; i += FORK) {
-            const int src = r.look(i);
-            kept[i] = src;
-            any = any || src == -2 || src != r.base + i;
-        }
-        any = __syncthreads_or(any);
-        if (f.in_place && !any && !f.keep) return;           // every row is its own child
-        r.kept = kept;
-        free_lds += (n + 3) / 4 * 16;
-    }
+    const int g = blockIdx.x / a.tiles, tile = blockIdx.x - g * a.tiles, tid = threadIdx.x, base = g * a.rows;
+    const ForkRows r{f, reinterpret_cast<int32_t*>(shared), base, min(a.rows, f.to.n - base), f.group ? f.group : f.from.n, a.page_size};
+    const int n = r.n, parent = r.parent_of(tid), keep = r.keep_of(tid);
+    char* free_lds = reinterpret_cast<char*>(shared) + (a.rows + 1) / 2 * 16;
     int32_t* lds = reinterpret_cast<int32_t*>(free_lds);
     if (tile == 0) {                                         // lengths
-        if (f.in_place) {
-            for (int i = threadIdx.x; i < n; i += FORK) lds[i] = f.to.len[r.base + i];
-            __syncthreads();
-        }
-        for (int i = threadIdx.x; i < n; i += FORK) {
-            const int src = r.source(i);
+        if (f.in_place)
+            for (int i = tid; i < n; i += FORK) lds[i] = f.to.len[base + i];
+        r.keep_rows(parent, keep);
+        __syncthreads();
+        for (int i = tid; i < n; i += FORK) {
+            const int src = r.row(i).src;
             if (src == -2) {
                 if (f.status) atomicOr(f.status, 8);
                 continue;
             }
-            int len = src < 0 ? 0 : f.in_place ? lds[src - r.base] : f.from.len[src];
-            if (f.keep) len = min(len, f.keep[r.base + i]);
-            f.to.len[r.base + i] = len;
+            int len = src < 0 ? 0 : f.in_place ? lds[src - base] : f.from.len[src];
+            if (f.keep) len = min(len, f.keep[base + i]);
+            f.to.len[base + i] = len;
         }
         return;
     }
@@ -388,46 +399,118 @@ __global__ void __launch_bounds__(FORK) k_pages_fork(ForkLaunch a) {
         while (tile < a.state[k].first) --k;
         const int shift = a.state[k].shift;
         const int64_t c0 = (int64_t)(tile - a.state[k].first) << shift;
-        if (a.state[k].unit == 16) fork_states<words>(r, f.states[k], c0, shift, n, reinterpret_cast<words*>(free_lds));
-        else if (a.state[k].unit == 4) fork_states<uint32_t>(r, f.states[k], c0, shift, n, reinterpret_cast<uint32_t*>(free_lds));
-        else fork_states<uint8_t>(r, f.states[k], c0, shift, n, reinterpret_cast<uint8_t*>(free_lds));
+        if (a.state[k].unit == 16) fork_states<words>(r, f.states[k], c0, shift, parent, keep, reinterpret_cast<words*>(free_lds));
+        else if (a.state[k].unit == 4) fork_states<uint32_t>(r, f.states[k], c0, shift, parent, keep, reinterpret_cast<uint32_t*>(free_lds));
+        else fork_states<uint8_t>(r, f.states[k], c0, shift, parent, keep, reinterpret_cast<uint8_t*>(free_lds));
         return;
     }
-    const int shift = a.shift, at = threadIdx.x & ((1 << shift) - 1), j = ((tile - 1) << shift) + at;
-    const int first = threadIdx.x >> shift, step = FORK >> shift;
+    const int shift = a.shift, at = tid & ((1 << shift) - 1), j = ((tile - 1) << shift) + at, first = tid >> shift, step = FORK >> shift;
     const bool inside = j < f.to.width;
-    int32_t* column = f.to.pages + (int64_t)r.base * f.to.width + j;
-    if (f.in_place) {
-        if (inside)
-#pragma unroll 4
-            for (int i = first; i < n; i += step) lds[(i << shift) + at] = column[(int64_t)i * f.to.width];
+    int32_t* column = f.to.pages + (int64_t)base * f.to.width + j;
+    auto page_ok = [&](int page) { return page >= 0 && page < a.n_pages; };
+    auto free_page = [&](int page) { atomicOr(a.free_bits + (page >> 5), 1u << (page & 31)); };
+
+    if (f.in_place && a.rows <= FEW_ROWS) {
+        // A thread has a column.  Its atomics on one page are done in its order, so what it takes need not be waited for before it gives.
+        const bool mine = inside && first == 0;
+        int old[FEW_ROWS], fresh[FEW_ROWS], left[FEW_ROWS];
+#pragma unroll
+        for (int i = 0; i < FEW_ROWS; ++i) old[i] = mine && i < n ? column[(int64_t)i * f.to.width] : -1;
+        r.keep_rows(parent, keep);
+#pragma unroll
+        for (int i = 0; i < FEW_ROWS; ++i)
+            if (i < n) lds[i * FORK + tid] = old[i];
         __syncthreads();
+        if (!mine) return;
+#pragma unroll
+        for (int i = 0; i < FEW_ROWS; ++i) {
+            fresh[i] = old[i];
+            if (i >= n) continue;
+            const ForkRows::Row row = r.row(i);
+            if (row.src == -2) continue;
+            fresh[i] = row.src >= 0 && j < row.cols ? lds[(row.src - base) * FORK + tid] : -1;
+            if (fresh[i] != old[i]) {
+                column[(int64_t)i * f.to.width] = fresh[i];
+                if (page_ok(fresh[i])) atomicAdd(a.refs + fresh[i], 1);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < FEW_ROWS; ++i) left[i] = fresh[i] != old[i] && page_ok(old[i]) ? atomicSub(a.refs + old[i], 1) : 0;
+#pragma unroll
+        for (int i = 0; i < FEW_ROWS; ++i)
+            if (left[i] == 1) free_page(old[i]);
+        return;
     }
-    auto each = [&](auto&& change) {                         // change(place, old page, new page) of every entry that changes
-        if (!inside) return;
-        for (int i = first; i < n; i += step) {
-            const int src = r.source(i);
-            if (src == -2) continue;
-            int fresh = -1;
-            if (src >= 0 && j < f.from.width && (!f.keep || (int64_t)j * a.page_size < f.keep[r.base + i]))
-                fresh = f.in_place ? lds[((src - r.base) << shift) + at] : f.from.pages[(int64_t)src * f.from.width + j];
-            int32_t* place = column + (int64_t)i * f.to.width;
-            const int old = f.in_place ? lds[(i << shift) + at] : *place;
-            if (fresh != old) change(place, old, fresh);
+
+    if (f.in_place && inside)
+#pragma unroll 1
+        for (int i0 = first; i0 < n; i0 += AT_ONCE * step) {
+            int x[AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) x[k] = column[(int64_t)min(i0 + k * step, n - 1) * f.to.width];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k)
+                if (i0 + k * step < n) lds[((i0 + k * step) << shift) + at] = x[k];
+        }
+    r.keep_rows(parent, keep);
+    __syncthreads();
+    // AT_ONCE entries of a column: what they are and what they become, the same where a row stays
+    int old[AT_ONCE], fresh[AT_ONCE];
+    auto look = [&](int i0) {
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int i = min(i0 + k * step, n - 1);
+            const ForkRows::Row row = r.row(i);
+            old[k] = f.in_place ? lds[(i << shift) + at] : column[(int64_t)i * f.to.width];
+            fresh[k] = -1;
+            if (row.src >= 0 && j < row.cols && j < f.from.width)
+                fresh[k] = f.in_place ? lds[((row.src - base) << shift) + at] : f.from.pages[(int64_t)row.src * f.from.width + j];
+            if (row.src == -2 || i0 + k * step >= n) fresh[k] = old[k];
         }
     };
-    auto take = [&](int page) { return page >= 0 && page < a.n_pages ? atomicAdd(a.refs + page, 1) : 0; };
-    auto give = [&](int page) {
-        if (page >= 0 && page < a.n_pages && atomicSub(a.refs + page, 1) == 1) atomicOr(a.free_bits + (page >> 5), 1u << (page & 31));
+    auto take = [&] {
+        int counted = 0;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k)
+            if (fresh[k] != old[k] && page_ok(fresh[k])) counted += atomicAdd(a.refs + fresh[k], 1);
+        return counted;
+    };
+    auto give = [&](int i0) {
+        int left[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            left[k] = 0;
+            if (fresh[k] == old[k]) continue;
+            column[(int64_t)(i0 + k * step) * f.to.width] = fresh[k];
+            if (page_ok(old[k])) left[k] = atomicSub(a.refs + old[k], 1);
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k)
+            if (left[k] == 1) free_page(old[k]);
     };
     if (f.in_place) {
         int counted = 0;
-        each([&](int32_t*, int, int fresh) { counted += take(fresh); });
+        if (inside)
+#pragma unroll 1
+            for (int i0 = first; i0 < n; i0 += AT_ONCE * step) {
+                look(i0);
+                counted += take();
+            }
         asm volatile("" ::"v"(counted));                     // all of them are done when their results are there
         __syncthreads();
-        each([&](int32_t* place, int old, int fresh) { *place = fresh; give(old); });
-    } else {
-        each([&](int32_t* place, int old, int fresh) { take(fresh); *place = fresh; give(old); });
+        if (inside)
+#pragma unroll 1
+            for (int i0 = first; i0 < n; i0 += AT_ONCE * step) {
+                look(i0);
+                give(i0);
+            }
+    } else if (inside) {
+#pragma unroll 1
+        for (int i0 = first; i0 < n; i0 += AT_ONCE * step) {
+            look(i0);
+            take();
+            give(i0);
+        }
     }
 }
 
@@ -445,13 +528,15 @@ int launch_pages_fork(const PagesView& v, const ForkView& f, hipStream_t s) {
     a.n_pages = v.n_pages;
     a.page_size = v.page_size;
     a.rows = f.in_place ? (f.group ? f.group : f.to.n) : std::min(16, f.to.n);
-    const size_t kept = a.rows <= IN_LDS ? (a.rows + 3) / 4 * 16 : 0, room = LDS - kept;
-    // two entries a thread, but at least 16 columns while LDS has room
+    const size_t kept = (a.rows + 1) / 2 * 16, room = LDS - kept;
+    const bool few = f.in_place && a.rows <= FEW_ROWS;
+    // few rows: a column a thread.  Else about an entry a thread, but at least four columns while LDS has room.
     const int64_t fit = f.in_place ? room / 4 / a.rows : FORK;
-    a.shift = below_shift(std::max<int64_t>(1, std::min<int64_t>(fit, std::max(512 / a.rows, 16))));
+    a.shift = few ? below_shift(std::max(f.to.width, 1)) : below_shift(std::max<int64_t>(1, std::min<int64_t>(fit, std::max(FORK / a.rows, 4))));
+    if (few && (1 << a.shift) < std::min(f.to.width, FORK)) ++a.shift;
     a.table_tiles = (int)(((int64_t)f.to.width + (1 << a.shift) - 1) >> a.shift);
     int64_t tiles = 1 + a.table_tiles;
-    size_t lds = f.in_place ? (size_t)4 * a.rows << a.shift : 0;
+    size_t lds = f.in_place ? (size_t)4 * a.rows * (few ? FORK : 1 << a.shift) : 0;
     for (int k = 0; k < f.n_states; ++k) {
         const StateRows& st = f.states[k];
         const uintptr_t all = (uintptr_t)st.p | (uintptr_t)st.stride | (uintptr_t)st.bytes;
@@ -478,8 +563,9 @@ constexpr int PLAN = 1024;
 __global__ void __launch_bounds__(PLAN) k_pages_plan(PagesView v) {
     __shared__ uint32_t sums[2 * PLAN / 64];
     const int tid = threadIdx.x, words = (v.n_pages + 31) / 32;
-    uint32_t n_free[1] = {0}, all[1];
-    for (int w = tid; w < words; w += PLAN) n_free[0] += __popc(v.free_bits[w]);
+    const uint32_t first = tid < words ? v.free_bits[tid] : 0u;
+    uint32_t n_free[1] = {(uint32_t)__popc(first)}, all[1];
+    for (int w = tid + PLAN; w < words; w += PLAN) n_free[0] += __popc(v.free_bits[w]);
     sum_before<PLAN>(n_free, all, sums);
     const int used = v.n_pages - (int)all[0];
     for (int i = tid; i < v.n_pages; i += PLAN) v.name[i] = -1;
@@ -488,7 +574,7 @@ __global__ void __launch_bounds__(PLAN) k_pages_plan(PagesView v) {
         const int w = w0 + tid;
         uint32_t holes = 0, moved = 0;
         if (w < words) {
-            const uint32_t bits = v.free_bits[w], there = w == words - 1 && v.n_pages % 32 ? (1u << v.n_pages % 32) - 1 : ~0u;
+            const uint32_t bits = w0 == 0 ? first : v.free_bits[w], there = w == words - 1 && v.n_pages % 32 ? (1u << v.n_pages % 32) - 1 : ~0u;
             const int64_t low = (int64_t)used - (int64_t)w * 32;             // pages of this word that lie below `used`
             const uint32_t below = low >= 32 ? ~0u : low <= 0 ? 0u : (1u << low) - 1;
             holes = bits & below;
@@ -502,8 +588,7 @@ __global__ void __launch_bounds__(PLAN) k_pages_plan(PagesView v) {
         n_holes += (int)both[0];
         n_moved += (int)both[1];
     }
-    __threadfence();
-    __syncthreads();
+    __syncthreads();                                         // the lists are this workgroup's own
     for (int r = tid; r < n_moved; r += PLAN) {
         const int old = v.src[r], page = v.dst[r];
         v.name[old] = page;

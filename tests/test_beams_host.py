@@ -114,7 +114,7 @@ def test_bookkeeping_calls():
     assert fork(source=_table(n_seqs=8, **other), group=4) == SHAPE                # groups of unlike tables
     assert fork(source=_table(pages_per_seq=4, **other)) == SHAPE                  # rows that do not fit
     assert fork(source=_table(dev_pages=16384)) == BAD and fork(source=_table(dev_kv_len=16384)) == BAD and fork(source=_table(n_seqs=3)) == BAD
-    assert fork(to=_table(n_seqs=16385)) == SHAPE and fork(to=_table(n_seqs=32770), group=16385) == SHAPE
+    assert fork(to=_table(n_seqs=4097)) == SHAPE and fork(to=_table(n_seqs=8194), group=4097) == SHAPE
     rows = ee.ee_rows(4096, 64, 64)
     assert fork(states=[rows] * 9) == SHAPE and fork(source=_table(**other), states=[rows]) == BAD
     assert fork(states=[ee.ee_rows(4096, 63, 64)]) == BAD and fork(states=[ee.ee_rows(4096, 64, -1)]) == BAD

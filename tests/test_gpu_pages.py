@@ -204,8 +204,8 @@ def test_forks_in_place(n, group, width):
     assert torch.equal(dev.cpu(), want)
 
 
-def test_a_fork_among_more_rows_than_grow():
-    """16384 rows of another table, forked in place among each other"""
+def test_forks_of_more_rows_than_grow():
+    """16384 rows from another table, in groups of 4096 among each other"""
     print("[case] fork 16384", flush=True)
     n = 16384
     c = Pair(50, 32, layers=1, hkv=1, hd=4, values=False)
@@ -214,10 +214,12 @@ def test_a_fork_among_more_rows_than_grow():
     c.grow(store, [r.randint(1, 64) for _ in range(20)])
     c.fork(t, [r.randrange(-1, 20) for _ in range(n)], source=store)
     c.check("taken")
-    c.fork(t, [r.randrange(-1, n) for _ in range(n)], rows=[torch.randint(0, 99, (n, 8), dtype=torch.int32)], keep=[r.randint(0, 70) for _ in range(n)])
+    c.fork(t, [r.randrange(-1, 4096) for _ in range(n)], group=4096, rows=[torch.randint(0, 99, (n, 8), dtype=torch.int32)],
+           keep=[r.randint(0, 70) for _ in range(n)])
     c.check("forked")
-    with pytest.raises(ee.EEError):
-        c.pages.grow(t[0])
+    for call in (lambda: c.pages.grow(t[0]), lambda: c.pages.fork(t[0], _i32([0] * n))):
+        with pytest.raises(ee.EEError):
+            call()
 
 
 @pytest.mark.parametrize("n,n_pages", [(1, 1), (3, 32), (700, 5000), (1024, 9000), (1025, 9000), (4096, 40000)])
