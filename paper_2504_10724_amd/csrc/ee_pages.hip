@@ -218,21 +218,29 @@ k_pages_grow(PagesView v, TableView t, const int32_t* __restrict__ more, int32_t
 }
 
 // ------------------------------------------------------------------ copies
-// 16 bytes a lane, four at a time.  Bound by the bytes read and written.
+// 16 bytes a lane, four at a time.  Bound by the bytes read and written.  ONCE: past the caches.
 typedef uint32_t words __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void copy_run(const char* __restrict__ src, char* __restrict__ dst, int bytes) {
+template <bool ONCE> __device__ __forceinline__ words get(const words* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool ONCE> __device__ __forceinline__ void put(words w, words* p) {
+    if constexpr (ONCE) __builtin_nontemporal_store(w, p);
+    else *p = w;
+}
+template <bool ONCE> __device__ __forceinline__ void copy_run(const char* __restrict__ src, char* __restrict__ dst, int bytes) {
     const words* a = reinterpret_cast<const words*>(src);
     words* b = reinterpret_cast<words*>(dst);
     const int n = bytes / 16;
     int o = threadIdx.x;
     for (; o + 768 < n; o += 1024) {
-        const words w = a[o], x = a[o + 256], y = a[o + 512], z = a[o + 768];
-        b[o] = w;
-        b[o + 256] = x;
-        b[o + 512] = y;
-        b[o + 768] = z;
+        const words w = get<ONCE>(a + o), x = get<ONCE>(a + o + 256), y = get<ONCE>(a + o + 512), z = get<ONCE>(a + o + 768);
+        put<ONCE>(w, b + o);
+        put<ONCE>(x, b + o + 256);
+        put<ONCE>(y, b + o + 512);
+        put<ONCE>(z, b + o + 768);
     }
-    for (; o < n; o += 256) b[o] = a[o];
+    for (; o < n; o += 256) put<ONCE>(get<ONCE>(a + o), b + o);
 }
 
 // the listed pages' first groups of 32 positions, in all layers: an item is one group of one block
@@ -243,14 +251,15 @@ __global__ void __launch_bounds__(256) k_pages_copy_groups(PagesView v, PoolView
         const int c = (int)(i / per), layer = (int)((i - c * per) / per_page), piece = (int)(i - c * per - (int64_t)layer * per_page);
         if (piece % pool.subs >= v.groups[c]) continue;
         char* p = pool.p + layer * pool.layer + (int64_t)piece * pool.sub;
-        copy_run(p + v.src[c] * pool.page, p + v.dst[c] * pool.page, pool.sub);
+        copy_run<false>(p + v.src[c] * pool.page, p + v.dst[c] * pool.page, pool.sub);
     }
 }
 
 // Whole pages in all layers: an item is PIECE bytes of a page in one layer.  n_moves null: `pairs` of them.  The first n_rename workgroups
 // give the tables' pages that move their new numbers instead.
-constexpr int PIECE = 16384, WORKGROUPS = 2048;              // eight a compute unit
+constexpr int PIECE = 16384;
 struct Tables { TableView t[EE_PAGES_MAX_ROWS]; int32_t n; };
+template <bool ONCE>
 __global__ void __launch_bounds__(256)
 k_pages_copy(PoolView from, PoolView to, const int32_t* __restrict__ src, const int32_t* __restrict__ dst, const int32_t* __restrict__ n_moves,
              int pairs, int32_t* status, Tables tables, const int32_t* __restrict__ name, int n_rename) {
@@ -276,27 +285,34 @@ k_pages_copy(PoolView from, PoolView to, const int32_t* __restrict__ src, const 
             continue;
         }
         const int64_t at = (int64_t)piece * PIECE;
-        copy_run(from.p + layer * from.layer + a * from.page + at, to.p + layer * to.layer + b * to.page + at, (int)min((int64_t)PIECE, from.page - at));
+        copy_run<ONCE>(from.p + layer * from.layer + a * from.page + at, to.p + layer * to.layer + b * to.page + at, (int)min((int64_t)PIECE, from.page - at));
     }
 }
 
-static unsigned copy_grid(double items) { return (unsigned)std::max(1.0, std::min(items, (double)WORKGROUPS)); }
+// Groups: eight workgroups a CU (54.6 us for beams_70b_b256's 279 MB, four 54.2, two 58.1).  Whole pages past the caches: two a CU of 16 KB each, or
+// as many bytes under way of smaller pages (173 pages of 4 MB: 269 us, 5.4 TB/s, with one a CU 262, four 276, eight 276; through the caches two 284,
+// eight 285).
+static unsigned copy_grid(double items, double most) { return (unsigned)std::max(1.0, std::min(items, most)); }
+static unsigned whole_grid(const PoolView& p, double pages) {
+    return copy_grid(pages * p.n_layers * ((p.page + PIECE - 1) / PIECE), std::min(2048.0, 512.0 * PIECE / std::min<int64_t>(PIECE, p.page)));
+}
+constexpr double CACHED_BYTES = 100e6;                       // read and written; past the caches and through them: 67 MB 13.5 and 11.5 us, 134 MB 24.9 and 27.9
 
 int launch_pages_grow(const PagesView& v, const PoolView& pool, const TableView& t, const int32_t* more, int32_t* status, hipStream_t s) {
     if (t.n <= GROW) hipLaunchKernelGGL(k_pages_grow<1>, dim3(1), dim3(GROW), 0, s, v, t, more, status);
     else             hipLaunchKernelGGL(k_pages_grow<EE_PAGES_MAX_SEQS / GROW>, dim3(1), dim3(GROW), 0, s, v, t, more, status);
     EE_LAUNCH_CHECK();
-    hipLaunchKernelGGL(k_pages_copy_groups, dim3(copy_grid((double)t.n * pool.n_layers * pool.blocks * pool.subs)), dim3(256), 0, s, v, pool);
+    hipLaunchKernelGGL(k_pages_copy_groups, dim3(copy_grid((double)t.n * pool.n_layers * pool.blocks * pool.subs, 2048)), dim3(256), 0, s, v, pool);
     EE_LAUNCH_CHECK();
     return EE_OK;
 }
 
 int launch_pages_copy(const PoolView& from, const PoolView& to, const int32_t* src, const int32_t* dst, int n, int32_t* status, hipStream_t s) {
-    const double items = (double)n * from.n_layers * ((from.page + PIECE - 1) / PIECE);
     Tables none;
     none.n = 0;
-    hipLaunchKernelGGL(k_pages_copy, dim3(copy_grid(items)), dim3(256), 0, s, from, to, src, dst, (const int32_t*)nullptr, n, status, none,
-                       (const int32_t*)nullptr, 0);
+    const bool once = 2.0 * n * from.n_layers * from.page > CACHED_BYTES;
+    hipLaunchKernelGGL((once ? k_pages_copy<true> : k_pages_copy<false>), dim3(whole_grid(from, n)), dim3(256), 0, s, from, to, src, dst,
+                       (const int32_t*)nullptr, n, status, none, (const int32_t*)nullptr, 0);
     EE_LAUNCH_CHECK();
     return EE_OK;
 }
@@ -609,9 +625,10 @@ int launch_pages_compact(const PagesView& v, const PoolView& pool, const TableVi
         entries += (double)tables[i].n * tables[i].width;
     }
     const int n_rename = (int)std::min(256.0, (entries + 1023) / 1024);
-    const double items = (double)(v.n_pages / 2 + 1) * pool.n_layers * ((pool.page + PIECE - 1) / PIECE);
-    hipLaunchKernelGGL(k_pages_copy, dim3(copy_grid(items) + n_rename), dim3(256), 0, s, pool, pool, v.src, v.dst, v.n_moves, 0, (int32_t*)nullptr, t,
-                       v.name, n_rename);
+    // how many pages move is known on the device only
+    const bool once = (double)v.n_pages * pool.n_layers * pool.page > CACHED_BYTES;
+    hipLaunchKernelGGL((once ? k_pages_copy<true> : k_pages_copy<false>), dim3(whole_grid(pool, v.n_pages / 2 + 1) + n_rename), dim3(256), 0, s, pool, pool,
+                       v.src, v.dst, v.n_moves, 0, (int32_t*)nullptr, t, v.name, n_rename);
     EE_LAUNCH_CHECK();
     return EE_OK;
 }
