@@ -82,7 +82,7 @@ __device__ __forceinline__ float of_order(uint32_t u) { return __uint_as_float(u
 // values still reach it.  No smaller than the lowest finite number.
 template <int N> __device__ __forceinline__ float reached_by(const uint32_t (&v)[N], int keep) {
     uint32_t t = 0;
-#pragma unroll 1
+#pragma unroll 4
     for (int bit = 31; bit >= 0; --bit) {
         const uint32_t u = t | (1u << bit);
         int n = 0;
@@ -351,7 +351,7 @@ struct Ratio {
     explicit Ratio(uint32_t d) : d(d), m((uint32_t)(((1ull << 32) + d - 1) / d)) {}
     __device__ __forceinline__ int of(int j) const { return d == 1 ? j : (int)__umulhi((uint32_t)j, m); }
 };
-template <bool FEW, int JOIN = FEW ? 256 : 1024>
+template <bool FEW, int JOIN = FEW ? 256 : 512>
 __global__ void __launch_bounds__(JOIN)
 k_beam_join(BeamParts parts, const float* score, const uint8_t* done, int beams, int vocab, int n_slices, int keep, int end_token, Ratio by_room,
             Ratio by_slices, ee_beam_choice out) {
@@ -530,7 +530,7 @@ int launch_beam_select(const ee_beam_config& c, const void* logits, int64_t stri
     else go((const float*)logits);
     EE_LAUNCH_CHECK();
     const bool few = (int64_t)c.beams * n_slices * parts.room <= FEW_PLACES;
-    hipLaunchKernelGGL((few ? k_beam_join<true> : k_beam_join<false>), dim3((unsigned)c.n_groups), dim3(few ? 256 : 1024), 0, s, parts, score, done, c.beams,
+    hipLaunchKernelGGL((few ? k_beam_join<true> : k_beam_join<false>), dim3((unsigned)c.n_groups), dim3(few ? 256 : 512), 0, s, parts, score, done, c.beams,
                        c.vocab, n_slices, c.keep, c.end_token, Ratio((uint32_t)parts.room), Ratio((uint32_t)n_slices), out);
     EE_LAUNCH_CHECK();
     return EE_OK;

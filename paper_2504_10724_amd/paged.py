@@ -322,12 +322,12 @@ class Pages:
         _number("Pages.fork", group)
         packed = []
         for x in rows:
-            if x.dim() < 1 or x.shape[0] != table.n_seqs or x.get_device() != self.device or not (x.shape[0] == 0 or x[0].is_contiguous()):
+            if x.dim() < 1 or x.shape[0] != table.n_seqs or x.get_device() != self.device or not (x.is_contiguous() or x[0].is_contiguous()):
                 _refuse(f"Pages.fork: rows must be [{table.n_seqs}][...] on device {self.device}, each row contiguous, got {tuple(x.shape)} on {x.device}")
             if x.requires_grad and torch.is_grad_enabled():
                 _lost("Pages.fork")
             size = x.element_size()
-            packed.append(_pack_rows(x.data_ptr(), x.stride(0) * size, x.numel() // max(x.shape[0], 1) * size))
+            packed.append(_pack_rows(x.data_ptr(), x.stride(0) * size, x.numel() // max(table.n_seqs, 1) * size))
         ee.check(self.lib.ee_pages_fork(self.h, table.ref, None if source is None else source.ref, self._ints(parent, "Pages.fork: parent", table.n_seqs),
                                         self._ints(keep, "Pages.fork: keep", table.n_seqs), group, b"".join(packed) or None, len(packed),
                                         self._ints(status, "Pages.fork: status", 1), _stream(self.device)))

@@ -40,7 +40,10 @@ def _inputs(groups, beams, vocab, dtype, seed, spread=2.0):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("groups,beams,vocab,keep", [
     (1, 1, 1, 1), (1, 1, 1, 5), (3, 2, 1, 2), (2, 4, 2048, 4), (1, 5, 32000, 10), (5, 3, 4097, 7), (2, 2, 8193, 128), (1, 64, 333, 128),
-    (2, 7, 12289, 64), (3, 1, 4095, 1), (1, 3, 70001, 33), (65, 4, 130, 8), (1, 12, 100, 100), (2, 64, 4200, 64)])
+    (2, 7, 12289, 64), (3, 1, 4095, 1), (1, 3, 70001, 33), (65, 4, 130, 8), (1, 12, 100, 100), (2, 64, 4200, 64),
+    # what one workgroup has at most, and one more
+    (2, 1, 16384, 32), (2, 1, 16385, 32), (3, 4, 4096, 32), (3, 4, 4097, 32), (1, 9, 1024, 18), (1, 9, 1025, 18), (2, 64, 1024, 32), (2, 2, 8192, 33),
+    (1, 3, 3, 9), (2, 5, 7, 4), (1, 2, 8, 16)])
 def test_against_the_definition(groups, beams, vocab, keep, dtype):
     print(f"[case] select {groups} x {beams} of {vocab}, {keep} kept, {dtype}", flush=True)
     z, score = _inputs(groups, beams, vocab, dtype, 7 * vocab + keep)
@@ -76,22 +79,24 @@ def test_rows_at_any_stride_and_alignment(dtype, offset, pad):
     _check(B.select(same, score.cuda(), 3, keep=6), R.choose(z[:1].expand(6, vocab), score, 3, 6))
 
 
-def test_values_that_are_no_numbers():
+@pytest.mark.parametrize("vocab", [6000, 1500])
+def test_values_that_are_no_numbers(vocab):
     """masks of -inf and of the type's lowest value, rows that leave nothing, infinities and NaN, scores that are none"""
-    print("[case] no numbers", flush=True)
+    print(f"[case] no numbers {vocab}", flush=True)
+    last = vocab * 3 // 4
     for dtype in ("f32", "bf16"):
         low = torch.finfo(DT[dtype]).min
-        z, score = _inputs(9, 3, 6000, dtype, 21)
+        z, score = _inputs(9, 3, vocab, dtype, 21)
         z[0, 1:] = -math.inf                                 # one token left
         z[1] = -math.inf                                     # none
         z[3] = math.nan
-        z[4, 4500] = math.nan
+        z[4, last] = math.nan
         z[6, 17] = math.inf
         z[9, 10:] = low                                      # ten tokens that matter; the others are candidates
         z[10] = low                                          # all equal
         z[11] = -math.inf
         z[12:15, 3:] = -math.inf                             # nine candidates of a request
-        z[15, :4096], z[15, 4097:] = -math.inf, -math.inf    # one token, behind the first slice
+        z[15, :last], z[15, last + 1:] = -math.inf, -math.inf          # one token, far behind
         z[18:21] = -math.inf                                 # a request that has no candidate
         score[21], score[22], score[24] = -math.inf, math.nan, math.inf
         score[25] = -3e38
@@ -102,7 +107,7 @@ def test_values_that_are_no_numbers():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("vocab,keep", [(40, 8), (700, 128), (20000, 5), (20000, 128)])
+@pytest.mark.parametrize("vocab,keep", [(40, 8), (700, 20), (700, 128), (4000, 32), (4000, 1), (20000, 5), (20000, 128)])
 def test_equal_candidates_go_by_their_place(dtype, vocab, keep):
     """logits of few values, a row of one value, zeros of both signs, beams that are alike"""
     print(f"[case] ties {dtype} {vocab} {keep}", flush=True)
