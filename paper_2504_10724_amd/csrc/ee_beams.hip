@@ -82,12 +82,12 @@ __device__ __forceinline__ float of_order(uint32_t u) { return __uint_as_float(u
 // values still reach it.  No smaller than the lowest finite number.
 template <int N> __device__ __forceinline__ float reached_by(const uint32_t (&v)[N], int keep) {
     uint32_t t = 0;
-#pragma unroll 4
+#pragma unroll 1
     for (int bit = 31; bit >= 0; --bit) {
         const uint32_t u = t | (1u << bit);
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) n += __popcll(__ballot(v[i] >= u));
+        for (int i = 0; i < N; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(v[i] >= u));
         if (n >= keep) t = u;
         if (n == keep) break;
     }
@@ -104,22 +104,24 @@ __device__ __forceinline__ float reached_by_quads(const uint32_t* tops, int lane
     return reached_by(v, keep);
 }
 
-// Over the lanes of a wave, in the lanes of a row of 16 first.
-template <int CTRL> __device__ __forceinline__ float lane_of(float from, float none) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(from), CTRL, 0xf, 0xf, false));
+// Over the lanes of a wave: in rows of 16 lanes first (from the lane before, then two, four and eight before), then from row to row; the last lane
+// has it all.  Lanes without a source get 0.
+template <int CTRL> __device__ __forceinline__ uint32_t lane_of(uint32_t from) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)from, CTRL, 0xf, 0xf, true);
 }
-__device__ __forceinline__ float wave_max(float v) {
-    v = fmaxf(v, lane_of<0x111>(v, -INFINITY));              // the lane before, then two, four and eight before
-    v = fmaxf(v, lane_of<0x112>(v, -INFINITY));
-    v = fmaxf(v, lane_of<0x114>(v, -INFINITY));
-    v = fmaxf(v, lane_of<0x118>(v, -INFINITY));
-    v = fmaxf(v, lane_of<0x142>(v, -INFINITY));              // the last lane of the row before, then of the half before
-    v = fmaxf(v, lane_of<0x143>(v, -INFINITY));
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+// the largest float: of its order as unsigned numbers an instruction a step
+__device__ __forceinline__ float wave_max(float f) {
+    uint32_t v = order_of(f);
+    v = max(v, lane_of<0x111>(v));
+    v = max(v, lane_of<0x112>(v));
+    v = max(v, lane_of<0x114>(v));
+    v = max(v, lane_of<0x118>(v));
+    v = max(v, lane_of<0x142>(v));
+    v = max(v, lane_of<0x143>(v));
+    return of_order((uint32_t)__builtin_amdgcn_readlane((int)v, 63));
 }
 template <int CTRL> __device__ __forceinline__ double lane_of(double from) {
-    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(from), CTRL, 0xf, 0xf, false),
-                            __builtin_amdgcn_update_dpp(0, __double2loint(from), CTRL, 0xf, 0xf, false));
+    return __hiloint2double((int)lane_of<CTRL>((uint32_t)__double2hiint(from)), (int)lane_of<CTRL>((uint32_t)__double2loint(from)));
 }
 __device__ __forceinline__ double wave_sum(double v) {
     v += lane_of<0x111>(v);
@@ -246,7 +248,7 @@ k_beam_slices(const T* __restrict__ logits, int64_t stride, const uint8_t* __res
         const float b = reached_by_quads(tops, lane, keep);
         if (lane == 0) reach = b;
     }
-    const bool plain = __all(low >= -700.f && top <= 600.f);
+    const bool plain = __builtin_amdgcn_ballot_w64(low < -700.f || top > 600.f) == 0;
     const float most = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
     const double beside = top == -INFINITY ? 0.0 : (double)top;
     double sum = 0.0;
@@ -274,13 +276,13 @@ k_beam_slices(const T* __restrict__ logits, int64_t stride, const uint8_t* __res
     if (wt >= bound) {                                       // the elements that reach the bound: a place for each by the waves' and the lanes' counts
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < E; ++i) n += __popcll(__ballot(x[i] >= bound));
+        for (int i = 0; i < E; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(x[i] >= bound));
         int c = 0;
         if (lane == 0) c = atomicAdd(&n_found, n);
         c = __builtin_amdgcn_readfirstlane(c);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            const uint64_t who = __ballot(x[i] >= bound);
+            const uint64_t who = __builtin_amdgcn_ballot_w64(x[i] >= bound);
             if (who == 0) continue;
             const int o = c + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
             if (x[i] >= bound && o < CANDIDATES) { value[o] = x[i] + 0.f; place[o] = at(i); }
