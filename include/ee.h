@@ -658,6 +658,7 @@ int ee_pages_grow(ee_pages* g, const ee_page_table* t, const int32_t* dev_new, i
  * before any is written.  So it forks, reorders, cuts and frees.  group > 0: rows group * j .. group * j + group - 1 have their
  * parents, numbered 0 .. group - 1, among each other; group 0: parents are rows of the whole table.
  * states: further rows that go along in place (tokens so far, hidden states); those of a parent of -1 stay as they are.
+ * Parents, lengths to keep, tables and states lie apart from each other.
  * Errors: EE_ERR_SHAPE if to's width is below from's, n_seqs is no multiple of group, with group > 0 the tables' n_seqs
  * differ, or more than EE_PAGES_MAX_GROUP rows are forked in place among each other; EE_ERR_INVALID_ARG (states without a fork in place; tables that
  * share only part of their memory). */

@@ -66,17 +66,17 @@ template <int THREADS, int N> __device__ __forceinline__ void sum_before(uint32_
 //   all or nothing: the sums are known before anything is written
 //   the free pages' numbers go to LDS some words at a time; the threads then take a needed page each
 // Copies are listed for the launch behind this one.  A thread's need is cut above the most pages that a state has, so that sums stay in 32 bits.
-constexpr int GROW = 1024, GROW_WORDS = 256;                 // threads; words of free bits at a time
+constexpr int GROW = 1024;                                   // threads, and words of free bits at a time
 template <int PER>
 __global__ void __launch_bounds__(GROW)
 k_pages_grow(PagesView v, TableView t, const int32_t* __restrict__ more, int32_t* status) {
     constexpr int ROWS = PER * GROW, SLOTS = 2 * ROWS;
     // the writers' table first, then what the rows take
     struct Meet { int32_t page[SLOTS], writers[SLOTS], first[SLOTS]; };
-    struct Take { int32_t first[ROWS], place[ROWS]; uint16_t page_of[GROW_WORDS * 32]; };    // a row's first needed page; its first new place, sign bit: a copy comes first
+    struct Take { int32_t first[ROWS], place[ROWS]; uint16_t page_of[GROW * 32]; };    // a row's first needed page; its first new place, sign bit: a copy comes first
     __shared__ union { Meet meet; Take take; } lds;
     __shared__ uint32_t sums[3 * GROW / 64];
-    __shared__ int n_copies;
+    __shared__ int n_copies, first_word;                     // the first word that has a free page
     const int tid = threadIdx.x, ps = v.page_size, words = (v.n_pages + 31) / 32;
     int len[PER], add[PER], held[PER], refs[PER];
 #pragma unroll
@@ -85,9 +85,18 @@ k_pages_grow(PagesView v, TableView t, const int32_t* __restrict__ more, int32_t
         len[i] = s < t.n ? t.len[s] : 0;
         add[i] = s < t.n ? (more ? more[s] : 1) : 0;
     }
-    uint32_t bits = tid < GROW_WORDS && tid < words ? v.free_bits[tid] : 0u, n_free = 0;
-    for (int w = tid; w < words; w += GROW) n_free += __popc(v.free_bits[w]);
-    if (tid == 0) n_copies = 0;
+    uint32_t bits = tid < words ? v.free_bits[tid] : 0u, n_free = 0;
+    int first_here = 0x7fffffff;                             // of this wave's words
+    for (int w0 = 0; w0 < words; w0 += GROW) {
+        const uint32_t word = w0 == 0 ? bits : w0 + tid < words ? v.free_bits[w0 + tid] : 0u;
+        const uint64_t any = __builtin_amdgcn_ballot_w64(word != 0);
+        if (any != 0) first_here = min(first_here, w0 + (tid & ~63) + __builtin_ctzll(any));
+        n_free += __popc(word);
+    }
+    if (tid == 0) {
+        n_copies = 0;
+        first_word = 0x7fffffff;
+    }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int s = tid * PER + i;
@@ -120,7 +129,9 @@ k_pages_grow(PagesView v, TableView t, const int32_t* __restrict__ more, int32_t
     bool copy[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) copy[i] = false;
-    if (__syncthreads_or(shared)) {
+    const bool meet = __syncthreads_or(shared);
+    if ((tid & 63) == 0 && first_here != 0x7fffffff) atomicMin(&first_word, first_here);
+    if (meet) {
         int slot[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i)
@@ -163,10 +174,10 @@ k_pages_grow(PagesView v, TableView t, const int32_t* __restrict__ more, int32_t
         before[0] += need[i];
     }
     int taken = 0;
-    for (int w0 = 0; w0 < words && taken < total; w0 += GROW_WORDS) {
+    for (int w0 = first_word / GROW * GROW; w0 < words && taken < total; w0 += GROW) {
         const int w = w0 + tid;
         if (w0 > 0) {                                        // the first words are in the sums above
-            bits = tid < GROW_WORDS && w < words ? v.free_bits[w] : 0u;
+            bits = w < words ? v.free_bits[w] : 0u;
             uint32_t one[1] = {(uint32_t)__popc(bits)}, here[1];
             sum_before<GROW>(one, here, sums);
             before[2] = one[0];

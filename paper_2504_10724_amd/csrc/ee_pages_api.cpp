@@ -115,6 +115,9 @@ int ee_pages_fork(ee_pages* g, const ee_page_table* to, const ee_page_table* fro
         return ee_fail(EE_ERR_SHAPE, "ee_pages_fork: more than EE_PAGES_MAX_GROUP rows in place");
     if (n_states > 0 && !in_place) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: states go along in place only");
     if (n_states > 0 && !states) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: null pointer");
+    // read by some workgroups when others have written
+    auto written = [&](const void* p) { return p && (p == to->dev_kv_len || p == to->dev_pages); };
+    if (written(dev_parent) || written(dev_keep)) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: parents or lengths are the table's own memory");
     ForkView f;
     f.to = make_table(to);
     f.from = make_table(from);
@@ -129,6 +132,8 @@ int ee_pages_fork(ee_pages* g, const ee_page_table* to, const ee_page_table* fro
         if (r.bytes < 0) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: negative count");
         if (r.bytes == 0) continue;
         if (!r.dev) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: null pointer");
+        if (written(r.dev) || r.dev == dev_parent || r.dev == dev_keep)
+            return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: a state is the table's, the parents' or the lengths' memory");
         for (int j = 0; j < f.n_states; ++j)
             if (f.states[j].p == r.dev) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: a state is given twice");
         if (to->n_seqs > 1 && r.stride < r.bytes) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: rows of a state share their memory");

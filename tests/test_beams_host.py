@@ -102,7 +102,7 @@ def test_bookkeeping_calls():
     assert lib.ee_pages_grow(None, T(t), None, None, None) == BAD and lib.ee_pages_grow(g, None, None, None, None) == BAD
     assert lib.ee_pages_grow(g, T(wide), None, None, None) == CAPACITY and lib.ee_pages_grow(g, T(none), None, None, None) == ee.EE_OK
 
-    def fork(to=t, source=None, parent=DUMMY, keep=None, group=0, states=(), n=None):
+    def fork(to=t, source=None, parent=C.c_void_p(32768), keep=None, group=0, states=(), n=None):
         a = (ee.ee_rows * 9)(*states)
         return lib.ee_pages_fork(g, T(to), None if source is None else T(source), parent, keep, group, a if states else None,
                                  len(states) if n is None else n, None, None)
@@ -115,10 +115,14 @@ def test_bookkeeping_calls():
     assert fork(source=_table(pages_per_seq=4, **other)) == SHAPE                  # rows that do not fit
     assert fork(source=_table(dev_pages=16384)) == BAD and fork(source=_table(dev_kv_len=16384)) == BAD and fork(source=_table(n_seqs=3)) == BAD
     assert fork(to=_table(n_seqs=4097)) == SHAPE and fork(to=_table(n_seqs=8194), group=4097) == SHAPE
-    rows = ee.ee_rows(4096, 64, 64)
+    rows = ee.ee_rows(65536, 64, 64)
     assert fork(states=[rows] * 9) == SHAPE and fork(source=_table(**other), states=[rows]) == BAD
-    assert fork(states=[ee.ee_rows(4096, 63, 64)]) == BAD and fork(states=[ee.ee_rows(4096, 64, -1)]) == BAD
+    assert fork(states=[ee.ee_rows(65536, 63, 64)]) == BAD and fork(states=[ee.ee_rows(65536, 64, -1)]) == BAD
     assert fork(states=[ee.ee_rows(None, 64, 64)]) == BAD and fork(states=[rows, rows]) == BAD
+    own = [C.c_void_p(t.dev_pages), C.c_void_p(t.dev_kv_len)]
+    assert all(fork(parent=a) == BAD and fork(parent=C.c_void_p(24576), keep=a) == BAD for a in own)            # of the table that is written
+    for a in (t.dev_pages, t.dev_kv_len, 24576, 28672):
+        assert fork(parent=C.c_void_p(24576), keep=C.c_void_p(28672), states=[ee.ee_rows(a, 4, 4)]) == BAD
     assert lib.ee_pages_compact(None, T(t), 1, None) == BAD and lib.ee_pages_compact(g, None, 1, None) == BAD
     assert lib.ee_pages_compact(g, T(t), -1, None) == BAD and lib.ee_pages_compact(g, T(t), 9, None) == SHAPE
     assert lib.ee_pages_compact(g, (ee.ee_page_table * 2)(t, t), 2, None) == BAD

@@ -262,6 +262,26 @@ def test_a_row_that_needs_thousands_of_pages():
     c.check("compacted")
 
 
+def test_free_pages_far_behind():
+    """a pool of more words of free bits than are looked at at a time, full but for its end and some pages on the way"""
+    print("[case] almost full", flush=True)
+    n_pages = 150000
+    c = Pair(n_pages, 32, layers=1, hkv=1, hd=4, values=False)
+    t = c.table(4, n_pages)
+    c.grow(t, [32 * 70000, 32 * 3, 32 * (n_pages - 70000 - 20), 0])
+    assert c.check("full") == 17
+    c.grow(t, [0, 0, 0, 32 * 17])
+    assert c.check("none left") == 0
+    c.fork(t, [0, -1, 2, 3])
+    c.grow(t, [1, 0, 0, 64])
+    assert c.check("three in the middle") == 0
+    c.fork(t, [0, 1, 2, 3], keep=[32 * 40000, 0, 2 ** 30, 32 * 5])
+    c.grow(t, [5, 32 * 100, 0, 7])
+    c.check("again")
+    c.compact()
+    c.check("compacted")
+
+
 @pytest.mark.parametrize("dtype,hkv,hd,page", [("f32", 1, 4, 32), ("bf16", 3, 96, 96), ("f32", 2, 252, 64), ("bf16", 5, 128, 256)])
 def test_copies_between_pools(dtype, hkv, hd, page):
     """pages out of order, into a pool of another size; pages outside either pool are left out"""
@@ -348,6 +368,8 @@ def test_refusals():
            lambda: c.pages.fork(t, parent, source=other, rows=[x]), lambda: c.pages.fork(t, parent, rows=[x.cpu()]), lambda: c.pages.fork(t, parent, rows=[x[:3]]),
            lambda: c.pages.fork(t, parent, rows=[x.t().contiguous().t()]), lambda: c.pages.fork(t, parent, rows=[x[:1].expand(4, 8)]),
            lambda: c.pages.fork(t, parent, rows=[x, x]), lambda: c.pages.fork(t, parent, rows=[torch.zeros(4, k + 1, device="cuda") for k in range(9)]),
+           lambda: c.pages.fork(t, t.kv_len), lambda: c.pages.fork(t, parent, keep=t.kv_len), lambda: c.pages.fork(t, parent, rows=[parent]),
+           lambda: c.pages.fork(t, parent, rows=[t.kv_len]), lambda: c.pages.fork(t, parent, rows=[t.pages]),
            lambda: c.pages.fork(t, parent, rows=[x.clone().requires_grad_()]), lambda: c.pages.compact(t, far), lambda: c.pages.compact(t, t),
            lambda: c.pages.compact(*(P.PageTable(c.kv, 1, 1) for _ in range(9))), lambda: P.Pages(c.kv, 0), lambda: P.Pages(c.kv, 4097),
            lambda: P.Pages(c.kv, 2 ** 32 + 1), lambda: P.PageTable(c.kv, -1, 3), lambda: P.PageTable(c.kv, 2 ** 32, 3),
