@@ -645,7 +645,7 @@ int ee_pages_destroy(ee_pages* g);
 /* Every page is free.  Enqueue only. */
 int ee_pages_reset(ee_pages* g, void* stream);
 
-/* Row i gains dev_new[i] positions (NULL: one each; 0 is allowed): the table gets the pages that it lacks, the length grows.  A row that will write
+/* Row i gains dev_new[i] positions (NULL: one each; 0 is allowed, dev_kv_len too): the table gets the pages that it lacks, the length grows.  A row that will write
  * into a page that other rows hold gets a page of its own instead, with the groups of 32 positions copied that hold any of the row's, in
  * every layer; where all rows that hold the page are written by this call, the first of them keeps it.  Pages are handed out by
  * row, then by place in the row, the lowest free one first.  All or nothing: with too few free pages status bit 4 is set.

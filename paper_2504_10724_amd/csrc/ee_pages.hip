@@ -61,7 +61,8 @@ template <int THREADS, int N> __device__ __forceinline__ void sum_before(uint32_
 // Row s needs pages(len + new) - pages(len) pages, and one more where its last page is shared and it does not keep it; a prefix sum
 // over the rows gives each its places among the free pages in rising order, which the free bits give, 32 a word, by another prefix sum.  One
 // workgroup, since every row's pages hang on the rows before it; a thread has PER rows.  It is bound by its trips to memory one behind the other (rows, their last
-// pages, these pages' counts, the results), about 1.2 us each with the kernel's start and end, so nothing else leaves the compute unit:
+// pages, these pages' counts, the results), about 1.2 us each with the kernel's start and end, so nothing else leaves the compute unit (256 rows of 16
+// pages, 1491 in the pool: 5.6 us; with marks, atomics and fences in device memory 16.0; 8 rows 4.2):
 //   shared pages: writers meet in a table in LDS, where a page's writers are counted and the first is found
 //   all or nothing: the sums are known before anything is written
 //   the free pages' numbers go to LDS some words at a time; the threads then take a needed page each
@@ -69,7 +70,7 @@ template <int THREADS, int N> __device__ __forceinline__ void sum_before(uint32_
 constexpr int GROW = 1024;                                   // threads, and words of free bits at a time
 template <int PER>
 __global__ void __launch_bounds__(GROW)
-k_pages_grow(PagesView v, TableView t, const int32_t* __restrict__ more, int32_t* status) {
+k_pages_grow(PagesView v, TableView t, const int32_t* more, int32_t* status) {
     constexpr int ROWS = PER * GROW, SLOTS = 2 * ROWS;
     // the writers' table first, then what the rows take
     struct Meet { int32_t page[SLOTS], writers[SLOTS], first[SLOTS]; };
@@ -254,7 +255,8 @@ template <bool ONCE> __device__ __forceinline__ void copy_run(const char* __rest
     for (; o < n; o += 256) put<ONCE>(get<ONCE>(a + o), b + o);
 }
 
-// the listed pages' first groups of 32 positions, in all layers: an item is one group of one block
+// the listed pages' first groups of 32 positions, in all layers: an item is one group of one block.  256 rows' copies of 64 positions
+// and less, 8 layers, 8 heads of 128: 131 MB written, as many read, 54.7 us, 4.8 TB/s.  Through the caches: 85 MB in all 14.8 us, past them 18.7.
 __global__ void __launch_bounds__(256) k_pages_copy_groups(PagesView v, PoolView pool) {
     const int per_page = pool.blocks * pool.subs;
     const int64_t per = (int64_t)per_page * pool.n_layers, n = *v.n_moves * per;
@@ -332,7 +334,9 @@ int launch_pages_copy(const PoolView& from, const PoolView& to, const int32_t* s
 // A workgroup takes a tile: some columns of the rows that are forked among each other (in place: all of them, through LDS, so that every
 // entry is read before one is written) or of 16 rows (from another table).  Tile 0 has the lengths, then come the table's columns, then those
 // of the states.  Entries that stay cost nothing but their reads: beams of one request share most of theirs.  Bound by trips to memory one behind the
-// other: parents and entries are asked for together, then counts go up and down, then pages that are free are marked.
+// other: parents and entries are asked for together, then counts go up and down, then pages that are free are marked.  64 groups of four rows of
+// 16 entries with 32 KB of states each (16 MB moved): 8.3 us (in larger tiles, entries asked for behind parents, 19.8); 96 rows of 24 among each
+// other, a third of them given back, 6.5 (19.1); 16 rows of 469 from another table 4.2.
 //
 // Counts: what a row takes is counted before what it gives up is counted down, each by atomics; and a page that a row takes is named by that row's
 // parent until the tile that takes it has counted it.  So a count falls to 0 once, in the thread that frees the page, whatever the order.
@@ -585,7 +589,8 @@ int launch_pages_fork(const PagesView& v, const ForkView& f, hipStream_t s) {
 
 // ------------------------------------------------------------------ compact
 // With U pages in use, the j-th page in use from U on goes to the j-th free page below U: two ranks, by prefix sums over the free bits in one
-// workgroup.  Pages read and pages written are apart, so the copies behind need no order.
+// workgroup.  Pages read and pages written are apart, so the copies behind need no order.  1430 pages: 4.8 us, trips to memory (7.9 with a fence that
+// empties the L2 between lists and their use).
 constexpr int PLAN = 1024;
 __global__ void __launch_bounds__(PLAN) k_pages_plan(PagesView v) {
     __shared__ uint32_t sums[2 * PLAN / 64];

@@ -390,3 +390,15 @@ def test_refusals():
         with pytest.raises(ee.EEError):
             call()
     assert not t.kv_len.any() and (t.pages == -1).all()
+
+
+@pytest.mark.parametrize("n", [3, 1500])
+def test_rows_grow_by_their_own_lengths(n):
+    """the lengths are read as new positions and written as lengths in one call"""
+    a = Pair(6 * n, values=False)
+    t = a.table(n, 4)
+    a.grow(t, [1 + i % 40 for i in range(n)])
+    for _ in range(2):                                       # rows that would pass the table's end stay
+        a.pages.grow(t[0], t[0].kv_len, status=a.status)
+        a.book.grow(t[1], list(t[1].len))
+        a.check()
