@@ -204,3 +204,17 @@ def test_refusals():
             call()
     with torch.no_grad():
         B.select(z.clone().requires_grad_(), score, 4, workspace=ws)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("groups,beams,vocab", [(600, 2, 3), (1025, 1, 1), (300, 4, 7), (270, 4, 8), (70, 16, 50)])
+def test_many_rows_of_few_tokens(groups, beams, vocab, dtype):
+    z, score = _inputs(groups, beams, vocab, dtype, vocab)
+    _check(B.select(z.cuda(), score.cuda(), beams), R.choose(z, score, beams, beams))
+
+
+def test_rows_that_are_one():
+    """a stride of 0: all beams have the same logits, and their candidates differ by the scores alone"""
+    z, score = _inputs(1, 1, 5000, "f32", 11)
+    score = torch.tensor([-1.0, -0.5, -0.5, -3.0])
+    _check(B.select(z.cuda().expand(4, 5000), score.cuda(), 4, keep=20), R.choose(z.expand(4, 5000), score, 4, 20))
