@@ -182,7 +182,7 @@ __device__ __forceinline__ void shrink(float* value, int* place, int n, int keep
 // half (with an exponential in fp32 59 us), the rest a wave's work over its 16 elements a lane; they fill 69 % of the cycles.  32 elements a lane
 // took 87 us, slices streamed tile by tile under a bound that rises 86 a wave's and 177 a workgroup's.  256 rows of 32000 bf16: 12.4; 8 of 2048 fp32: 4.1.
 template <class T, int E, bool SHORT>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 8)
 k_beam_slices(const T* __restrict__ logits, int64_t stride, const uint8_t* __restrict__ done, int vocab, int n_slices, int keep, BeamParts parts) {
     constexpr int VEC = 16 / (int)sizeof(T), RUNS = E / VEC;
     __shared__ __align__(16) uint32_t tops[256];
@@ -277,19 +277,24 @@ k_beam_slices(const T* __restrict__ logits, int64_t stride, const uint8_t* __res
     __syncthreads();
     float bound = reach;
     if (wt >= bound) {                                       // the elements that reach the bound: a place for each by the waves' and the lanes' counts
+        uint64_t who[E];
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < E; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(x[i] >= bound));
+        for (int i = 0; i < E; ++i) {
+            who[i] = __builtin_amdgcn_ballot_w64(x[i] >= bound);
+            n += __popcll(who[i]);
+        }
         int c = 0;
         if (lane == 0) c = atomicAdd(&n_found, n);
         c = __builtin_amdgcn_readfirstlane(c);
+        if (c + n <= CANDIDATES) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const uint64_t who = __builtin_amdgcn_ballot_w64(x[i] >= bound);
-            if (who == 0) continue;
-            const int o = c + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
-            if (x[i] >= bound && o < CANDIDATES) { value[o] = x[i] + 0.f; place[o] = at(i); }
-            c += __popcll(who);
+            for (int i = 0; i < E; ++i) {
+                if (who[i] == 0) continue;
+                const int o = __builtin_amdgcn_mbcnt_hi((uint32_t)(who[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who[i], c));
+                if (__builtin_amdgcn_inverse_ballot_w64(who[i])) { value[o] = x[i]; place[o] = at(i); }
+                c += __popcll(who[i]);
+            }
         }
     }
     __syncthreads();
