@@ -178,9 +178,10 @@ __device__ __forceinline__ void shrink(float* value, int* place, int n, int keep
 
 // Sums are taken of exp(z) itself where a wave's logits lie in -700 .. 600 (fp64 holds that), so that they wait for no maximum and NaN need
 // no look; else of exp(z - the lane's largest).  Candidates: what reaches a bound that `keep` of the threads' largest reach.
-// 512 rows of 131071 fp32 logits: 82 to 85 us, 3.2 TB/s (a pure read of them 43).  Bound by vector instructions: 30 an element, of which the sum in fp64 is
-// half (with an exponential in fp32 59 us), the rest a wave's work over its 16 elements a lane; they fill 69 % of the cycles.  32 elements a lane
-// took 87 us, slices streamed tile by tile under a bound that rises 86 a wave's and 177 a workgroup's.  256 rows of 32000 bf16: 12.4; 8 of 2048 fp32: 4.1.
+// 512 rows of 131071 fp32 logits: 77 to 79 us, 3.4 TB/s (a pure read of them 43).  Bound by vector instructions: 27 an element, of which the sum in fp64 is
+// half (with an exponential in fp32 59 us), the rest a wave's work over its 16 elements a lane; they fill 68 % of the cycles.  Of the tries when it took
+// 83, 32 elements a lane took 87, slices streamed tile by tile under a bound that rises 86 a wave's and 177 a workgroup's.  Registers for eight
+// waves a SIMD: 84.3 us a call for 87.0.  256 rows of 32000 bf16: 12.3; 8 of 2048 fp32: 4.1.
 template <class T, int E, bool SHORT>
 __global__ void __launch_bounds__(256, 8)
 k_beam_slices(const T* __restrict__ logits, int64_t stride, const uint8_t* __restrict__ done, int vocab, int n_slices, int keep, BeamParts parts) {
