@@ -32,8 +32,17 @@ def _refuse(what):
     raise ee.EEError(ee.EE_ERR_INVALID_ARG, what)
 
 
-# handle of the current stream of a device, by its number (a fifth of the time the way through the current device takes)
-_stream = _raw_stream or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_stream_of = _raw_stream or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _stream(device):
+    """Handle of the current stream of a device, by its number (a fifth of the time the way through the current device takes).  A default
+    stream's handle is 0 on every device and means the current one's: work for another device's memory would go there."""
+    handle = _stream_of(device)
+    if not handle and _current_device() != device:
+        _refuse(f"tensors are on device {device}, whose stream is its default one, but device {_current_device()} is current: use torch.cuda.device({device})")
+    return handle
 
 
 _MOST = 2 ** 31 - 1

@@ -135,3 +135,15 @@ def test_bookkeeping_calls():
     assert lib.ee_pages_copy(p, p, None, DUMMY, 1, None, None) == BAD and lib.ee_pages_copy(p, p, None, None, 0, None, None) == ee.EE_OK
     lib.ee_pages_destroy(g)
     lib.ee_paged_destroy(p)
+
+
+def test_default_streams_are_those_of_the_current_device(monkeypatch):
+    """their handle is 0 on every device; a stream that was made knows its device"""
+    from paper_2504_10724_amd import beams, paged
+    handles = {0: 0, 1: 0, 2: 0x5000}
+    monkeypatch.setattr(paged, "_stream_of", handles.__getitem__)
+    monkeypatch.setattr(paged, "_current_device", lambda: 0)
+    assert beams._stream is paged._stream
+    assert paged._stream(0) == 0 and paged._stream(2) == 0x5000
+    with pytest.raises(ee.EEError, match="device 0 is current"):
+        paged._stream(1)
