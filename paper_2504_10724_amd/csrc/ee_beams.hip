@@ -346,10 +346,13 @@ k_beam_slices(const T* __restrict__ logits, int64_t stride, const uint8_t* __res
 }
 
 // ------------------------------------------------------------------ second launch
-// A candidate of the request: its key, its beam, its token.  Better: a larger key, then the smaller beam * vocab + token.
-struct Candidate { double key; int beam, token; };
+// A candidate of the request: its key, its beam, its token, its logit.  Better: a larger key, then the smaller beam, then the larger logit, then the
+// smaller token.  A key may swallow its logit (a score of -3e38, logits of 1e-30): in a beam, where keys never fall as logits rise, this is the
+// order of the logits, by which the slices made their lists, so that the choice does not hang on how wide a slice is.
+struct Candidate { double key; int beam, token; float value; };
 __device__ __forceinline__ bool better(const Candidate& a, const Candidate& b) {
-    return a.key > b.key || (a.key == b.key && (a.beam < b.beam || (a.beam == b.beam && a.token < b.token)));
+    return a.key > b.key ||
+           (a.key == b.key && (a.beam < b.beam || (a.beam == b.beam && (a.value > b.value || (a.value == b.value && a.token < b.token)))));
 }
 
 // A number that `keep` of the slices' largest reach leaves out most lists at once; where there are fewer slices than that, the threads' largest of
@@ -371,7 +374,10 @@ k_beam_join(BeamParts parts, const float* score, const uint8_t* done, int beams,
     __shared__ float most[BEAM_MAX_BEAMS];                   // maximum, apart: a mask's lowest value beside it would swallow the logarithm
     __shared__ uint8_t ended[BEAM_MAX_BEAMS];
     __shared__ __align__(16) uint32_t tops[256];
-    __shared__ Candidate found[CANDIDATES], best[JOIN / 64];
+    __shared__ __align__(16) double found_key[CANDIDATES];   // keys apart: the sort reads little else
+    __shared__ int found_beam[CANDIDATES], found_token[CANDIDATES];
+    __shared__ float found_value[CANDIDATES];
+    __shared__ Candidate best[JOIN / 64];
     __shared__ int left[FEW ? 1 : CANDIDATES], n_left, n_found, own_place[FEW ? JOIN * OWN : 1];
     __shared__ float own_value[FEW ? JOIN * OWN : 1];
     const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lists = beams * n_slices, room = parts.room;
@@ -426,12 +432,13 @@ k_beam_join(BeamParts parts, const float* score, const uint8_t* done, int beams,
     auto key_of = [&](int b, float value) { return base[b] + ((double)value - (double)most[b]); };
     // what place i of a list holds; of a beam that has ended, its one candidate at place 0 of its first list
     auto candidate = [&](int list, int b, bool is_first, bool there, float value, int place) {
-        Candidate c{-INFINITY, b, -1};
+        Candidate c{-INFINITY, b, -1, 0.f};
         if (ended[b]) {
             if (is_first && list == b * n_slices && base[b] == base[b]) { c.key = base[b]; c.token = end_token; }
         } else if (there && base[b] == base[b]) {
             c.key = key_of(b, value);
             c.token = place;
+            c.value = value;
         }
         return c;
     };
@@ -470,7 +477,12 @@ k_beam_join(BeamParts parts, const float* score, const uint8_t* done, int beams,
     auto collect = [&](const Candidate& c) {
         if (c.token < 0 || below(c.key) < bound) return;
         const int at = atomicAdd(&n_found, 1);
-        if (at < CANDIDATES) found[at] = c;
+        if (at < CANDIDATES) {
+            found_key[at] = c.key;
+            found_beam[at] = c.beam;
+            found_token[at] = c.token;
+            found_value[at] = c.value;
+        }
     };
     if constexpr (FEW) {
 #pragma unroll 1
@@ -495,26 +507,33 @@ k_beam_join(BeamParts parts, const float* score, const uint8_t* done, int beams,
     };
     const int m = n_found;
     if (n_left <= CANDIDATES && m <= CANDIDATES) {
+        auto found = [&](int c) { return Candidate{found_key[c], found_beam[c], found_token[c], found_value[c]}; };
         for (int c = tid; c < m; c += JOIN) {
-            const Candidate mine = found[c];
-            int rank = 0;
-            for (int o = 0; o < m; ++o) rank += better(found[o], mine);
+            const Candidate mine = found(c);
+            int rank = 0, same = 0;
+            for (int o = 0; o < m; ++o) {
+                const double key = found_key[o];
+                rank += key > mine.key;
+                same += key == mine.key;
+            }
+            if (same > 1)                                    // itself and others: few, or a beam whose score swallows its logits
+                for (int o = 0; o < m; ++o) rank += found_key[o] == mine.key && better(found(o), mine);
             if (rank < keep) put(rank, mine, true);
         }
         for (int c = m + tid; c < keep; c += JOIN) put(c, Candidate{}, false);
         return;
     }
     // many equal ones: the next best behind the last, `keep` times
-    Candidate last{INFINITY, -1, -1};
+    Candidate last{INFINITY, -1, -1, 0.f};
     for (int k = 0; k < keep; ++k) {
-        Candidate v{-INFINITY, 0x7fffffff, -1};
+        Candidate v{-INFINITY, 0x7fffffff, -1, 0.f};
         for (int64_t j = tid; j < (int64_t)lists * room; j += JOIN) {
             const Candidate c = take((int)(j / room), (int)(j % room));
             if (c.token >= 0 && better(last, c) && better(c, v)) v = c;
         }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
-            const Candidate u{__shfl_xor(v.key, o, 64), __shfl_xor(v.beam, o, 64), __shfl_xor(v.token, o, 64)};
+            const Candidate u{__shfl_xor(v.key, o, 64), __shfl_xor(v.beam, o, 64), __shfl_xor(v.token, o, 64), __shfl_xor(v.value, o, 64)};
             if (better(u, v)) v = u;
         }
         __syncthreads();

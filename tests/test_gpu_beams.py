@@ -218,3 +218,52 @@ def test_rows_that_are_one():
     z, score = _inputs(1, 1, 5000, "f32", 11)
     score = torch.tensor([-1.0, -0.5, -0.5, -3.0])
     _check(B.select(z.cuda().expand(4, 5000), score.cuda(), 4, keep=20), R.choose(z.expand(4, 5000), score, 4, 20))
+
+
+def _choose_by_logits(logits, score, n_beams, keep, done=None, end=-1):
+    """(parents, tokens): keys in 64 bits, and where they are equal the smaller beam, in a beam the larger logit, then the smaller token"""
+    out = [], []
+    for g in range(len(logits) // n_beams):
+        found = []
+        for b in range(n_beams):
+            s, z = float(score[g * n_beams + b]), logits[g * n_beams + b].double()
+            if not math.isfinite(s):
+                continue
+            if done is not None and done[g * n_beams + b]:
+                found.append((-s, b, 0.0, end))
+                continue
+            top, log = float(z.max()), math.log(float(torch.exp(z - z.max()).sum()))
+            found += [(-(s - log + (v - top)), b, -v, t) for t, v in enumerate(z.tolist())]
+        found = sorted(found)[:keep]
+        out[0].append([f[1] for f in found] + [-1] * (keep - len(found)))
+        out[1].append([f[3] for f in found] + [-1] * (keep - len(found)))
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,keep", [(8192, 4), (8192, 40), (8192, 128), (300, 5), (300, 128), (4097, 9)])
+def test_a_beam_whose_score_swallows_its_logits(vocab, keep, dtype):
+    """its candidates' keys are all equal in 64 bits, and it goes on with its largest logits, alone as in a batch, whose slices are wider"""
+    print(f"[case] swallowed {dtype} {vocab} {keep}", flush=True)
+    z, _ = _inputs(1, 4, vocab, dtype, vocab + keep)
+    score = torch.tensor([-math.inf, -3e38, math.nan, -math.inf])
+    want = torch.sort(z[1].double(), descending=True, stable=True).indices[:keep].tolist()
+    for groups in (1, 1200):
+        got = B.select(z.repeat(groups, 1).cuda(), score.repeat(groups).cuda(), 4, keep=keep)
+        at = torch.tensor([0, groups // 2, groups - 1], device="cuda")
+        assert got.token[at].tolist() == [want] * 3 and got.parent[at].tolist() == [[1] * keep] * 3
+        assert (got.score == score[1].cuda()).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,keep", [(20, 50), (700, 128), (5000, 20), (20000, 128)])
+def test_logits_that_differ_by_less_than_keys_can(vocab, keep, dtype):
+    """of 1e-30 and less, zeros of both signs among them: every sum is the vocabulary's size, two beams tie, one is ahead, one has ended"""
+    print(f"[case] tiny logits {dtype} {vocab} {keep}", flush=True)
+    z = (torch.randn(8, vocab, generator=_gen(vocab)) * 1e-30).to(DT[dtype])
+    z[:, ::7], z[:, 3::7] = 0.0, -0.0
+    score = torch.tensor([-5.0, -5.0, -4.5, -9.0, -math.inf, -2.0, -2.0, -2.0])
+    done = torch.tensor([0, 0, 0, 1, 0, 0, 0, 0], dtype=torch.uint8)
+    got = B.select(z.cuda(), score.cuda(), 4, keep=keep, done=done.cuda(), end_token=7)
+    parent, token = _choose_by_logits(z, score, 4, keep, done, 7)
+    assert got.parent.tolist() == parent and got.token.tolist() == token
