@@ -682,6 +682,7 @@ int ee_pages_compact(ee_pages* g, const ee_page_table* tables, int n_tables, voi
  * candidates come out in falling order.  The sums and the candidates' values are held in 64 bits; values that are equal there go by the
  * smaller b, then the larger logit, then the smaller v.  A beam that has ended (dev_done) has one candidate: end_token, at its score.
  * A beam whose score or logarithm is not finite (all logits -inf, a NaN or +inf among them) has none, nor has a logit of -inf.
+ * A chosen candidate's score is finite: a value below fp32's lowest number (masks of it taken twice) comes out as that number.
  * Places that no candidate is left for get score -inf, parent -1, token -1.  A search starts with one live beam: scores 0, -inf, .. */
 typedef struct {
     int32_t n_groups;    /* requests                                                    */

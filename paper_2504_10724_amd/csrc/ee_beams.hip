@@ -500,7 +500,7 @@ k_beam_join(BeamParts parts, const float* score, const uint8_t* done, int beams,
     __syncthreads();
     auto put = [&](int k, const Candidate& c, bool any) {
         const int64_t at = (int64_t)g * keep + k;
-        out.dev_score[at] = any ? (float)c.key : -INFINITY;
+        out.dev_score[at] = any ? fmaxf((float)c.key, -3.402823466e38f) : -INFINITY;       // -infinity is a place without a candidate, and no beam
         out.dev_parent[at] = any ? c.beam : -1;
         out.dev_token[at] = any ? c.token : -1;
         if (out.dev_done) out.dev_done[at] = any && (ended[c.beam] || c.token == end_token);

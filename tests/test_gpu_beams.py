@@ -267,3 +267,23 @@ def test_logits_that_differ_by_less_than_keys_can(vocab, keep, dtype):
     got = B.select(z.cuda(), score.cuda(), 4, keep=keep, done=done.cuda(), end_token=7)
     parent, token = _choose_by_logits(z, score, 4, keep, done, 7)
     assert got.parent.tolist() == parent and got.token.tolist() == token
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [9, 3000])
+def test_a_chosen_candidate_has_a_finite_score(vocab, dtype):
+    """a mask of the type's lowest value taken twice: the key is beyond fp32, the score is fp32's lowest finite number, and the beam goes on"""
+    print(f"[case] finite scores {dtype} {vocab}", flush=True)
+    low, lowest = torch.finfo(DT[dtype]).min, -torch.finfo(torch.float32).max
+    z = torch.zeros(4, vocab, dtype=DT[dtype])
+    z[:, 1:] = low                                           # one token is allowed
+    score = torch.tensor([0.0, -math.inf, -math.inf, -math.inf])
+    for aside, want_score in ((1, [0.0, low, low, low]), (3, [low, low, low, lowest]), (0, [lowest] * 4)):
+        got = B.select(z.cuda(), score.cuda(), 4)
+        parent, token = _choose_by_logits(z, score, 4, 4)
+        assert min(parent[0]) >= 0 and got.parent.tolist() == parent and got.token.tolist() == token
+        assert got.score[0].tolist() == want_score
+        score = got.score[0].cpu()
+        score[:aside] = -math.inf                            # the better ones are put aside
+    none = B.select(z[:, :1].cuda(), score.cuda(), 4, keep=6)              # places that no candidate is left for
+    assert none.score[0].tolist() == [lowest] * 4 + [-math.inf] * 2 and none.parent[0].tolist() == [0, 1, 2, 3, -1, -1]
