@@ -4,6 +4,7 @@
 #include "ee_internal.h"
 
 constexpr int BEAM_MAX_BEAMS = 64, BEAM_MAX_KEEP = 128;
+constexpr int BEAM_SLICE = 4096;     // logits of a workgroup; less where that makes no more than 1024 of them
 
 // What a slice of a row's logits leaves: its maximum, sum of exp(z - maximum) in 64 bits, and a list of logits with their places in the row,
 // in any order, the `keep` largest among them.

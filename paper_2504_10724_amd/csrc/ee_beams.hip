@@ -14,7 +14,7 @@
 #include "ee_device.h"
 
 // A workgroup takes a slice of a row, E elements a thread: 16 bytes where that makes no more than four workgroups a CU, else LARGE.
-constexpr int LARGE = 16;
+constexpr int LARGE = BEAM_SLICE / 256;
 template <class T> constexpr int SMALL = 16 / (int)sizeof(T);
 static int64_t beam_slices(const ee_beam_config& c, int E) { return ((int64_t)c.vocab + 256 * E - 1) / (256 * E); }
 static int beam_elements(const ee_beam_config& c) {
@@ -551,7 +551,7 @@ int launch_beam_select(const ee_beam_config& c, const void* logits, int64_t stri
     BeamParts parts;
     beam_parts(c, ws, &parts);
     const int E = beam_elements(c), n_slices = (int)beam_slices(c, E);
-    const dim3 grid((unsigned)(c.n_groups * c.beams * n_slices));
+    const dim3 grid((unsigned)(c.n_groups * c.beams * n_slices));           // below MOST_BLOCKS
     auto go = [&](auto* z) {
         using T = std::remove_const_t<std::remove_pointer_t<decltype(z)>>;
         auto kern = (size_t)c.vocab * sizeof(T) < 16 ? k_beam_slices<T, SMALL<T>, true> : E == LARGE ? k_beam_slices<T, LARGE, false> : k_beam_slices<T, SMALL<T>, false>;
@@ -560,6 +560,7 @@ int launch_beam_select(const ee_beam_config& c, const void* logits, int64_t stri
     if (c.dtype == EE_BF16) go((const bf16_t*)logits);
     else go((const float*)logits);
     EE_LAUNCH_CHECK();
+    // with 512 threads a request has more than two lists, so that a third of MOST_BLOCKS are not reached
     const bool few = (int64_t)c.beams * n_slices * parts.room <= FEW_PLACES;
     hipLaunchKernelGGL((few ? k_beam_join<true> : k_beam_join<false>), dim3((unsigned)c.n_groups), dim3(few ? 256 : 512), 0, s, parts, score, done, c.beams,
                        c.vocab, n_slices, c.keep, c.end_token, Ratio((uint32_t)parts.room), Ratio((uint32_t)n_slices), out);

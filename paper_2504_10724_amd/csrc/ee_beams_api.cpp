@@ -8,7 +8,7 @@ static int check_beams(const ee_beam_config* c) {
     if (c->vocab < 1 || c->vocab > 1 << 30) return ee_fail(EE_ERR_SHAPE, "ee_beam_select: vocab must be 1 to 2^30");
     if (c->dtype != EE_F32 && c->dtype != EE_BF16) return ee_fail(EE_ERR_DTYPE, "ee_beam_select: unknown dtype");
     if (c->end_token < -1 || c->end_token >= c->vocab) return ee_fail(EE_ERR_INVALID_ARG, "ee_beam_select: end_token outside the vocabulary");
-    if ((double)c->n_groups * c->beams * (c->vocab / 4096 + 1.0) > 2147483647.0)
+    if ((int64_t)c->n_groups * c->beams * ((c->vocab + (int64_t)BEAM_SLICE - 1) / BEAM_SLICE) >= MOST_BLOCKS)
         return ee_fail(EE_ERR_SHAPE, "ee_beam_select: more slices than a launch holds");
     return EE_OK;
 }

@@ -76,6 +76,8 @@ int  ee_fail(int code, const std::string& msg);
             return ee_fail(EE_ERR_HIP, std::string(#expr) + ": " + hipGetErrorString(_e)); \
     } while (0)
 #define EE_LAUNCH_CHECK()  EE_HIP_CHECK(hipGetLastError())
+// a launch's workgroups times 256 threads stay below 2^32
+constexpr int64_t MOST_BLOCKS = 1 << 24;
 
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

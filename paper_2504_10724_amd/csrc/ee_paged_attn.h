@@ -280,6 +280,4 @@ static inline size_t share_bytes(int hd) { return (size_t)hd * sizeof(float) + s
 
 int64_t f32_paged_columns(int hd, int64_t most_cols);       // of a workgroup
 int f32_paged_attention(AttnArgs a, char* ws, hipStream_t s);
-// a launch's workgroups times 256 threads stay below 2^32
-constexpr int64_t MOST_BLOCKS = 1 << 24;
 int launch_join(int dtype, const AttnArgs& a, int C, int64_t slots, hipStream_t s);

@@ -147,3 +147,15 @@ def test_default_streams_are_those_of_the_current_device(monkeypatch):
     assert paged._stream(0) == 0 and paged._stream(2) == 0x5000
     with pytest.raises(ee.EEError, match="device 0 is current"):
         paged._stream(1)
+
+
+@pytest.mark.parametrize("dtype", [ee.EE_F32, ee.EE_BF16])
+@pytest.mark.parametrize("kw", [dict(n_groups=2 ** 22, beams=4, keep=4, vocab=8), dict(n_groups=2 ** 24, beams=1, keep=1, vocab=1),
+                                dict(n_groups=2 ** 11, beams=2 ** 5, keep=1, vocab=2 ** 20), dict(n_groups=2 ** 11, beams=2 ** 5, keep=1, vocab=2 ** 20 - 4095)])
+def test_choices_of_more_slices_than_a_launch_holds(kw, dtype):
+    """2^24 workgroups of 256 threads are 2^32 threads, which no grid has; a request less is fine"""
+    lib, c, out = ee.load(), _beams(dtype=dtype, **kw), ee.ee_beam_choice(4096, 4096, 4096, None)
+    assert lib.ee_beam_workspace(C.byref(c)) == 0
+    assert lib.ee_beam_select(C.byref(c), DUMMY, c.vocab, DUMMY, None, C.byref(out), DUMMY, 1 << 60, None) == SHAPE
+    c.n_groups -= 1
+    assert lib.ee_beam_workspace(C.byref(c)) > 0
