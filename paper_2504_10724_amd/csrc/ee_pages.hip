@@ -580,7 +580,7 @@ int launch_pages_fork(const PagesView& v, const ForkView& f, hipStream_t s) {
         lds = std::max(lds, (size_t)a.rows * unit << a.state[k].shift);
     }
     const int64_t blocks = (f.to.n + a.rows - 1) / a.rows * tiles;
-    if (tiles > 0x7fffffff || blocks > 0x7fffffff) return ee_fail(EE_ERR_SHAPE, "ee_pages_fork: more workgroups than a launch holds");
+    if (tiles >= MOST_BLOCKS || blocks >= MOST_BLOCKS) return ee_fail(EE_ERR_SHAPE, "ee_pages_fork: more workgroups than a launch holds");
     a.tiles = (int)tiles;
     hipLaunchKernelGGL(k_pages_fork, dim3((unsigned)blocks), dim3(FORK), kept + lds, s, a);
     EE_LAUNCH_CHECK();

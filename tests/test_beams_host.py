@@ -159,3 +159,18 @@ def test_choices_of_more_slices_than_a_launch_holds(kw, dtype):
     assert lib.ee_beam_select(C.byref(c), DUMMY, c.vocab, DUMMY, None, C.byref(out), DUMMY, 1 << 60, None) == SHAPE
     c.n_groups -= 1
     assert lib.ee_beam_workspace(C.byref(c)) > 0
+
+
+def test_forks_of_more_workgroups_than_a_launch_holds():
+    """rows that are groups of one: a workgroup for each one's lengths and one for its column"""
+    lib, g = ee.load(), C.c_void_p()
+    p = _cache(lib)
+    assert lib.ee_pages_bind(p, 8, DUMMY, 1 << 40, C.byref(g)) == ee.EE_OK
+    far = [C.c_void_p(k << 32) for k in (1, 2, 3, 4)]
+    t = ee.ee_page_table(2 ** 23, 1, far[0], far[1])
+    assert lib.ee_pages_fork(g, C.byref(t), None, far[2], None, 1, None, 0, None, None) == SHAPE
+    t = ee.ee_page_table(2 ** 22, 2, far[0], far[1])
+    states = (ee.ee_rows * 1)(ee.ee_rows(far[3], 8192, 8192))
+    assert lib.ee_pages_fork(g, C.byref(t), None, far[2], None, 1, states, 1, None, None) == SHAPE
+    lib.ee_pages_destroy(g)
+    lib.ee_paged_destroy(p)
