@@ -693,7 +693,8 @@ typedef struct {
     int32_t end_token;   /* -1: no beam ends                                            */
 } ee_beam_config;
 
-/* The chosen: arrays [n_groups][keep].  With keep == beams, score and done may be the arrays that were read. */
+/* The chosen: arrays [n_groups][keep], apart from each other, the workspace and what is read; with keep == beams, score and done may be the
+ * arrays that were read. */
 typedef struct {
     float*   dev_score;
     int32_t* dev_parent;   /* beam of the request: 0 .. beams-1                           */

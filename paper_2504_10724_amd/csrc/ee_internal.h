@@ -81,6 +81,16 @@ constexpr int64_t MOST_BLOCKS = 1 << 24;
 
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
+// bytes from `p` on (null: none), and whether two of them share any
+struct Span {
+    const void* p;
+    size_t bytes;
+    bool meets(const Span& o) const {
+        const uintptr_t a = (uintptr_t)p, b = (uintptr_t)o.p;
+        return p && o.p && (a <= b ? b - a < bytes && o.bytes > 0 : a - b < o.bytes && bytes > 0);
+    }
+};
+
 // ----------------------------------------------------------------- kernel timing (opt-in)
 // Every launch of a kernel class whose bit is set in the mask is bracketed by a pair of
 // HIP events on the launch stream; ee_timing_read adds up the elapsed times.

@@ -174,3 +174,27 @@ def test_forks_of_more_workgroups_than_a_launch_holds():
     assert lib.ee_pages_fork(g, C.byref(t), None, far[2], None, 1, states, 1, None, None) == SHAPE
     lib.ee_pages_destroy(g)
     lib.ee_paged_destroy(p)
+
+
+def test_choices_whose_arrays_overlap():
+    """a request's workgroup writes its results while others still read: results lie apart from each other and from what is read, but for the
+    scores and the ended beams themselves in place"""
+    lib, c = ee.load(), _beams(end_token=3)                                        # 2 requests of 4 beams, 4 kept: arrays of 32 and of 8 bytes
+    need = lib.ee_beam_workspace(C.byref(c))
+    base = dict(score=1 << 20, parent=2 << 20, token=3 << 20, done=4 << 20, in_score=5 << 20, in_done=6 << 20, ws=1 << 30)
+
+    def call(**kw):
+        a = dict(base, **kw)
+        out = ee.ee_beam_choice(a["score"], a["parent"], a["token"], a["done"])
+        return lib.ee_beam_select(C.byref(c), DUMMY, 1000, C.c_void_p(a["in_score"]), C.c_void_p(a["in_done"]), C.byref(out), C.c_void_p(a["ws"]), need, None)
+    sizes = dict(score=32, parent=32, token=32, done=8, in_score=32, in_done=8)
+    assert need % 256 == 0
+    for one, n in sizes.items():
+        for other, m in sizes.items():
+            if one == other or {one, other} == {"in_score", "in_done"}:            # both only read
+                continue
+            for by in (4 - n, 4, m - 4, *(() if {one, other} in ({"score", "in_score"}, {"done", "in_done"}) else (0,))):
+                assert call(**{one: base[other] + by}) == BAD, (one, other, by)
+                assert b"memory" in lib.ee_last_error()
+        for by in (4 - n, 0, need - 4):
+            assert call(**{one: base["ws"] + by}) == BAD, (one, by)
