@@ -660,8 +660,8 @@ int ee_pages_grow(ee_pages* g, const ee_page_table* t, const int32_t* dev_new, i
  * states: further rows that go along in place (tokens so far, hidden states); those of a parent of -1 stay as they are.
  * Parents, lengths to keep, tables and states lie apart from each other.
  * Errors: EE_ERR_SHAPE if to's width is below from's, n_seqs is no multiple of group, with group > 0 the tables' n_seqs
- * differ, more than EE_PAGES_MAX_GROUP rows are forked in place among each other, or the call takes 2^24 workgroups or more; EE_ERR_INVALID_ARG (states without a fork in place; tables that
- * share only part of their memory). */
+ * differ, more than EE_PAGES_MAX_GROUP rows are forked in place among each other, or the call takes 2^24 workgroups or more; EE_ERR_INVALID_ARG (states without a fork in place; arrays
+ * that share part of their memory). */
 int ee_pages_fork(ee_pages* g, const ee_page_table* to, const ee_page_table* from, const int32_t* dev_parent, const int32_t* dev_keep,
                   int group, const ee_rows* states, int n_states, int32_t* dev_status, void* stream);
 

@@ -56,6 +56,28 @@ static int check_table(const std::string& who, const ee_pages* g, const ee_page_
     return EE_OK;
 }
 
+// `n` runs of `bytes` bytes, `stride` apart, none in another (null: none)
+struct Runs {
+    const void* p;
+    int64_t bytes, n, stride;
+    static Runs one(const void* p, int64_t bytes) { return Runs{p, bytes, 1, bytes}; }
+    uint64_t at(int64_t i) const { return (uint64_t)(uintptr_t)p + (uint64_t)i * (uint64_t)stride; }
+    Span span() const { return Span{p, (size_t)(at(n - 1) + bytes - at(0))}; }
+};
+// whether any byte is in both: from run to run of either that ends behind the other's present one
+static bool meet(const Runs& a, const Runs& b) {
+    if (!a.p || !b.p || a.bytes < 1 || b.bytes < 1 || !a.span().meets(b.span())) return false;
+    int64_t i = 0, j = 0;
+    // runs that far apart alike lie to each other the same way in every period
+    for (int turn = 0; i < a.n && j < b.n && (turn < 6 || a.stride != b.stride); ++turn) {
+        const uint64_t x = a.at(i), y = b.at(j);
+        if (x + a.bytes <= y)      i += (int64_t)((y - x - a.bytes) / a.stride) + 1;
+        else if (y + b.bytes <= x) j += (int64_t)((x - y - b.bytes) / b.stride) + 1;
+        else return true;
+    }
+    return false;
+}
+
 extern "C" {
 
 size_t ee_pages_state_bytes(const ee_paged* p, int max_seqs) {
@@ -116,8 +138,14 @@ int ee_pages_fork(ee_pages* g, const ee_page_table* to, const ee_page_table* fro
     if (n_states > 0 && !in_place) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: states go along in place only");
     if (n_states > 0 && !states) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: null pointer");
     // read by some workgroups when others have written
-    auto written = [&](const void* p) { return p && (p == to->dev_kv_len || p == to->dev_pages); };
-    if (written(dev_parent) || written(dev_keep)) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: parents or lengths are the table's own memory");
+    const int64_t n = to->n_seqs;
+    auto entries = [](const ee_page_table* t) { return Runs::one(t->dev_pages, 4ll * t->n_seqs * t->pages_per_seq); };
+    auto lengths = [](const ee_page_table* t) { return Runs::one(t->dev_kv_len, 4ll * t->n_seqs); };
+    const Runs parent = Runs::one(dev_parent, 4 * n), keep = Runs::one(dev_keep, 4 * n);
+    auto written = [&](const Runs& r) { return meet(r, entries(to)) || meet(r, lengths(to)); };
+    if (meet(entries(to), lengths(to)) || (!in_place && (written(entries(from)) || written(lengths(from)))))
+        return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: the tables share part of their memory");
+    if (written(parent) || written(keep)) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: parents or lengths are the table's own memory");
     ForkView f;
     f.to = make_table(to);
     f.from = make_table(from);
@@ -132,11 +160,14 @@ int ee_pages_fork(ee_pages* g, const ee_page_table* to, const ee_page_table* fro
         if (r.bytes < 0) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: negative count");
         if (r.bytes == 0) continue;
         if (!r.dev) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: null pointer");
-        if (written(r.dev) || r.dev == dev_parent || r.dev == dev_keep)
+        if (n > 1 && r.stride < r.bytes) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: rows of a state share their memory");
+        auto runs = [&](const void* p, int64_t bytes, int64_t stride) { return Runs{p, bytes, n, n > 1 ? stride : bytes}; };
+        const Runs mine = runs(r.dev, r.bytes, r.stride);
+        if (written(mine) || meet(mine, parent) || meet(mine, keep))
             return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: a state is the table's, the parents' or the lengths' memory");
         for (int j = 0; j < f.n_states; ++j)
-            if (f.states[j].p == r.dev) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: a state is given twice");
-        if (to->n_seqs > 1 && r.stride < r.bytes) return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: rows of a state share their memory");
+            if (meet(mine, runs(f.states[j].p, f.states[j].bytes, f.states[j].stride)))
+                return ee_fail(EE_ERR_INVALID_ARG, "ee_pages_fork: states share their memory");
         f.states[f.n_states++] = StateRows{(char*)r.dev, r.stride, r.bytes};
     }
     return launch_pages_fork(make_pages(g), f, as_stream(stream));

@@ -198,3 +198,39 @@ def test_choices_whose_arrays_overlap():
                 assert b"memory" in lib.ee_last_error()
         for by in (4 - n, 0, need - 4):
             assert call(**{one: base["ws"] + by}) == BAD, (one, by)
+
+
+def test_forks_whose_arrays_overlap():
+    """workgroups read parents, lengths to keep and the other table while others write: these, the table and the states lie apart, to the byte"""
+    lib, g = ee.load(), C.c_void_p()
+    p = _cache(lib)
+    assert lib.ee_pages_bind(p, 8, DUMMY, 1 << 40, C.byref(g)) == ee.EE_OK
+    n, width = 6, 5
+    base = dict(pages=1 << 20, kv_len=2 << 20, parent=3 << 20, keep=4 << 20, other_pages=5 << 20, other_len=6 << 20)
+    sizes = dict(pages=4 * n * width, kv_len=4 * n, parent=4 * n, keep=4 * n, other_pages=4 * n * width, other_len=4 * n)
+
+    def fork(states=(), source=False, **kw):
+        a = dict(base, **kw)
+        t, s = ee.ee_page_table(n, width, a["pages"], a["kv_len"]), ee.ee_page_table(n, width, a["other_pages"], a["other_len"])
+        rows = (ee.ee_rows * max(len(states), 1))(*states)
+        return lib.ee_pages_fork(g, C.byref(t), C.byref(s) if source else None, C.c_void_p(a["parent"]), C.c_void_p(a["keep"]), 0, rows, len(states), None, None)
+
+    def refused(*a, **kw):
+        code = fork(*a, **kw)
+        assert code == BAD and b"memory" in lib.ee_last_error(), (a, kw, code)
+    for one in ("pages", "kv_len"):
+        for other in ("parent", "keep", "other_pages", "other_len"):
+            for by in (4 - sizes[one], 0, sizes[other] - 4):
+                refused(source=True, **{one: base[other] + by})
+    refused(pages=base["kv_len"] - 4)
+    for a, at in base.items():                                                     # rows of 12 bytes every 16
+        if not a.startswith("other"):
+            for by in (1 - (16 * (n - 1) + 12), -28, 0, sizes[a] - 1):
+                refused(states=[ee.ee_rows(at + by, 16, 12)])
+    x = 8 << 20
+    for b in ((x + 1, 16, 4), (x + 11, 16, 1), (x + 12, 16, 5), (x - 4, 16, 5), (x + 5 * 16 + 11, 16, 4), (x - 5 * 16, 16, 1), (x + 12, 20, 4), (x + 13, 17, 1),
+              (x - 100, 24, 24), (x - 1000, 200, 5)):
+        refused(states=[ee.ee_rows(x, 16, 12), ee.ee_rows(*b)])
+        refused(states=[ee.ee_rows(*b), ee.ee_rows(x, 16, 12)])
+    lib.ee_pages_destroy(g)
+    lib.ee_paged_destroy(p)

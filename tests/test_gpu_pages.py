@@ -402,3 +402,19 @@ def test_rows_grow_by_their_own_lengths(n):
         a.pages.grow(t[0], t[0].kv_len, status=a.status)
         a.book.grow(t[1], list(t[1].len))
         a.check()
+
+
+def test_states_beside_each_other():
+    """columns of one tensor as states of their own: their rows lie between each other's, not in them; one column more is refused"""
+    print("[case] states beside each other", flush=True)
+    c = Pair(10, 32)
+    t = c.table(6, 2)
+    x = torch.arange(6 * 40, dtype=torch.int32, device="cuda").view(6, 40)
+    want, parent = x.clone(), [3, 3, 0, 1, 5, 2]
+    want[:, 1:9], want[:, 12:], want[:, 9] = x[parent, 1:9], x[parent, 12:], x[parent, 9]
+    c.pages.fork(t[0], _i32(parent), rows=[x[:, 1:9], x[:, 12:], x[:, 9:10]])
+    assert torch.equal(x, want)
+    for rows in ([x[:, :9], x[:, 8:]], [x[:, 8:9], x], [x.view(-1)[4:40].view(6, 6), x[:, 39:]], [x[:, 3], x[:, 3:]]):
+        with pytest.raises(ee.EEError):
+            c.pages.fork(t[0], _i32(parent), rows=rows)
+    assert torch.equal(x, want)
