@@ -10,7 +10,7 @@ from collections import namedtuple
 import torch
 
 from . import capi as ee
-from .paged import _DTYPES, _lost, _number, _refuse, _stream
+from .paged import _DTYPES, _keep_derivatives, _number, _refuse, _stream
 
 #: score (float32), parent (a beam of the request; int32), token (int32), each [n_groups][keep]; done (uint8) or None
 Selection = namedtuple("Selection", "score parent token done")
@@ -53,8 +53,7 @@ def select(logits, score, n_beams, *, keep=None, done=None, end_token=-1, out=No
     dev = logits.get_device()
     if dev < 0:
         _refuse("select: logits must be on a device")
-    if (logits.requires_grad or score.requires_grad) and torch.is_grad_enabled():
-        _lost("select")
+    _keep_derivatives("select", logits, score)
     n_groups = rows // n_beams
     flat = (rows,)
     if out is None:

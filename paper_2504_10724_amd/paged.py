@@ -19,6 +19,7 @@ import ctypes as C
 import struct
 
 import torch
+from torch.autograd import forward_ad
 
 from . import capi as ee
 from .session import _raw_stream
@@ -78,9 +79,15 @@ def _int32(t, what, n, device):
     return t
 
 
-def _lost(what):
-    """the operator has no gradient, and a result that the caller provides takes no part in a graph: nothing that needs one gets lost"""
-    _refuse(f"{what}: a tensor requires a gradient that is not computed; call it under torch.no_grad() or on detached tensors")
+def _keep_derivatives(what, *tensors):
+    """The operator has no gradient, and a result that the caller provides takes no part in a graph: where a tensor needs one, or carries the
+    tangent of a forward-mode derivative (no_grad leaves those on), the call is refused and nothing gets lost."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t.requires_grad:
+                _refuse(f"{what}: a tensor requires a gradient that is not computed; call it under torch.no_grad() or on detached tensors")
+    if getattr(forward_ad, "_current_level", 0) >= 0 and any(forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        _refuse(f"{what}: a tensor carries a forward-mode gradient that is not computed; call it on detached tensors")
 
 
 class _Turn(torch.autograd.Function):
@@ -134,11 +141,11 @@ class Rope:
         if len(shape) != 3 or dtype not in _DTYPES or shape[2] != self.cfg.head_dim:
             _refuse(f"Rope.apply: x must be [tokens][heads][{self.cfg.head_dim}] of float32 or bfloat16, got {tuple(shape)} of {dtype}")
         if out is not None:
-            if (x.requires_grad or out.requires_grad) and torch.is_grad_enabled():
-                _lost("Rope.apply with out")
+            _keep_derivatives("Rope.apply with out", x, out)
         elif x.requires_grad and torch.is_grad_enabled():
             return _Turn.apply(x, pos, self, inverse, status)
         else:
+            _keep_derivatives("Rope.apply", x)
             out = torch.empty(shape, dtype=dtype, device=x.device)
         n, heads, _ = shape
         dev = self.device
@@ -212,8 +219,7 @@ def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
         _refuse("append: the rotary table is closed")
     if not -_MOST <= layer <= _MOST:
         _number("append", layer)
-    if (k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
-        _lost("append")
+    _keep_derivatives("append", k, v)
     kh, vh = _heads(k, "append", shape, dtype, dev), _heads(v, "append", shape, dtype, dev)
     qh = qo = None
     n_q = 0
@@ -222,8 +228,7 @@ def append(kv, layer, step, k, v, *, rope=None, q=None, q_out=None):
         shape = (step.n_tokens, n_q, kv.head_dim)
         if q_out is None:
             q_out = torch.empty(shape, dtype=dtype, device=q.device)
-        if (q.requires_grad or q_out.requires_grad) and torch.is_grad_enabled():
-            _lost("append")
+        _keep_derivatives("append", q, q_out)
         qh, qo = _heads(q, "append", shape, dtype, dev), _heads(q_out, "append", shape, dtype, dev, True)
     ee.check(kv.lib.ee_paged_append(kv.h, layer, step.ref, None if rope is None else rope.h, kh, vh, qh, qo, n_q, _stream(dev)))
     return q_out
@@ -244,8 +249,7 @@ def attend(kv, layer, step, q, *, out=None, scale=None, window=0, workspace=None
         window = _MOST                                       # wider than any sequence
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=q.device)
-    if (q.requires_grad or out.requires_grad) and torch.is_grad_enabled():
-        _lost("attend")
+    _keep_derivatives("attend", q, out)
     if workspace is None:
         workspace = kv.workspace(step, heads)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
@@ -329,12 +333,12 @@ class Pages:
         positions; with `group`, parents are numbered inside groups of that many rows.  rows: tensors [n_seqs][...] whose rows go along."""
         self._check("Pages.fork", table, *(() if source is None else (source,)))
         _number("Pages.fork", group)
-        packed = []
+        packed, rows = [], tuple(rows)
+        if rows:
+            _keep_derivatives("Pages.fork", *rows)
         for x in rows:
             if x.dim() < 1 or x.shape[0] != table.n_seqs or x.get_device() != self.device or not (x.is_contiguous() or x[0].is_contiguous()):
                 _refuse(f"Pages.fork: rows must be [{table.n_seqs}][...] on device {self.device}, each row contiguous, got {tuple(x.shape)} on {x.device}")
-            if x.requires_grad and torch.is_grad_enabled():
-                _lost("Pages.fork")
             size = x.element_size()
             packed.append(_pack_rows(x.data_ptr(), x.stride(0) * size, x.numel() // max(table.n_seqs, 1) * size))
         ee.check(self.lib.ee_pages_fork(self.h, table.ref, None if source is None else source.ref, self._ints(parent, "Pages.fork: parent", table.n_seqs),

@@ -287,3 +287,20 @@ def test_a_chosen_candidate_has_a_finite_score(vocab, dtype):
         score[:aside] = -math.inf                            # the better ones are put aside
     none = B.select(z[:, :1].cuda(), score.cuda(), 4, keep=6)              # places that no candidate is left for
     assert none.score[0].tolist() == [lowest] * 4 + [-math.inf] * 2 and none.parent[0].tolist() == [0, 1, 2, 3, -1, -1]
+
+
+def test_tangents_are_not_lost():
+    """tensors of forward-mode derivatives, which no call computes, under no_grad too"""
+    print("[case] tangents", flush=True)
+    from torch.autograd import forward_ad
+    z, score = torch.zeros(8, 100, device="cuda"), torch.zeros(8, device="cuda")
+    with forward_ad.dual_level():
+        for call in (lambda: B.select(forward_ad.make_dual(z, torch.ones_like(z)), score, 4),
+                     lambda: B.select(z, forward_ad.make_dual(score, torch.ones_like(score)), 4)):
+            with pytest.raises(ee.EEError, match="gradient"):
+                call()
+            with torch.no_grad(), pytest.raises(ee.EEError, match="gradient"):
+                call()
+        dual = forward_ad.make_dual(z, torch.ones_like(z))
+        B.select(dual.detach(), score, 4)
+        B.select(z, score, 4)

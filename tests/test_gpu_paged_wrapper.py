@@ -188,3 +188,22 @@ def test_results_whose_rows_share_memory_are_refused():
     one = c.q[:1]                                                      # a single row shares with nobody, whatever its stride
     out = torch.empty(4, 64, dtype=one.dtype, device="cuda").as_strided((1, 4, 64), (0, 64, 1))
     assert torch.equal(rope.apply(one, pos[:1], out=out), rope.apply(one, pos[:1]))
+
+
+def test_tangents_that_nothing_computes_are_refused():
+    """forward-mode derivatives, which no_grad leaves on"""
+    print("[case] tangents", flush=True)
+    from torch.autograd import forward_ad
+    c = Call()
+    rope, pos = P.Rope(64, 3000), _i32([1, 2])
+    with forward_ad.dual_level():
+        q, k = (forward_ad.make_dual(t, torch.ones_like(t)) for t in (c.q, c.k))
+        calls = [lambda: rope.apply(q, pos), lambda: rope.apply(q, pos, out=torch.empty_like(c.q)), lambda: P.append(c.kv, 1, c.step, k, c.k),
+                 lambda: P.append(c.kv, 1, c.step, c.k, k), lambda: P.append(c.kv, 1, c.step, c.k, c.k, q=q), lambda: P.attend(c.kv, 1, c.step, q)]
+        for call in calls:
+            with pytest.raises(ee.EEError, match="gradient"):
+                call()
+            with torch.no_grad(), pytest.raises(ee.EEError, match="gradient"):
+                call()
+        P.append(c.kv, 1, c.step, k.detach(), c.k, rope=rope)
+        P.attend(c.kv, 1, c.step, q.detach())

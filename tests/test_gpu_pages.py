@@ -418,3 +418,19 @@ def test_states_beside_each_other():
         with pytest.raises(ee.EEError):
             c.pages.fork(t[0], _i32(parent), rows=rows)
     assert torch.equal(x, want)
+
+
+def test_tangents_of_states_are_not_lost():
+    print("[case] tangents", flush=True)
+    from torch.autograd import forward_ad
+    c = Pair(10, 32)
+    t, x = c.table(4, 2), torch.arange(8.0, device="cuda").view(4, 2)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, torch.ones_like(x))
+        for _ in range(2):
+            with pytest.raises(ee.EEError, match="gradient"):
+                c.pages.fork(t[0], _i32([1, 0, 2, 2]), rows=[dual])
+            with torch.no_grad(), pytest.raises(ee.EEError, match="gradient"):
+                c.pages.fork(t[0], _i32([1, 0, 2, 2]), rows=[dual])
+        c.pages.fork(t[0], _i32([1, 0, 2, 2]), rows=[dual.detach()])
+    assert x.tolist() == [[2.0, 3.0], [0.0, 1.0], [4.0, 5.0], [4.0, 5.0]]
