@@ -304,3 +304,21 @@ def test_tangents_are_not_lost():
         dual = forward_ad.make_dual(z, torch.ones_like(z))
         B.select(dual.detach(), score, 4)
         B.select(z, score, 4)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("keep", [1, 20, 128])
+@pytest.mark.parametrize("values", ["normal", "equal", "scores"])
+def test_more_lists_than_are_collected(values, keep, dtype):
+    """640 slices of one request: all of them in the running, or those of some beams; some beams have ended"""
+    print(f"[case] many lists {values} {keep} {dtype}", flush=True)
+    beams, vocab = 64, 40000
+    z, score = _inputs(1, beams, vocab, dtype, keep)
+    done = (torch.arange(beams) % 9 == 5).to(torch.uint8)
+    if values != "normal":
+        z.zero_()
+    if values == "equal":
+        score = torch.full((beams,), -3.0)
+        score[done.bool()] = -3.0 - 20.0                     # behind all others
+    want = R.choose(z, score, beams, keep, done, 11)
+    _check(B.select(z.cuda(), score.cuda(), beams, keep=keep, done=done.cuda(), end_token=11), want)
