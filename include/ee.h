@@ -680,7 +680,8 @@ int ee_pages_compact(ee_pages* g, const ee_page_table* tables, int n_tables, voi
  * The choice of a search's next beams from the logits of its present ones (an exit head's, say).  Request r has the rows r * beams .. of the
  * logits; beam b's candidate v counts  score[b] + z[b][v] - ln sum_u exp z[b][u].  The `keep` best of a request's beams * vocab
  * candidates come out in falling order.  The sums and the candidates' values are held in 64 bits; values that are equal there go by the
- * smaller b, then the larger logit, then the smaller v.  A beam that has ended (dev_done) has one candidate: end_token, at its score.
+ * smaller b, then the larger logit, then the smaller v.  An exponential is off by less than 1e-12 of itself, so that candidates of different
+ * beams whose values differ by less may come out the other way round; in a beam the order is that of the logits.  A beam that has ended (dev_done) has one candidate: end_token, at its score.
  * A beam whose score or logarithm is not finite (all logits -inf, a NaN or +inf among them) has none, nor has a logit of -inf.
  * A chosen candidate's score is finite: a value below fp32's lowest number (masks of it taken twice) comes out as that number.
  * Places that no candidate is left for get score -inf, parent -1, token -1.  A search starts with one live beam: scores 0, -inf, .. */

@@ -178,10 +178,11 @@ __device__ __forceinline__ void shrink(float* value, int* place, int n, int keep
 
 // Sums are taken of exp(z) itself where a wave's logits lie in -700 .. 600 (fp64 holds that), so that they wait for no maximum and NaN need
 // no look; else of exp(z - the lane's largest).  Candidates: what reaches a bound that `keep` of the threads' largest reach.
-// 512 rows of 131071 fp32 logits: 77 to 79 us, 3.4 TB/s (a pure read of them 43).  Bound by vector instructions: 27 an element, of which the sum in fp64 is
+// 512 rows of 131071 fp32 logits: 65 us behind each other without the second launch, 4.1 TB/s; 79 to 87 each by itself under the profiler (a pure read of
+// them 43).  Bound by vector instructions: 27 an element, of which the sum in fp64 is
 // half (with an exponential in fp32 59 us), the rest a wave's work over its 16 elements a lane; they fill 68 % of the cycles.  Of the tries when it took
 // 83, 32 elements a lane took 87, slices streamed tile by tile under a bound that rises 86 a wave's and 177 a workgroup's.  Registers for eight
-// waves a SIMD: 84.3 us a call for 87.0.  256 rows of 32000 bf16: 12.3; 8 of 2048 fp32: 4.1.
+// waves a SIMD: 84.3 us a call for 87.0.  256 rows of 32000 bf16: 12 under the profiler, 11 a call without the second launch; 8 of 2048 fp32: 4.1.
 template <class T, int E, bool SHORT>
 __global__ void __launch_bounds__(256, 8)
 k_beam_slices(const T* __restrict__ logits, int64_t stride, const uint8_t* __restrict__ done, int vocab, int n_slices, int keep, BeamParts parts) {
@@ -357,8 +358,9 @@ __device__ __forceinline__ bool better(const Candidate& a, const Candidate& b) {
 
 // A number that `keep` of the slices' largest reach leaves out most lists at once; where there are fewer slices than that, the threads' largest of
 // the lists' values give it.  Bound by trips to memory one behind the other: FEW, with up to two list places a thread, makes one, all
-// lists being on their way beside the sums; else the lists that are left come behind their first.  8 lists of 14 places 5.4 us,
-// 160 of 23 7.2 (8.2 by 1024 threads instead of 512), 512 of 56 in each of 32 requests 20.
+// lists being on their way beside the sums; else the lists that are left come behind their first.  8 lists of 14 places 4.9 us,
+// 160 of 23 5.7, 512 of 56 in each of 32 requests 14.9 (7.2 and 20 when the sort read whole candidates instead of keys; 1024 threads instead of
+// 512 took 8.2 for that 7.2).
 constexpr int FEW_PLACES = 512, OWN = FEW_PLACES / 256;
 // j / d by ceil(2^32 / d), exact where j * d is below 2^32
 struct Ratio {
@@ -523,7 +525,11 @@ k_beam_join(BeamParts parts, const float* score, const uint8_t* done, int beams,
         for (int c = m + tid; c < keep; c += JOIN) put(c, Candidate{}, false);
         return;
     }
-    // many equal ones: the next best behind the last, `keep` times
+    // More than CANDIDATES: the next best behind the last, `keep` times, each time of all places of all lists.  Equal candidates come here, and
+    // requests of which no more than about `keep` lists hold anything worth having: the bound is the worst of these lists' firsts then, and most
+    // places of the best lists reach it.  A wide search's first step is such a call, with one live beam (32 requests of 16 beams over 131071, 32
+    // kept: 767 us, with all beams live 91; one of 64 beams, 128 kept: 36 ms for 93 us), and one that keeps as many as it has lists
+    // (32 beams over 1000 tokens, 32 kept: 132 us, its first step 14).
     Candidate last{INFINITY, -1, -1, 0.f};
     for (int k = 0; k < keep; ++k) {
         Candidate v{-INFINITY, 0x7fffffff, -1, 0.f};

@@ -302,9 +302,10 @@ k_pages_copy(PoolView from, PoolView to, const int32_t* __restrict__ src, const 
     }
 }
 
-// Groups: eight workgroups a CU (54.6 us for beams_70b_b256's 279 MB, four 54.2, two 58.1).  Whole pages past the caches: two a CU of 16 KB each, or
-// as many bytes under way of smaller pages (173 pages of 4 MB: 269 us, 5.4 TB/s, with one a CU 262, four 276, eight 276; through the caches two 284,
-// eight 285).
+// Groups: eight workgroups a CU (54.6 us for the 262 MB that beams_70b_b256 reads and writes, four 54.2, two 58.1).  Whole pages: two a CU of 16 KB
+// each, or as many bytes under way of smaller pages.  That is the middle between many pages and few, in us with two a CU and with one: 173 pages of
+// 4 MB 269 and 262 (four 276, eight 276), 1000 of 2 MB 817 and 799, 4 of 4 MB 7.1 and 7.6, 10 of 2 MB 8.2 and 8.7, 4000 of 16 KB 27.2 and 33.4,
+// 1000 of 16 KB 7.5 and 9.0.
 static unsigned copy_grid(double items, double most) { return (unsigned)std::max(1.0, std::min(items, most)); }
 static unsigned whole_grid(const PoolView& p, double pages) {
     return copy_grid(pages * p.n_layers * ((p.page + PIECE - 1) / PIECE), std::min(2048.0, 512.0 * PIECE / std::min<int64_t>(PIECE, p.page)));
@@ -641,7 +642,8 @@ int launch_pages_compact(const PagesView& v, const PoolView& pool, const TableVi
         entries += (double)tables[i].n * tables[i].width;
     }
     const int n_rename = (int)std::min(256.0, (entries + 1023) / 1024);
-    // how many pages move is known on the device only
+    // How many pages move is known on the device only, so the pool decides: of 1200 pages of 2 MB 2, 8 and 100 move in 4.2, 9.3 and 73 us past the
+    // caches, through them in 4.4, 6.6 and 80; compact_70b_b96's moves in 310 and 329.
     const bool once = (double)v.n_pages * pool.n_layers * pool.page > CACHED_BYTES;
     hipLaunchKernelGGL((once ? k_pages_copy<true> : k_pages_copy<false>), dim3(whole_grid(pool, v.n_pages / 2 + 1) + n_rename), dim3(256), 0, s, pool, pool,
                        v.src, v.dst, v.n_moves, 0, (int32_t*)nullptr, t, v.name, n_rename);
